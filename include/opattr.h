@@ -33,6 +33,9 @@
  *    caller queues on the stream before or after a call keeps its order.
  *  - Each call of the library is one NVTX range named after its entry point
  *    (visible on an Nsight Systems timeline).
+ *  - The attention operators at the end of this header do not wait: they
+ *    return once their work is on the stream, and what they find wrong on the
+ *    device is kept for opattr_check.
  *  - n == 0 is valid everywhere and yields empty results.
  *  - Return value: negative = error (outputs undefined; the context stays
  *    usable except after OPATTR_E_CUDA, after which it must be destroyed),
@@ -61,7 +64,8 @@ typedef enum {
     OPATTR_E_CUDA = -5,            /* a CUDA call failed; destroy the context */
     OPATTR_E_OOM = -6,             /* device scratch could not be allocated */
     OPATTR_E_TIMEOUT = -7,         /* a bounded device-side wait gave up */
-    OPATTR_E_STATE = -8            /* the context is unusable (after OPATTR_E_CUDA) */
+    OPATTR_E_STATE = -8,           /* the context is unusable (after OPATTR_E_CUDA) */
+    OPATTR_E_PAGES = -9            /* the paged cache has no free page left (opattr_check) */
 } opattr_status;
 
 /* What to do when a kernel name is launched a different number of times in
@@ -498,6 +502,136 @@ int64_t opattr_launch_count(const opattr_ctx *ctx);
 opattr_status opattr_match_noalloc(const opattr_kernels *kernels, const opattr_ncu *ncu,
                                    opattr_mismatch_mode mismatch, int32_t *ncu_idx_of_kernel, uint8_t *match_kind,
                                    opattr_match_summary *host_summary, void *cuda_stream);
+
+/* ---- Attention, and the paged cache under it ----
+ * What a serving program puts in the place of the attention kernels that a
+ * profile points at (Sec. 4.5 takes scaled-dot-product attention as a case
+ * study), and a workload whose bytes and operations per launch are known.
+ *
+ * These calls order their work on the context's stream and do not wait for it
+ * (they can be captured into a CUDA graph once a first call of the same or a
+ * larger size has made the scratch).  Sizes and pointers are checked at the
+ * call; offsets, sequence ids, lengths and page numbers live on the device
+ * and are checked there.  A call that finds one of those out of range does
+ * nothing (the cache's calls), or leaves out the rows concerned (the two
+ * attention calls: a sequence id or length out of range gives rows of zeros,
+ * a page out of range counts as not seen); opattr_check tells.
+ *
+ * Values are bfloat16 or IEEE half; products are summed, and the softmax is
+ * held, in 32 bits; its weights are rounded to the values' type before they
+ * are multiplied with the values, and the results once at the end.  A key
+ * outside a row's mask has no influence on it, whatever it holds. */
+typedef enum { OPATTR_BF16 = 0, OPATTR_F16 = 1 } opattr_dtype;
+
+/* Rows of heads, DEVICE memory: element e of head h of row t is
+ * data[t * token_stride + h * head_stride + e].  Strides count elements and
+ * are multiples of 8; data is 16-byte aligned. */
+typedef struct {
+    void *data;
+    int64_t token_stride;
+    int64_t head_stride;
+} opattr_rows;
+
+/* Attention over packed sequences.  Sequence b has the query rows
+ * q_offsets[b] .. q_offsets[b + 1] and the key and value rows k_offsets[b] ..
+ * k_offsets[b + 1]; query head h reads key head h / (q_heads / kv_heads).
+ * With `causal`, the sequence's last query sees its last key, the one before
+ * it one key fewer, and so on: keys may begin before the queries (a prompt
+ * taken in pieces).  A row that sees no key gets zeros, and -inf as its lse.
+ *   q, out     rows of q_heads heads, q_tokens of them
+ *   k, v       rows of kv_heads heads, k_tokens of them
+ *   q_offsets  i32[n_seqs + 1] device, from 0 to q_tokens, not decreasing
+ *   k_offsets  i32[n_seqs + 1] device, from 0 to k_tokens; may be q_offsets
+ *   lse        f32[q_tokens * q_heads] device: log of the row's sum of
+ *              exp(scale * q.k) over its keys; may be NULL
+ * head_dim is a multiple of 8 from 8 to 128. */
+typedef struct {
+    int32_t dtype;                 /* opattr_dtype of q, k, v and out */
+    int32_t n_seqs;
+    int32_t q_heads;
+    int32_t kv_heads;
+    int32_t head_dim;
+    int32_t causal;
+    float scale;
+    int32_t reserved;
+    int64_t q_tokens;
+    int64_t k_tokens;
+    opattr_rows q, k, v, out;
+    const int32_t *q_offsets;
+    const int32_t *k_offsets;
+    float *lse;
+} opattr_prompt;
+
+/* Errors: OPATTR_E_INVALID_ARG (type, sizes, alignment), OPATTR_E_OOM,
+ * OPATTR_E_CUDA. */
+opattr_status opattr_attention(opattr_ctx *ctx, const opattr_prompt *args);
+
+/* A paged key-value cache; everything in it is the caller's DEVICE memory.
+ *   k_pages, v_pages  [n_pages][kv_heads][page_size][head_dim], 16-byte aligned
+ *   table    i32[n_seqs][pages_per_seq]: page of each page_size tokens of a
+ *            sequence; -1 past its length
+ *   length   i32[n_seqs]: tokens that a sequence has
+ *   refs     i32[n_pages]: sequences that hold a page; 0: it is free
+ *   low      i32[1]: no page below it is free (0 is always true)
+ * page_size is a power of two from 16 to 1024, head_dim a multiple of 8 from 8
+ * to 128.  An empty cache has table -1 and length, refs and low 0. */
+typedef struct {
+    int32_t dtype;                 /* opattr_dtype */
+    int32_t page_size;
+    int32_t kv_heads;
+    int32_t head_dim;
+    int32_t n_seqs;
+    int32_t pages_per_seq;
+    int64_t n_pages;
+    void *k_pages;
+    void *v_pages;
+    int32_t *table;
+    int32_t *length;
+    int32_t *refs;
+    int32_t *low;
+} opattr_cache;
+
+/* One new query per sequence over the cache: row i of q and out is sequence
+ * seqs[i] (i32[n] device, repeats allowed; NULL: sequence i), which sees all
+ * of its length.  lse f32[n * q_heads] device, may be NULL.  A length of 0
+ * gives zeros and -inf.
+ * Errors: as opattr_attention. */
+opattr_status opattr_cache_attention(opattr_ctx *ctx, const opattr_cache *cache, const int32_t *seqs, int32_t n,
+                                     int32_t q_heads, const opattr_rows *q, const opattr_rows *out, float *lse,
+                                     float scale);
+
+/* Rows offsets[i] .. offsets[i + 1] of k and v (i32[n + 1] device, from 0 to
+ * tokens, not decreasing) to the end of sequence seqs[i] (i32[n] device, each
+ * once).  Sequence after sequence, a page that is filled in part and held by
+ * others as well is copied first (its filled part), and pages are taken from
+ * the lowest free one on.  Too few free pages: OPATTR_E_PAGES from
+ * opattr_check, and nothing is changed.
+ * Errors: as opattr_attention. */
+opattr_status opattr_cache_append(opattr_ctx *ctx, const opattr_cache *cache, const int32_t *seqs, int32_t n,
+                                  const int32_t *offsets, int64_t tokens, const opattr_rows *k, const opattr_rows *v);
+
+/* Sequence dst[i] (empty, each once, none of them in src) becomes a second
+ * holder of src[i]'s pages.  Errors: as opattr_attention. */
+opattr_status opattr_cache_fork(opattr_ctx *ctx, const opattr_cache *cache, const int32_t *src, const int32_t *dst,
+                                int32_t n);
+
+/* Sequence seqs[i] (each once) keeps its first lengths[i] tokens (i32[n]
+ * device, at most its length, not the cache's own array; NULL: none), and
+ * lets go of the pages past them.  Errors: as opattr_attention. */
+opattr_status opattr_cache_trim(opattr_ctx *ctx, const opattr_cache *cache, const int32_t *seqs,
+                                const int32_t *lengths, int32_t n);
+
+/* Moves pages until those in use are the first ones: with L of them, those at
+ * L and past it move, in order, into the free ones below L, in order, and the
+ * tables follow.  live i32[1] device receives L; may be NULL.
+ * Errors: as opattr_attention. */
+opattr_status opattr_cache_compact(opattr_ctx *ctx, const opattr_cache *cache, int32_t *live);
+
+/* Waits for the context's stream and returns what the calls above found wrong
+ * on the device since the last check: OPATTR_OK, OPATTR_E_INVALID_ARG, or
+ * OPATTR_E_PAGES (of both, the first of these two).  The context stays usable.  Collects the
+ * timing of their launches (opattr_set_timing) too. */
+opattr_status opattr_check(opattr_ctx *ctx);
 
 #ifdef __cplusplus
 }

@@ -21,15 +21,16 @@ from . import _build
 
 __all__ = [
     "OK", "W_COUNT_MISMATCH", "W_DEDUP_MISMATCH", "E_INVALID_ARG", "E_NOT_NESTED", "E_DEPTH",
-    "E_COUNT_MISMATCH", "E_CUDA", "E_OOM", "E_TIMEOUT", "E_STATE", "OP_STRUCTURAL", "OP_NONOP",
-    "N_COUNTERS", "OpattrError", "Context", "library", "build",
+    "E_COUNT_MISMATCH", "E_CUDA", "E_OOM", "E_TIMEOUT", "E_STATE", "E_PAGES", "OP_STRUCTURAL", "OP_NONOP",
+    "N_COUNTERS", "OpattrError", "Context", "KVCache", "library", "build",
     "opattr_create", "opattr_enclose", "opattr_match", "opattr_aggregate", "opattr_join", "opattr_destroy",
-    "opattr_status_string", "opattr_match_noalloc", "MATCH_NOALLOC_MAX",
+    "opattr_status_string", "opattr_match_noalloc", "MATCH_NOALLOC_MAX", "opattr_attention", "opattr_cache_attention",
+    "opattr_cache_append", "opattr_cache_fork", "opattr_cache_trim", "opattr_cache_compact", "opattr_check",
 ]
 
 OK, W_COUNT_MISMATCH, W_DEDUP_MISMATCH = 0, 1, 2
 E_INVALID_ARG, E_NOT_NESTED, E_DEPTH, E_COUNT_MISMATCH = -1, -2, -3, -4
-E_CUDA, E_OOM, E_TIMEOUT, E_STATE = -5, -6, -7, -8
+E_CUDA, E_OOM, E_TIMEOUT, E_STATE, E_PAGES = -5, -6, -7, -8, -9
 OP_STRUCTURAL = 0xFFFFFFFF
 OP_NONOP = 0xFFFFFFFE
 N_COUNTERS = 20
@@ -118,6 +119,24 @@ class Totals(ctypes.Structure):
                 "unattributed_frac": self.unattributed_frac}
 
 
+class Rows(ctypes.Structure):
+    _fields_ = [("data", _vp), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class Prompt(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int32) for f in ("dtype", "n_seqs", "q_heads", "kv_heads", "head_dim", "causal")] + \
+               [("scale", ctypes.c_float), ("reserved", ctypes.c_int32), ("q_tokens", ctypes.c_int64),
+                ("k_tokens", ctypes.c_int64), ("q", Rows), ("k", Rows), ("v", Rows), ("out", Rows),
+                ("q_offsets", _vp), ("k_offsets", _vp), ("lse", _vp)]
+
+
+class Cache(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int32) for f in ("dtype", "page_size", "kv_heads", "head_dim", "n_seqs",
+                                              "pages_per_seq")] + \
+               [("n_pages", ctypes.c_int64)] + \
+               [(f, _vp) for f in ("k_pages", "v_pages", "table", "length", "refs", "low")]
+
+
 _lib_lock = threading.Lock()
 _lib = None
 
@@ -167,8 +186,18 @@ def library():
             lib.opattr_launch_count.restype = ctypes.c_int64
             lib.opattr_match_noalloc.argtypes = [P(Kernels), P(Ncu), ctypes.c_int, _vp, _vp, P(MatchSummary), _vp]
             lib.opattr_match_noalloc.restype = ctypes.c_int
+            i32, i64, f32 = ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+            lib.opattr_attention.argtypes = [_vp, P(Prompt)]
+            lib.opattr_cache_attention.argtypes = [_vp, P(Cache), _vp, i32, i32, P(Rows), P(Rows), _vp, f32]
+            lib.opattr_cache_append.argtypes = [_vp, P(Cache), _vp, i32, _vp, i64, P(Rows), P(Rows)]
+            lib.opattr_cache_fork.argtypes = [_vp, P(Cache), _vp, _vp, i32]
+            lib.opattr_cache_trim.argtypes = [_vp, P(Cache), _vp, _vp, i32]
+            lib.opattr_cache_compact.argtypes = [_vp, P(Cache), _vp]
+            lib.opattr_check.argtypes = [_vp]
             for f in ("opattr_create", "opattr_enclose", "opattr_match", "opattr_aggregate", "opattr_attribute",
-                      "opattr_rollup", "opattr_set_timing", "opattr_timing_report"):
+                      "opattr_rollup", "opattr_set_timing", "opattr_timing_report", "opattr_attention",
+                      "opattr_cache_attention", "opattr_cache_append", "opattr_cache_fork", "opattr_cache_trim",
+                      "opattr_cache_compact", "opattr_check"):
                 getattr(lib, f).restype = ctypes.c_int
             _lib = lib
         return _lib
@@ -294,6 +323,38 @@ def opattr_match_noalloc(kernels: Kernels, ncu: Ncu, mismatch: str, idx_ptr: int
                                           _vp(idx_ptr), _vp(kind_ptr or 0), ctypes.byref(summary), _vp(stream or 0))
 
 
+def opattr_attention(handle, args: Prompt) -> int:
+    return (_lib or library()).opattr_attention(handle, ctypes.byref(args))
+
+
+def opattr_cache_attention(handle, cache: Cache, seqs_ptr: int | None, n: int, q_heads: int, q: Rows, out: Rows,
+                           lse_ptr: int | None, scale: float) -> int:
+    return (_lib or library()).opattr_cache_attention(handle, ctypes.byref(cache), seqs_ptr, n, q_heads,
+                                                      ctypes.byref(q), ctypes.byref(out), lse_ptr, scale)
+
+
+def opattr_cache_append(handle, cache: Cache, seqs_ptr: int, n: int, offsets_ptr: int, tokens: int, k: Rows,
+                        v: Rows) -> int:
+    return (_lib or library()).opattr_cache_append(handle, ctypes.byref(cache), seqs_ptr, n, offsets_ptr, tokens,
+                                                   ctypes.byref(k), ctypes.byref(v))
+
+
+def opattr_cache_fork(handle, cache: Cache, src_ptr: int, dst_ptr: int, n: int) -> int:
+    return (_lib or library()).opattr_cache_fork(handle, ctypes.byref(cache), src_ptr, dst_ptr, n)
+
+
+def opattr_cache_trim(handle, cache: Cache, seqs_ptr: int, lengths_ptr: int | None, n: int) -> int:
+    return (_lib or library()).opattr_cache_trim(handle, ctypes.byref(cache), seqs_ptr, lengths_ptr, n)
+
+
+def opattr_cache_compact(handle, cache: Cache, live_ptr: int | None) -> int:
+    return (_lib or library()).opattr_cache_compact(handle, ctypes.byref(cache), live_ptr)
+
+
+def opattr_check(handle) -> int:
+    return (_lib or library()).opattr_check(handle)
+
+
 def opattr_destroy(handle) -> None:
     if handle:
         library().opattr_destroy(handle)
@@ -379,6 +440,74 @@ def to_device(trace, device: int = 0, pin: bool = False) -> DeviceTrace:
                        trace.rep_of_class, d(getattr(trace, "ncu_stream", None)), d(getattr(trace, "corr_name", None)),
                        d(getattr(trace, "corr_inv", None)), d(getattr(trace, "corr_op", None)),
                        d(getattr(trace, "fusion_op", None)), d(getattr(trace, "fusion_len", None)))
+
+
+def _dtype(t, name) -> int:
+    """opattr_dtype of a tensor of 16-bit values."""
+    torch = _torch()
+    if t.dtype is torch.bfloat16:
+        return 0
+    if t.dtype is torch.float16:
+        return 1
+    raise TypeError(f"{name}: expected torch.bfloat16 or torch.float16, got {t.dtype}")
+
+
+def _rows(t, heads: int | None, dim: int, like, name, device) -> Rows:
+    """[tokens, heads, dim] of `like`'s type as opattr_rows; a view whose heads
+    are contiguous and whose rows lie 16 bytes apart or a multiple of that."""
+    if t.dim() != 3 or (heads is not None and t.shape[1] != heads) or t.shape[2] != dim:
+        raise ValueError(f"{name}: expected [tokens, {heads if heads is not None else 'heads'}, {dim}], "
+                         f"got {list(t.shape)}")
+    if t.dtype is not like:
+        raise TypeError(f"{name}: expected {like}, got {t.dtype}")
+    if t.get_device() != device:
+        raise ValueError(f"{name}: must live on cuda:{device}")
+    if t.numel() == 0:
+        return Rows(None, 0, 0)
+    st, sh, se = t.stride()
+    n, h, _ = t.shape
+    p = t.data_ptr()
+    if (se != 1 and dim > 1) or p % 16 or (n > 1 and (st % 8 or st < 0)) or (h > 1 and (sh % 8 or sh < 0)):
+        raise ValueError(f"{name}: a row's elements must be contiguous and rows 16-byte aligned")
+    return Rows(p, st if n > 1 else h * dim, sh if h > 1 else dim)
+
+
+def _distinct(t, name):
+    """An output's rows must not overlap."""
+    if t.numel() and any(s == 0 and n > 1 for s, n in zip(t.stride(), t.shape)):
+        raise ValueError(f"{name}: must not be expanded")
+
+
+@dataclass
+class KVCache:
+    """A paged key-value cache as device tensors (opattr_cache in
+    include/opattr.h has the layouts); Context.cache makes an empty one."""
+    k_pages: object                 # [n_pages, kv_heads, page_size, head_dim] bfloat16 or float16
+    v_pages: object
+    table: object                   # int32 [n_seqs, pages_per_seq], -1 past a sequence's length
+    length: object                  # int32 [n_seqs]
+    refs: object                    # int32 [n_pages]: sequences that hold a page
+    low: object                     # int32 [1]: no page below it is free
+
+    def __post_init__(self):
+        dv = self.k_pages.get_device()
+        if self.k_pages.dim() != 4 or self.v_pages.shape != self.k_pages.shape:
+            raise ValueError("k_pages, v_pages: expected one shape [n_pages, kv_heads, page_size, head_dim]")
+        dtype = _dtype(self.k_pages, "k_pages")
+        n, g, page, dim = self.k_pages.shape
+        torch = _torch()
+        if page < 16 or page > 1024 or page & (page - 1):
+            raise ValueError(f"page_size: expected a power of two from 16 to 1024, got {page}")
+        if dim < 8 or dim > 128 or dim % 8:
+            raise ValueError(f"head_dim: expected a multiple of 8 from 8 to 128, got {dim}")
+        if self.table.dim() != 2 or self.length.shape != (self.table.shape[0],) or self.refs.shape != (n,) or \
+                self.low.numel() != 1 or n < 1 or g < 1 or self.table.numel() < 1:
+            raise ValueError("expected table [n_seqs, pages_per_seq], length [n_seqs], refs [n_pages], low [1]")
+        self.struct = Cache(dtype, page, g, dim, self.table.shape[0], self.table.shape[1], n,
+                            _ptr(self.k_pages, self.k_pages.dtype, "k_pages", dv),
+                            _ptr(self.v_pages, self.k_pages.dtype, "v_pages", dv),
+                            _ptr(self.table, torch.int32, "table", dv), _ptr(self.length, torch.int32, "length", dv),
+                            _ptr(self.refs, torch.int32, "refs", dv), _ptr(self.low, torch.int32, "low", dv))
 
 
 class Context:
@@ -601,6 +730,165 @@ class Context:
         st_a, ops, tot = self.aggregate(tr, rk, idx)
         return dict(enclose_status=st_e, range_of_kernel=rk, n_op_enclosing=nop, match_status=st_m, ncu_idx=idx,
                     match_kind=kind, summary=summ, aggregate_status=st_a, ops=ops, totals=tot)
+
+    # -- attention, and the paged cache under it.  These calls do not wait; on
+    # another stream than the context's they are ordered as calls on that stream
+    def _enter(self):
+        cur = _torch().cuda.current_stream(self.device)
+        if cur == self.stream:
+            return None
+        self.stream.wait_stream(cur)
+        return cur
+
+    def _leave(self, cur, status: int, call: str) -> int:
+        if cur is not None:
+            cur.wait_stream(self.stream)
+        if status < 0:
+            raise OpattrError(status, call)
+        return status
+
+    def _i32(self, t, n: int | None, name):
+        if t is None:
+            return None
+        if t.dim() != 1 or (n is not None and t.shape[0] != n):
+            raise ValueError(f"{name}: expected [{n if n is not None else 'n'}], got {list(t.shape)}")
+        return _ptr(t, _torch().int32, name, self.device)
+
+    def attention(self, q, k, v, q_offsets=None, k_offsets=None, causal: bool = True, scale: float | None = None,
+                  out=None, need_lse: bool = False):
+        """Attention over packed sequences (opattr_attention): q [tokens, heads,
+        dim], k and v [tokens, kv_heads, dim]; offsets int32 [n_seqs + 1] on the
+        device (none: one sequence; k_offsets none: q_offsets).  scale: by
+        default 1 / sqrt(dim).  Returns (status, out, lse or None)."""
+        torch = _torch()
+        dv = self.device
+        if q.dim() != 3 or k.dim() != 3:
+            raise ValueError("q, k: expected [tokens, heads, dim]")
+        dim, dt = q.shape[2], q.dtype
+        dtype = _dtype(q, "q")
+        if dim < 8 or dim > 128 or dim % 8:
+            raise ValueError(f"dim: expected a multiple of 8 from 8 to 128, got {dim}")
+        if k.shape[1] < 1 or q.shape[1] < 1 or q.shape[1] % k.shape[1]:
+            raise ValueError(f"heads: {q.shape[1]} of q are no multiple of {k.shape[1]} of k")
+        if v.shape[0] != k.shape[0]:
+            raise ValueError(f"v: expected {k.shape[0]} rows, got {v.shape[0]}")
+        rq, rk, rv = (_rows(t, h, dim, dt, nm, dv) for t, h, nm in ((q, None, "q"), (k, None, "k"), (v, k.shape[1], "v")))
+        if q_offsets is None:
+            if k_offsets is not None:
+                raise ValueError("k_offsets: needs q_offsets")
+            q_offsets = torch.tensor([0, q.shape[0]], dtype=torch.int32, device=self._dev)
+            if k.shape[0] != q.shape[0]:
+                k_offsets = torch.tensor([0, k.shape[0]], dtype=torch.int32, device=self._dev)
+        if q_offsets.dim() != 1 or q_offsets.shape[0] < 1:
+            raise ValueError("q_offsets: expected [n_seqs + 1]")
+        n_seqs = q_offsets.shape[0] - 1
+        if k_offsets is None and k.shape[0] != q.shape[0]:
+            raise ValueError("k_offsets: k has other rows than q")
+        if out is None:
+            out = torch.empty(q.shape, dtype=dt, device=self._dev)
+        elif out.shape != q.shape:
+            raise ValueError(f"out: expected {list(q.shape)}, got {list(out.shape)}")
+        _distinct(out, "out")
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=self._dev) if need_lse else None
+        p_qo = self._i32(q_offsets, None, "q_offsets")
+        args = Prompt(dtype, n_seqs, q.shape[1], k.shape[1], dim, int(bool(causal)),
+                      dim ** -0.5 if scale is None else scale, 0, q.shape[0], k.shape[0], rq, rk, rv,
+                      _rows(out, q.shape[1], dim, dt, "out", dv), p_qo,
+                      p_qo if k_offsets is None else self._i32(k_offsets, n_seqs + 1, "k_offsets"),
+                      _ptr(lse, torch.float32, "lse", dv))
+        cur = self._enter()
+        return self._leave(cur, opattr_attention(self.handle, args), "opattr_attention"), out, lse
+
+    def cache(self, n_pages: int, page_size: int, kv_heads: int, head_dim: int, n_seqs: int, pages_per_seq: int,
+              dtype=None) -> KVCache:
+        """An empty cache of `n_pages` pages for `n_seqs` sequences of at most
+        pages_per_seq pages each (dtype: by default torch.bfloat16)."""
+        torch = _torch()
+        new = lambda shape, value: torch.full(shape, value, dtype=torch.int32, device=self._dev)  # noqa: E731
+        pool = [torch.zeros((n_pages, kv_heads, page_size, head_dim), dtype=dtype or torch.bfloat16, device=self._dev)
+                for _ in range(2)]
+        return KVCache(*pool, new((n_seqs, pages_per_seq), -1), new((n_seqs,), 0), new((n_pages,), 0), new((1,), 0))
+
+    def _cache(self, cache: KVCache) -> Cache:
+        if cache.k_pages.get_device() != self.device:
+            raise ValueError(f"cache: must live on cuda:{self.device}")
+        return cache.struct
+
+    def cache_attention(self, cache: KVCache, seqs, q, scale: float | None = None, out=None, need_lse: bool = False):
+        """Attention of one new token per sequence over the cache
+        (opattr_cache_attention): q [n, heads, dim], row i of sequence seqs[i]
+        (int32 [n], or None: sequence i).  Returns (status, out, lse or None)."""
+        torch = _torch()
+        dv = self.device
+        kv = self._cache(cache)
+        dim, dt = kv.head_dim, cache.k_pages.dtype
+        rq = _rows(q, None, dim, dt, "q", dv)
+        n, heads = q.shape[:2]
+        if heads < 1 or heads % kv.kv_heads:
+            raise ValueError(f"heads: {heads} of q are no multiple of {kv.kv_heads} of the cache")
+        if seqs is None and n > kv.n_seqs:
+            raise ValueError(f"q: {n} rows for {kv.n_seqs} sequences")
+        if out is None:
+            out = torch.empty(q.shape, dtype=dt, device=self._dev)
+        elif out.shape != q.shape:
+            raise ValueError(f"out: expected {list(q.shape)}, got {list(out.shape)}")
+        _distinct(out, "out")
+        lse = torch.empty((n, heads), dtype=torch.float32, device=self._dev) if need_lse else None
+        ro = _rows(out, heads, dim, dt, "out", dv)
+        p_seqs, p_lse = self._i32(seqs, n, "seqs"), _ptr(lse, torch.float32, "lse", dv)
+        cur = self._enter()
+        st = opattr_cache_attention(self.handle, kv, p_seqs, n, heads, rq, ro, p_lse,
+                                    dim ** -0.5 if scale is None else scale)
+        return self._leave(cur, st, "opattr_cache_attention"), out, lse
+
+    def cache_append(self, cache: KVCache, seqs, offsets, k, v) -> int:
+        """Rows offsets[i] .. offsets[i + 1] of k and v ([tokens, kv_heads, dim])
+        to the end of sequence seqs[i], each sequence once (opattr_cache_append)."""
+        dv = self.device
+        kv = self._cache(cache)
+        if v.shape != k.shape:
+            raise ValueError(f"v: expected {list(k.shape)}, got {list(v.shape)}")
+        rk, rv = (_rows(t, kv.kv_heads, kv.head_dim, cache.k_pages.dtype, nm, dv) for t, nm in ((k, "k"), (v, "v")))
+        p_seqs = self._i32(seqs, None, "seqs")
+        p_off = self._i32(offsets, seqs.shape[0] + 1, "offsets")
+        cur = self._enter()
+        st = opattr_cache_append(self.handle, kv, p_seqs, seqs.shape[0], p_off, k.shape[0], rk, rv)
+        return self._leave(cur, st, "opattr_cache_append")
+
+    def cache_fork(self, cache: KVCache, src, dst) -> int:
+        """The empty sequences dst[i] share the pages of src[i] (opattr_cache_fork)."""
+        kv = self._cache(cache)
+        p_dst = self._i32(dst, None, "dst")
+        p_src = self._i32(src, dst.shape[0], "src")
+        cur = self._enter()
+        return self._leave(cur, opattr_cache_fork(self.handle, kv, p_src, p_dst, dst.shape[0]), "opattr_cache_fork")
+
+    def cache_trim(self, cache: KVCache, seqs, lengths=None) -> int:
+        """Sequence seqs[i] keeps its first lengths[i] tokens (none: it is
+        freed), and the pages past them are let go (opattr_cache_trim)."""
+        kv = self._cache(cache)
+        p_seqs = self._i32(seqs, None, "seqs")
+        p_len = self._i32(lengths, seqs.shape[0], "lengths")
+        cur = self._enter()
+        st = opattr_cache_trim(self.handle, kv, p_seqs, p_len, seqs.shape[0])
+        return self._leave(cur, st, "opattr_cache_trim")
+
+    def cache_compact(self, cache: KVCache):
+        """The pages in use become the cache's first ones (opattr_cache_compact).
+        Returns (status, int32 [1] tensor of how many those are)."""
+        torch = _torch()
+        kv = self._cache(cache)
+        live = torch.empty(1, dtype=torch.int32, device=self._dev)
+        cur = self._enter()
+        st = opattr_cache_compact(self.handle, kv, live.data_ptr())
+        return self._leave(cur, st, "opattr_cache_compact"), live
+
+    def check(self) -> None:
+        """Waits for the calls above and raises what they found wrong on the
+        device since the last check (opattr_check)."""
+        st = opattr_check(self.handle)
+        if st < 0:
+            raise OpattrError(st, "opattr_check")
 
     # -- accounting
     def set_timing(self, on: bool):

@@ -6,7 +6,7 @@
 #include <algorithm>
 #include <new>
 
-#include "common.cuh"
+#include "serve.cuh"
 
 // One NVTX range per call of the C ABI, named after the entry point, so a
 // timeline (Nsight Systems) shows the library's calls around their kernels.
@@ -38,6 +38,17 @@ opattr_status do_attribute(Ctx &c, const opattr_kernels *kern, const opattr_rang
 opattr_status do_rollup(Ctx &c, const opattr_kernels *kern, const opattr_ranges *rng, const int32_t *rok,
                         const opattr_ncu *ncu, const int32_t *nidx, uint32_t n_ops, const uint32_t *class_of_op,
                         uint32_t n_classes, const opattr_op_aggregates *out);
+
+opattr_status do_attention(Ctx &c, Serve &s, const opattr_prompt *a);
+opattr_status do_cache_attention(Ctx &c, Serve &s, const opattr_cache *kv, const int32_t *seqs, int32_t n,
+                                 int32_t q_heads, const opattr_rows *q, const opattr_rows *out, float *lse,
+                                 float scale);
+opattr_status do_cache_append(Ctx &c, Serve &s, const opattr_cache *kv, const int32_t *seqs, int32_t n,
+                              const int32_t *offsets, int64_t tokens, const opattr_rows *k, const opattr_rows *v);
+opattr_status do_cache_fork(Ctx &c, Serve &s, const opattr_cache *kv, const int32_t *src, const int32_t *dst, int32_t n);
+opattr_status do_cache_trim(Ctx &c, Serve &s, const opattr_cache *kv, const int32_t *seqs, const int32_t *lengths,
+                            int32_t n);
+opattr_status do_cache_compact(Ctx &c, Serve &s, const opattr_cache *kv, int32_t *live);
 
 opattr_status cuda_status(Ctx &c, cudaError_t e) {
     if (e == cudaSuccess) e = c.last_error;
@@ -326,6 +337,7 @@ using namespace opattr;
 
 struct opattr_ctx {
     Ctx c;
+    Serve serve;
 };
 
 extern "C" {
@@ -590,6 +602,91 @@ opattr_status opattr_rollup(opattr_ctx *ctx, const opattr_kernels *kernels, cons
                                n_classes, dev_out));
 }
 
+opattr_status opattr_attention(opattr_ctx *ctx, const opattr_prompt *args) {
+    NvtxCall nvtx("opattr_attention");
+    if (!ctx || !args) return OPATTR_E_INVALID_ARG;
+    Ctx &c = ctx->c;
+    if (c.broken) return OPATTR_E_STATE;
+    DeviceGuard g(c.device);
+    if (!g.ok) return OPATTR_E_CUDA;
+    return finish(c, do_attention(c, ctx->serve, args));
+}
+
+opattr_status opattr_cache_attention(opattr_ctx *ctx, const opattr_cache *cache, const int32_t *seqs, int32_t n,
+                                     int32_t q_heads, const opattr_rows *q, const opattr_rows *out, float *lse,
+                                     float scale) {
+    NvtxCall nvtx("opattr_cache_attention");
+    if (!ctx || !cache || !q || !out) return OPATTR_E_INVALID_ARG;
+    Ctx &c = ctx->c;
+    if (c.broken) return OPATTR_E_STATE;
+    DeviceGuard g(c.device);
+    if (!g.ok) return OPATTR_E_CUDA;
+    return finish(c, do_cache_attention(c, ctx->serve, cache, seqs, n, q_heads, q, out, lse, scale));
+}
+
+opattr_status opattr_cache_append(opattr_ctx *ctx, const opattr_cache *cache, const int32_t *seqs, int32_t n,
+                                  const int32_t *offsets, int64_t tokens, const opattr_rows *k, const opattr_rows *v) {
+    NvtxCall nvtx("opattr_cache_append");
+    if (!ctx || !cache || !k || !v) return OPATTR_E_INVALID_ARG;
+    Ctx &c = ctx->c;
+    if (c.broken) return OPATTR_E_STATE;
+    DeviceGuard g(c.device);
+    if (!g.ok) return OPATTR_E_CUDA;
+    return finish(c, do_cache_append(c, ctx->serve, cache, seqs, n, offsets, tokens, k, v));
+}
+
+opattr_status opattr_cache_fork(opattr_ctx *ctx, const opattr_cache *cache, const int32_t *src, const int32_t *dst,
+                                int32_t n) {
+    NvtxCall nvtx("opattr_cache_fork");
+    if (!ctx || !cache) return OPATTR_E_INVALID_ARG;
+    Ctx &c = ctx->c;
+    if (c.broken) return OPATTR_E_STATE;
+    DeviceGuard g(c.device);
+    if (!g.ok) return OPATTR_E_CUDA;
+    return finish(c, do_cache_fork(c, ctx->serve, cache, src, dst, n));
+}
+
+opattr_status opattr_cache_trim(opattr_ctx *ctx, const opattr_cache *cache, const int32_t *seqs,
+                                const int32_t *lengths, int32_t n) {
+    NvtxCall nvtx("opattr_cache_trim");
+    if (!ctx || !cache) return OPATTR_E_INVALID_ARG;
+    Ctx &c = ctx->c;
+    if (c.broken) return OPATTR_E_STATE;
+    DeviceGuard g(c.device);
+    if (!g.ok) return OPATTR_E_CUDA;
+    return finish(c, do_cache_trim(c, ctx->serve, cache, seqs, lengths, n));
+}
+
+opattr_status opattr_cache_compact(opattr_ctx *ctx, const opattr_cache *cache, int32_t *live) {
+    NvtxCall nvtx("opattr_cache_compact");
+    if (!ctx || !cache) return OPATTR_E_INVALID_ARG;
+    Ctx &c = ctx->c;
+    if (c.broken) return OPATTR_E_STATE;
+    DeviceGuard g(c.device);
+    if (!g.ok) return OPATTR_E_CUDA;
+    return finish(c, do_cache_compact(c, ctx->serve, cache, live));
+}
+
+opattr_status opattr_check(opattr_ctx *ctx) {
+    NvtxCall nvtx("opattr_check");
+    if (!ctx) return OPATTR_E_INVALID_ARG;
+    Ctx &c = ctx->c;
+    if (c.broken) return OPATTR_E_STATE;
+    DeviceGuard g(c.device);
+    if (!g.ok) return OPATTR_E_CUDA;
+    unsigned found = 0;
+    cudaError_t e = cudaSuccess;
+    if (ctx->serve.err) {
+        e = cudaMemcpyAsync(c.h_small, ctx->serve.err, sizeof(unsigned), cudaMemcpyDeviceToHost, c.stream);
+        if (e == cudaSuccess) e = cudaMemsetAsync(ctx->serve.err, 0, sizeof(unsigned), c.stream);
+    }
+    if (e == cudaSuccess) e = cudaStreamSynchronize(c.stream);
+    if (e != cudaSuccess || c.last_error != cudaSuccess) return finish(c, cuda_status(c, e));
+    if (ctx->serve.err) found = c.h_small[0];
+    if (c.timing) timing_collect(c);
+    return found & SERVE_INVALID ? OPATTR_E_INVALID_ARG : found & SERVE_PAGES ? OPATTR_E_PAGES : OPATTR_OK;
+}
+
 void opattr_destroy(opattr_ctx *ctx) {
     if (!ctx) return;
     Ctx &c = ctx->c;
@@ -602,6 +699,7 @@ void opattr_destroy(opattr_ctx *ctx) {
         if (c.h_small) cudaFreeHost(c.h_small);
         if (c.h_stage) cudaFreeHost(c.h_stage);
         if (c.ev_status) cudaEventDestroy(c.ev_status);
+        serve_free(ctx->serve);
         for (auto &p : c.pending) {
             cudaEventDestroy(p.second.first);
             cudaEventDestroy(p.second.second);
@@ -625,6 +723,7 @@ const char *opattr_status_string(opattr_status s) {
     case OPATTR_E_OOM: return "out of device memory";
     case OPATTR_E_TIMEOUT: return "device-side wait timed out";
     case OPATTR_E_STATE: return "context unusable after a CUDA error";
+    case OPATTR_E_PAGES: return "no free page left in the cache";
     }
     return "unknown status";
 }

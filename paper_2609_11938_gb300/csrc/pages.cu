@@ -1,0 +1,480 @@
+// pages.cu -- the paged key-value cache: appending tokens, sharing pages between
+// sequences, freeing them, and moving the live ones together.
+//
+// The cache's state is the caller's: a table of each sequence's pages, its
+// length, and for each page how many sequences hold it (a page held by none is
+// free).  Every call reads that state, checks its own arguments against it in
+// one block (`*_plan`), and changes it in a second launch only where they hold;
+// otherwise the call changes nothing and opattr_check reports it.  What a call
+// does is defined without reference to the order in which threads run: pages
+// are given out from the lowest free one on, sequence after sequence.
+#include <algorithm>
+
+#include "serve.cuh"
+
+namespace opattr {
+
+constexpr int PLAN_THREADS = 1024;
+constexpr int COPY_THREADS = 256;
+
+bool cache_ok(const opattr_cache *k) {
+    if (k->dtype != OPATTR_BF16 && k->dtype != OPATTR_F16) return false;
+    if (k->page_size < 16 || k->page_size > 1024 || (k->page_size & (k->page_size - 1))) return false;
+    if (k->kv_heads < 1 || k->head_dim < 8 || k->head_dim > 128 || k->head_dim % 8) return false;
+    if (k->n_seqs < 1 || k->pages_per_seq < 1 || k->n_pages < 1 || k->n_pages > INT32_MAX) return false;
+    if ((int64_t)k->pages_per_seq * k->page_size > INT32_MAX) return false;
+    if (!k->k_pages || !k->v_pages || !k->table || !k->length || !k->refs || !k->low) return false;
+    return ((reinterpret_cast<uintptr_t>(k->k_pages) | reinterpret_cast<uintptr_t>(k->v_pages)) & 15) == 0;
+}
+
+opattr_status serve_ready(Ctx &c, Serve &s, int64_t tickets) {
+    if (!s.err) {
+        cudaError_t e = cudaMalloc(&s.err, 256);
+        if (e == cudaErrorMemoryAllocation) {
+            cudaGetLastError();
+            s.err = nullptr;
+            return OPATTR_E_OOM;
+        }
+        if (e == cudaSuccess) e = cudaMemsetAsync(s.err, 0, 256, c.stream);
+        if (e != cudaSuccess) return cuda_status(c, e);
+    }
+    if (tickets > s.n_tickets) {
+        // launches before this one may still count in the old tickets
+        if (s.tickets) {
+            const cudaError_t e = cudaStreamSynchronize(c.stream);
+            if (e != cudaSuccess) return cuda_status(c, e);
+            cudaFree(s.tickets);
+            s.tickets = nullptr;
+            s.n_tickets = 0;
+        }
+        const int64_t n = tickets < 4096 ? 4096 : 2 * tickets;
+        cudaError_t e = cudaMalloc(&s.tickets, sizeof(uint32_t) * n);
+        if (e == cudaErrorMemoryAllocation) {
+            cudaGetLastError();
+            s.tickets = nullptr;
+            return OPATTR_E_OOM;
+        }
+        if (e == cudaSuccess) e = cudaMemsetAsync(s.tickets, 0, sizeof(uint32_t) * n, c.stream);
+        if (e != cudaSuccess) return cuda_status(c, e);
+        s.n_tickets = n;
+    }
+    return OPATTR_OK;
+}
+
+void serve_free(Serve &s) {
+    if (s.err) cudaFree(s.err);
+    if (s.tickets) cudaFree(s.tickets);
+    s = Serve{};
+}
+
+__host__ __device__ __forceinline__ int pages_for(int tokens, int page) { return (tokens + page - 1) / page; }
+
+// ---------------------------------------------------------------- checks of a plan
+// Every block-wide check ends in `bad` (shared): whether the call is void.
+__device__ __forceinline__ bool any_bad(bool mine, unsigned bit, unsigned *err) {
+    const bool bad = __syncthreads_or(mine);
+    if (bad && threadIdx.x == 0) atomicOr(err, bit);
+    return bad;
+}
+// Sequences of the table, each at most once.  `mark` has a word per table row;
+// of a sequence's entries one is the last to store its index, the others see it.
+__device__ __forceinline__ bool seqs_bad(const int32_t *seqs, int n, int rows, int32_t *mark, unsigned *err) {
+    bool bad = false;
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+        const int s = seqs[i];
+        if (s < 0 || s >= rows) bad = true;
+        else mark[s] = i;
+    }
+    if (any_bad(bad, SERVE_INVALID, err)) return true;
+    for (int i = threadIdx.x; i < n; i += blockDim.x) bad = bad || mark[seqs[i]] != i;
+    return any_bad(bad, SERVE_INVALID, err);
+}
+__device__ __forceinline__ bool length_bad(const opattr_cache &kv, int seq) {
+    const int len = kv.length[seq];
+    return len < 0 || len > kv.pages_per_seq * kv.page_size;
+}
+
+// ---------------------------------------------------------------- append
+// What the plan leaves for the launch that moves the rows.
+struct AppendPlan {
+    int32_t *go;        // [1] 1: the call holds
+    int32_t *old;       // [n] lengths before
+    int32_t *from, *to; // [n] a partly filled page that is copied first, and where to; -1 none
+    int32_t *mark;      // [n_seqs]
+    int32_t *first;     // [n + 1] new pages before this sequence's
+    int32_t *fresh;     // new pages in the order they are given out
+    int32_t room;       // entries of fresh
+};
+
+// One block: a call has few sequences, and their new pages are found where the
+// lowest free ones are (`low`: none below it is free), a thousand times four
+// reference counts at a time.
+__global__ void __launch_bounds__(PLAN_THREADS)
+k_append_plan(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offsets, int tokens, AppendPlan p,
+              unsigned *err) {
+    __shared__ int warp_buf[33];
+    pdl_wait();
+    if (threadIdx.x == 0) *p.go = 0;
+    if (seqs_bad(seqs, n, kv.n_seqs, p.mark, err)) return;
+    bool bad = threadIdx.x == 0 && (offsets[0] != 0 || offsets[n] != tokens);
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+        const int more = offsets[i + 1] - offsets[i], s = seqs[i];
+        bad = bad || more < 0 || offsets[i] < 0 || length_bad(kv, s) ||
+              (int64_t)kv.length[s] + more > (int64_t)kv.pages_per_seq * kv.page_size;
+    }
+    if (any_bad(bad, SERVE_INVALID, err)) return;
+    // pages of each sequence that others hold too and that it is about to write into
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+        const int s = seqs[i], old = kv.length[s], more = offsets[i + 1] - offsets[i];
+        int last = -1;
+        if (more > 0 && old % kv.page_size) {
+            last = kv.table[(int64_t)s * kv.pages_per_seq + old / kv.page_size];
+            if (last < 0 || last >= kv.n_pages) {
+                bad = true;
+                last = -1;
+            }
+        }
+        p.old[i] = old;
+        p.to[i] = last;
+    }
+    if (any_bad(bad, SERVE_INVALID, err)) return;
+    int total = 0;
+    for (int i0 = 0; i0 < n; i0 += PLAN_THREADS) {
+        const int i = i0 + threadIdx.x;
+        int need = 0;
+        if (i < n) {
+            const int old = p.old[i], more = offsets[i + 1] - offsets[i], last = p.to[i];
+            need = pages_for(old + more, kv.page_size) - pages_for(old, kv.page_size);
+            int from = -1;
+            if (last >= 0 && kv.refs[last] > 1) {
+                // one after another: those before it have copied theirs and let go
+                int held = kv.refs[last];
+                for (int k = 0; k < i && held > 1; ++k) held -= p.to[k] == last;
+                if (held > 1) from = last;
+            }
+            p.from[i] = from;
+            need += from >= 0;
+        }
+        int sum;
+        const int before = block_exclusive_scan(need, warp_buf, &sum);
+        if (i < n) p.first[i] = total + before;
+        total += sum;
+        if (total > p.room) break;       // (also keeps the sum from running over)
+    }
+    if (threadIdx.x == 0) p.first[n] = total;
+    if (any_bad(total > p.room, SERVE_PAGES, err)) return;
+    // the lowest `total` free pages
+    int found = 0;
+    const int64_t low = max(0, *kv.low);
+    for (int64_t at = low; found < total && at < kv.n_pages; at += 4 * PLAN_THREADS) {
+        const int64_t i = at + 4 * threadIdx.x;
+        int r[4], mine = 0;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            r[q] = i + q < kv.n_pages ? kv.refs[i + q] : 1;
+            mine += r[q] == 0;
+        }
+        int sum, rank = found + block_exclusive_scan(mine, warp_buf, &sum);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (r[q] == 0 && rank < total) p.fresh[rank++] = (int)(i + q);
+        found += sum;
+    }
+    __syncthreads();
+    if (any_bad(found < total, SERVE_PAGES, err)) return;
+    // it holds: the tables change
+    for (int k = threadIdx.x; k < total; k += blockDim.x) {
+        const int i = seq_of_row(p.first, n, k), s = seqs[i], page = p.fresh[k];
+        const int have = pages_for(p.old[i], kv.page_size), copied = p.from[i] >= 0;
+        kv.table[(int64_t)s * kv.pages_per_seq + have - copied + (k - p.first[i])] = page;
+        kv.refs[page] = 1;
+    }
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+        p.to[i] = -1;
+        if (p.from[i] >= 0) {
+            p.to[i] = p.fresh[p.first[i]];
+            atomicSub(&kv.refs[p.from[i]], 1);
+        }
+        kv.length[seqs[i]] = p.old[i] + (offsets[i + 1] - offsets[i]);
+    }
+    if (threadIdx.x == 0) {
+        if (total > 0) *kv.low = p.fresh[total - 1] + 1;
+        *p.go = 1;
+    }
+}
+
+// Rows into their pages, 16 bytes at a time, keys and values side by side; the
+// blocks past `row_blocks` copy the pages that were shared.
+__global__ void __launch_bounds__(COPY_THREADS)
+k_append_rows(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offsets, int tokens, opattr_rows k,
+              opattr_rows v, AppendPlan p, unsigned row_blocks) {
+    pdl_wait();
+    if (*p.go == 0) return;
+    const int per = kv.head_dim / 8;                              // pieces of a head's row
+    uint4 *kp = reinterpret_cast<uint4 *>(kv.k_pages), *vp = reinterpret_cast<uint4 *>(kv.v_pages);
+    if (blockIdx.x >= row_blocks) {
+        for (int i = blockIdx.x - row_blocks; i < n; i += gridDim.x - row_blocks) {
+            if (p.from[i] < 0) continue;
+            const int live = (p.old[i] % kv.page_size) * per;
+            const int64_t block = (int64_t)kv.page_size * per;
+            for (int x = threadIdx.x; x < live * kv.kv_heads; x += COPY_THREADS) {
+                const int64_t g = x / live, e = x % live;
+                const int64_t src = (p.from[i] * (int64_t)kv.kv_heads + g) * block + e;
+                const int64_t dst = (p.to[i] * (int64_t)kv.kv_heads + g) * block + e;
+                kp[dst] = kp[src];
+                vp[dst] = vp[src];
+            }
+        }
+        return;
+    }
+    const int64_t pieces = (int64_t)tokens * kv.kv_heads * per;
+    for (int64_t x = (int64_t)blockIdx.x * COPY_THREADS + threadIdx.x; x < pieces; x += (int64_t)row_blocks * COPY_THREADS) {
+        const int e = (int)(x % per), g = (int)(x / per % kv.kv_heads), t = (int)(x / per / kv.kv_heads);
+        const int i = seq_of_row(offsets, n, t), pos = p.old[i] + t - offsets[i];
+        const int page = kv.table[(int64_t)seqs[i] * kv.pages_per_seq + pos / kv.page_size];
+        if (page < 0 || page >= kv.n_pages) continue;             // a table that was not consistent before the call
+        const int64_t dst = ((page * (int64_t)kv.kv_heads + g) * kv.page_size + pos % kv.page_size) * per + e;
+        kp[dst] = *reinterpret_cast<const uint4 *>((const uint16_t *)k.data + t * k.token_stride + g * k.head_stride + 8 * e);
+        vp[dst] = *reinterpret_cast<const uint4 *>((const uint16_t *)v.data + t * v.token_stride + g * v.head_stride + 8 * e);
+    }
+}
+
+static opattr_status seqs_ok(const opattr_cache *kv, const int32_t *seqs, int32_t n) {
+    return cache_ok(kv) && n >= 0 && n <= kv->n_seqs && (n == 0 || seqs) ? OPATTR_OK : OPATTR_E_INVALID_ARG;
+}
+
+opattr_status do_cache_append(Ctx &c, Serve &s, const opattr_cache *kv, const int32_t *seqs, int32_t n,
+                              const int32_t *offsets, int64_t tokens, const opattr_rows *k, const opattr_rows *v) {
+    opattr_status st = seqs_ok(kv, seqs, n);
+    if (st) return st;
+    if (tokens < 0 || tokens > INT32_MAX || (n == 0 && tokens > 0) || (n > 0 && !offsets)) return OPATTR_E_INVALID_ARG;
+    if (!rows_ok(*k, tokens, kv->kv_heads, kv->head_dim) || !rows_ok(*v, tokens, kv->kv_heads, kv->head_dim))
+        return OPATTR_E_INVALID_ARG;
+    if (n == 0) return OPATTR_OK;
+    if ((st = serve_ready(c, s, 0))) return st;
+    // at most: a page copied and one begun by each sequence, and the full ones
+    const int64_t most = std::min<int64_t>(kv->n_pages, 2ll * n + tokens / kv->page_size);
+    if ((st = ensure_arena(c, Need().add<int32_t>(1).add<int32_t>(n).add<int32_t>(n).add<int32_t>(n).add<int32_t>(n + 1)
+                                  .add<int32_t>(kv->n_seqs).add<int32_t>(most).bytes)))
+        return st;
+    Arena a(c);
+    AppendPlan p{};
+    p.go = a.take<int32_t>(1);
+    p.old = a.take<int32_t>(n);
+    p.from = a.take<int32_t>(n);
+    p.to = a.take<int32_t>(n);
+    p.first = a.take<int32_t>(n + 1);
+    p.mark = a.take<int32_t>(kv->n_seqs);
+    p.fresh = a.take<int32_t>(most);
+    p.room = (int32_t)most;
+    launch(c, "append_plan", k_append_plan, dim3(1), dim3(PLAN_THREADS), 0, *kv, seqs, n, offsets, (int)tokens, p, s.err);
+    const int64_t pieces = tokens * kv->kv_heads * (kv->head_dim / 8);
+    const unsigned rows = grid_for(pieces, COPY_THREADS, 8u * sm_count(c)), shared = std::min<unsigned>(n, sm_count(c));
+    launch(c, "append_rows", k_append_rows, dim3(rows + shared), dim3(COPY_THREADS), 0, *kv, seqs, n, offsets, (int)tokens,
+           *k, *v, p, rows);
+    return cuda_status(c, c.last_error);
+}
+
+// ---------------------------------------------------------------- fork
+__global__ void __launch_bounds__(PLAN_THREADS)
+k_fork_plan(opattr_cache kv, const int32_t *src, const int32_t *dst, int n, int32_t *mark, int32_t *go, unsigned *err) {
+    pdl_wait();
+    if (threadIdx.x == 0) *go = 0;
+    if (seqs_bad(dst, n, kv.n_seqs, mark, err)) return;
+    bool bad = false;
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+        const int s = src[i];
+        bad = bad || s < 0 || s >= kv.n_seqs || length_bad(kv, s) || kv.length[dst[i]] != 0;
+        if (bad) continue;
+        // a source is no destination (its mark, where it has one, names its entry in dst)
+        const int m = mark[s];
+        bad = m >= 0 && m < n && dst[m] == s;
+    }
+    if (any_bad(bad, SERVE_INVALID, err)) return;
+    if (threadIdx.x == 0) *go = 1;
+}
+__global__ void __launch_bounds__(COPY_THREADS)
+k_fork(opattr_cache kv, const int32_t *src, const int32_t *dst, const int32_t *go) {
+    pdl_wait();
+    if (*go == 0) return;
+    const int s = src[blockIdx.x], d = dst[blockIdx.x], len = kv.length[s], held = pages_for(len, kv.page_size);
+    for (int j = blockIdx.y * COPY_THREADS + threadIdx.x; j < held; j += gridDim.y * COPY_THREADS) {
+        const int page = kv.table[(int64_t)s * kv.pages_per_seq + j];
+        kv.table[(int64_t)d * kv.pages_per_seq + j] = page;
+        if (page >= 0 && page < kv.n_pages) atomicAdd(&kv.refs[page], 1);
+    }
+    // (a source is no destination here: its length stands)
+    if (blockIdx.y == 0 && threadIdx.x == 0 && len > 0) kv.length[d] = len;
+}
+
+opattr_status do_cache_fork(Ctx &c, Serve &s, const opattr_cache *kv, const int32_t *src, const int32_t *dst, int32_t n) {
+    opattr_status st = seqs_ok(kv, dst, n);
+    if (st || n == 0) return st;
+    if (!src) return OPATTR_E_INVALID_ARG;
+    if ((st = serve_ready(c, s, 0))) return st;
+    if ((st = ensure_arena(c, Need().add<int32_t>(1).add<int32_t>(kv->n_seqs).bytes))) return st;
+    Arena a(c);
+    int32_t *go = a.take<int32_t>(1), *mark = a.take<int32_t>(kv->n_seqs);
+    launch(c, "fork_plan", k_fork_plan, dim3(1), dim3(PLAN_THREADS), 0, *kv, src, dst, n, mark, go, s.err);
+    launch(c, "fork", k_fork, dim3(n, grid_for(kv->pages_per_seq, 4 * COPY_THREADS, 64)), dim3(COPY_THREADS), 0, *kv, src,
+           dst, (const int32_t *)go);
+    return cuda_status(c, c.last_error);
+}
+
+// ---------------------------------------------------------------- trim
+__global__ void __launch_bounds__(PLAN_THREADS)
+k_trim_plan(opattr_cache kv, const int32_t *seqs, const int32_t *lengths, int n, int32_t *mark, int32_t *old,
+            int32_t *go, unsigned *err) {
+    pdl_wait();
+    if (threadIdx.x == 0) *go = 0;
+    if (seqs_bad(seqs, n, kv.n_seqs, mark, err)) return;
+    bool bad = false;
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+        const int len = kv.length[seqs[i]], to = lengths ? lengths[i] : 0;
+        bad = bad || length_bad(kv, seqs[i]) || to < 0 || to > len;
+        old[i] = len;
+    }
+    if (any_bad(bad, SERVE_INVALID, err)) return;
+    for (int i = threadIdx.x; i < n; i += blockDim.x) kv.length[seqs[i]] = lengths ? lengths[i] : 0;
+    if (threadIdx.x == 0) *go = 1;
+}
+__global__ void __launch_bounds__(COPY_THREADS)
+k_trim(opattr_cache kv, const int32_t *seqs, const int32_t *lengths, const int32_t *old, const int32_t *go) {
+    pdl_wait();
+    if (*go == 0) return;
+    const int i = blockIdx.x, s = seqs[i], held = pages_for(old[i], kv.page_size);
+    const int keep = pages_for(lengths ? lengths[i] : 0, kv.page_size);
+    int low = INT32_MAX;
+    for (int j = keep + blockIdx.y * COPY_THREADS + threadIdx.x; j < held; j += gridDim.y * COPY_THREADS) {
+        int32_t *e = &kv.table[(int64_t)s * kv.pages_per_seq + j];
+        const int page = *e;
+        *e = -1;
+        if (page >= 0 && page < kv.n_pages && atomicSub(&kv.refs[page], 1) == 1) low = min(low, page);
+    }
+    low = __reduce_min_sync(0xffffffffu, low);
+    if (lane_id() == 0 && low < INT32_MAX) atomicMin(kv.low, low);
+}
+
+opattr_status do_cache_trim(Ctx &c, Serve &s, const opattr_cache *kv, const int32_t *seqs, const int32_t *lengths,
+                            int32_t n) {
+    opattr_status st = seqs_ok(kv, seqs, n);
+    if (st || n == 0) return st;
+    if ((st = serve_ready(c, s, 0))) return st;
+    if ((st = ensure_arena(c, Need().add<int32_t>(1).add<int32_t>(n).add<int32_t>(kv->n_seqs).bytes))) return st;
+    Arena a(c);
+    int32_t *go = a.take<int32_t>(1), *old = a.take<int32_t>(n), *mark = a.take<int32_t>(kv->n_seqs);
+    launch(c, "trim_plan", k_trim_plan, dim3(1), dim3(PLAN_THREADS), 0, *kv, seqs, lengths, n, mark, old, go, s.err);
+    launch(c, "trim", k_trim, dim3(n, grid_for(kv->pages_per_seq, 4 * COPY_THREADS, 64)), dim3(COPY_THREADS), 0, *kv, seqs,
+           lengths, (const int32_t *)old, (const int32_t *)go);
+    return cuda_status(c, c.last_error);
+}
+
+// ---------------------------------------------------------------- compact
+// L pages are live.  The live ones at L and past it, in order, move into the
+// free ones below L, in order: as many of the one as of the other, so no page
+// is read after it was written and none moves twice.
+constexpr int TILE_PAGES = 4096;
+
+__device__ __forceinline__ int live_in(const opattr_cache &kv, int64_t from, int64_t to, int *warp_buf) {
+    int mine = 0;
+    for (int64_t i = from + threadIdx.x; i < to; i += blockDim.x) mine += kv.refs[i] > 0;
+    return block_sum(mine, warp_buf);
+}
+__global__ void __launch_bounds__(PLAN_THREADS) k_compact_count(opattr_cache kv, int32_t *tile_live) {
+    __shared__ int warp_buf[33];
+    pdl_wait();
+    const int64_t at = (int64_t)blockIdx.x * TILE_PAGES;
+    const int live = live_in(kv, at, min(at + TILE_PAGES, kv.n_pages), warp_buf);
+    if (threadIdx.x == 0) tile_live[blockIdx.x] = live;
+}
+// rank[page] of the pages that move, hole[rank] where they go.
+__global__ void __launch_bounds__(PLAN_THREADS)
+k_compact_place(opattr_cache kv, const int32_t *tile_live, int tiles, int32_t *rank, int32_t *hole, int32_t *mover,
+                int32_t *counts, int32_t *out_live) {
+    __shared__ int warp_buf[33];
+    pdl_wait();
+    const int tile = blockIdx.x;
+    int all = 0, before = 0;
+    for (int t = threadIdx.x; t < tiles; t += blockDim.x) {
+        all += tile_live[t];
+        if (t < tile) before += tile_live[t];
+    }
+    const int L = block_sum(all, warp_buf);
+    before = block_sum(before, warp_buf);
+    // live pages below L
+    const int edge = L / TILE_PAGES;
+    int below = 0;
+    for (int t = threadIdx.x; t < edge; t += blockDim.x) below += tile_live[t];
+    below = block_sum(below, warp_buf) + live_in(kv, (int64_t)edge * TILE_PAGES, L, warp_buf);
+    const int64_t at = (int64_t)tile * TILE_PAGES + 4 * threadIdx.x;
+    int r[4], mine = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        r[q] = at + q < kv.n_pages ? kv.refs[at + q] : 0;
+        mine += r[q] > 0;
+    }
+    int live = before + block_exclusive_scan(mine, warp_buf, (int *)nullptr);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int64_t i = at + q;
+        if (i < L && r[q] == 0) hole[i - live] = (int)i;
+        if (i >= L && r[q] > 0) {
+            rank[i] = live - below;
+            mover[live - below] = (int)i;
+        }
+        live += r[q] > 0;
+    }
+    if (tile == 0 && threadIdx.x == 0) {
+        counts[0] = L - below;
+        counts[1] = L;
+        if (out_live) *out_live = L;
+    }
+}
+// Pages over the grid, 16 bytes a thread; then the tables.
+__global__ void __launch_bounds__(COPY_THREADS)
+k_compact_move(opattr_cache kv, const int32_t *rank, const int32_t *hole, const int32_t *mover, const int32_t *counts) {
+    pdl_wait();
+    const int moves = counts[0], L = counts[1];
+    const int64_t page = (int64_t)kv.kv_heads * kv.page_size * (kv.head_dim / 8), all = moves * page;
+    const int64_t t0 = (int64_t)blockIdx.x * COPY_THREADS + threadIdx.x, step = (int64_t)gridDim.x * COPY_THREADS;
+    uint4 *kp = reinterpret_cast<uint4 *>(kv.k_pages), *vp = reinterpret_cast<uint4 *>(kv.v_pages);
+    for (int64_t x = t0; x < all; x += step) {
+        const int64_t m = x / page, e = x % page, src = mover[m] * page + e, dst = hole[m] * page + e;
+        kp[dst] = kp[src];
+        vp[dst] = vp[src];
+    }
+    for (int64_t m = t0; m < moves; m += step) {
+        kv.refs[hole[m]] = kv.refs[mover[m]];
+        kv.refs[mover[m]] = 0;
+    }
+    const int64_t entries = (int64_t)kv.n_seqs * kv.pages_per_seq;
+    for (int64_t x = t0; x < entries; x += step) {
+        const int e = kv.table[x];
+        if (e >= L && e < kv.n_pages) {
+            const int r = rank[e];
+            if (r >= 0 && r < moves && mover[r] == e) kv.table[x] = hole[r];
+        }
+    }
+    if (t0 == 0) *kv.low = L;
+}
+
+opattr_status do_cache_compact(Ctx &c, Serve &s, const opattr_cache *kv, int32_t *live) {
+    if (!cache_ok(kv)) return OPATTR_E_INVALID_ARG;
+    opattr_status st = serve_ready(c, s, 0);
+    if (st) return st;
+    const int tiles = (int)((kv->n_pages + TILE_PAGES - 1) / TILE_PAGES);
+    if ((st = ensure_arena(c, Need().add<int32_t>(2).add<int32_t>(tiles).add<int32_t>(kv->n_pages).add<int32_t>(kv->n_pages)
+                                  .add<int32_t>(kv->n_pages).bytes)))
+        return st;
+    Arena a(c);
+    int32_t *counts = a.take<int32_t>(2), *tile_live = a.take<int32_t>(tiles), *rank = a.take<int32_t>(kv->n_pages);
+    int32_t *hole = a.take<int32_t>(kv->n_pages), *mover = a.take<int32_t>(kv->n_pages);
+    launch(c, "compact_count", k_compact_count, dim3(tiles), dim3(PLAN_THREADS), 0, *kv, tile_live);
+    launch(c, "compact_place", k_compact_place, dim3(tiles), dim3(PLAN_THREADS), 0, *kv, (const int32_t *)tile_live, tiles,
+           rank, hole, mover, counts, live);
+    launch(c, "compact_move", k_compact_move, dim3(8 * sm_count(c)), dim3(COPY_THREADS), 0, *kv, (const int32_t *)rank,
+           (const int32_t *)hole, (const int32_t *)mover, (const int32_t *)counts);
+    return cuda_status(c, c.last_error);
+}
+
+}  // namespace opattr
