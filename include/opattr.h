@@ -525,7 +525,7 @@ typedef enum { OPATTR_BF16 = 0, OPATTR_F16 = 1 } opattr_dtype;
 
 /* Rows of heads, DEVICE memory: element e of head h of row t is
  * data[t * token_stride + h * head_stride + e].  Strides count elements and
- * are multiples of 8; data is 16-byte aligned. */
+ * are multiples of 8, the token stride at least 8; data is 16-byte aligned. */
 typedef struct {
     void *data;
     int64_t token_stride;
@@ -628,9 +628,10 @@ opattr_status opattr_cache_trim(opattr_ctx *ctx, const opattr_cache *cache, cons
 opattr_status opattr_cache_compact(opattr_ctx *ctx, const opattr_cache *cache, int32_t *live);
 
 /* Waits for the context's stream and returns what the calls above found wrong
- * on the device since the last check: OPATTR_OK, OPATTR_E_INVALID_ARG, or
- * OPATTR_E_PAGES (of both, the first of these two).  The context stays usable.  Collects the
- * timing of their launches (opattr_set_timing) too. */
+ * on the device since the last check: OPATTR_OK, OPATTR_E_INVALID_ARG,
+ * OPATTR_E_PAGES, or OPATTR_E_TIMEOUT where a bounded wait gave up (then the
+ * results do not count).  The context stays usable.  Collects the timing of
+ * their launches (opattr_set_timing) too. */
 opattr_status opattr_check(opattr_ctx *ctx);
 
 #ifdef __cplusplus

@@ -467,7 +467,7 @@ def _rows(t, heads: int | None, dim: int, like, name, device) -> Rows:
     st, sh, se = t.stride()
     n, h, _ = t.shape
     p = t.data_ptr()
-    if (se != 1 and dim > 1) or p % 16 or (n > 1 and (st % 8 or st < 0)) or (h > 1 and (sh % 8 or sh < 0)):
+    if (se != 1 and dim > 1) or p % 16 or (n > 1 and (st % 8 or st < 8)) or (h > 1 and (sh % 8 or sh < 0)):
         raise ValueError(f"{name}: a row's elements must be contiguous and rows 16-byte aligned")
     return Rows(p, st if n > 1 else h * dim, sh if h > 1 else dim)
 

@@ -684,6 +684,7 @@ opattr_status opattr_check(opattr_ctx *ctx) {
     if (e != cudaSuccess || c.last_error != cudaSuccess) return finish(c, cuda_status(c, e));
     if (ctx->serve.err) found = c.h_small[0];
     if (c.timing) timing_collect(c);
+    if (found & SERVE_TIMEOUT) return OPATTR_E_TIMEOUT;
     return found & SERVE_INVALID ? OPATTR_E_INVALID_ARG : found & SERVE_PAGES ? OPATTR_E_PAGES : OPATTR_OK;
 }
 

@@ -13,6 +13,7 @@ namespace opattr {
 enum ServeErr : unsigned {
     SERVE_INVALID = 1u,   // an offset, sequence, length or page that is out of range
     SERVE_PAGES = 2u,     // no free page left
+    SERVE_TIMEOUT = 4u,   // a bounded wait gave up
 };
 
 // Device state of the context's operators, made by the first of their calls.

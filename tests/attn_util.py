@@ -6,7 +6,7 @@ import math
 
 import torch
 
-UNIT = {torch.bfloat16: 2.0 ** -9, torch.float16: 2.0 ** -12}      # half a spacing, relative
+UNIT = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}      # half a spacing, relative: 8 and 11 significant bits
 TINY = {torch.bfloat16: 2.0 ** -134, torch.float16: 2.0 ** -25}    # half the smallest spacing
 
 
