@@ -678,7 +678,8 @@ opattr_status opattr_check(opattr_ctx *ctx) {
     cudaError_t e = cudaSuccess;
     if (ctx->serve.err) {
         e = cudaMemcpyAsync(c.h_small, ctx->serve.err, sizeof(unsigned), cudaMemcpyDeviceToHost, c.stream);
-        if (e == cudaSuccess) e = cudaMemsetAsync(ctx->serve.err, 0, sizeof(unsigned), c.stream);
+        // (with the count of work items, which a wait that gave up may leave behind)
+        if (e == cudaSuccess) e = cudaMemsetAsync(ctx->serve.err, 0, 256, c.stream);
     }
     if (e == cudaSuccess) e = cudaStreamSynchronize(c.stream);
     if (e != cudaSuccess || c.last_error != cudaSuccess) return finish(c, cuda_status(c, e));

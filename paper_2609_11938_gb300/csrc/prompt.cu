@@ -6,6 +6,7 @@
 // A row that sees no key gets o = 0 and lse = -inf.
 #include <math.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "tc.cuh"
@@ -23,10 +24,11 @@ bool rows_ok(const opattr_rows &r, int64_t tokens, int heads, int dim) {
 constexpr int KEYS = 128;                // keys of a tile
 constexpr int ROWS = 128;                // queries of a sub-tile: one thread and one lane of tensor memory each
 constexpr int THREADS = 384;             // two warpgroups for the softmax of two sub-tiles, one for the rest
-constexpr int MMA_WARP = 8, LOAD_WARP = 9, TAIL_WARP = 10;
+constexpr int MMA_WARP = 8, LOAD_WARP = 9, TAIL_WARP = 10;   // and the last one looks up items
 // registers: 384 x 168 at launch = 256 x 208 + 128 x 88
 constexpr int REGS_SOFTMAX = 208, REGS_OTHERS = 88;
-constexpr int MOST_MASKED = 4;           // key tiles that an item's masks cut: three at most (256 queries)
+constexpr int CUTS = 4;                  // value tiles cut by a mask that can be under way: half the ring's stages
+constexpr int ITEMS = 3;                 // work items looked up ahead
 
 // Shapes by the padded head width DP (64 or 128; the copies fill what a head
 // lacks with zeros).
@@ -36,26 +38,63 @@ struct Shape {
     static constexpr int TILE = DP / 64 * HALF;
     static constexpr int STAGES = DP == 128 ? 5 : 8;       // key and value tiles in flight
     static constexpr int SMEM = 2 * TILE + STAGES * TILE + 1024 /* alignment */;
+    static_assert(STAGES <= 2 * CUTS, "a cut tile's slot is taken again only once its stage was free");
 };
 
 struct PromptArgs {
     opattr_prompt a;
     int heads_x;                         // work items side by side: pairs of heads, or heads
     int pair;                            // 1: an item's sub-tiles are two heads of one key head; 0: 256 queries of one
-    int tiles;                           // upper bound of query tiles over the sequences
+    int tiles;                           // places of query tiles
     int q_mul, k_mul, v_mul;             // 0 where all heads read the same rows
+    unsigned *next;                      // items given out past each block's first; zero between launches
+};
+
+// A work item: two sub-tiles of queries of one sequence.
+struct Item {
+    int q0, lq, k0, lk;                  // the sequence's rows
+    int t0, head0;                       // first query within it, (first) head
+    int some;                            // 0: there are no more
 };
 
 struct Ctrl {
-    uint64_t q_full, kv_full[8], kv_empty[8], s_full[2], p_full[2], o_full[2], v_full[MOST_MASKED], v_ready[MOST_MASKED], drain;
+    uint64_t item_full[ITEMS], item_free[ITEMS], q_full, q_free, kv_full[8], kv_free[8];
+    uint64_t s_full[2], p_half[2], p_full[2], o_full[2], o_free[2], v_full[CUTS], v_ready[CUTS], drain;
     uint32_t tmem;
     int stop;
-    int poison[MOST_MASKED];
-    int item[4];                         // sequence, tile, -1: none
-    int scan[33];
+    int poison[CUTS];
+    Item item[ITEMS];
 };
 
-// 16-bit value i of a swizzled tile's row r, columns 32 * at .. + 32, four to a register pair.
+// A place in a ring of N, and the parity of its barrier.
+template <int N>
+struct Place {
+    int at = 0, ph = 0;
+    __device__ __forceinline__ void step() {
+        if (++at == N) at = 0, ph ^= 1;
+    }
+};
+
+// What an item's sub-tiles have to do.
+struct Work {
+    int base[2], tiles[2], clean[2];     // first query; key tiles; the first of them that a mask cuts
+    int n, cut, ahead;                   // key tiles of either; the first that is looked over; query i sees keys up to i + ahead
+    __device__ __forceinline__ Work(const Item &it, int pair, int causal) {
+        ahead = it.lk - it.lq;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            base[s] = pair ? it.t0 : it.t0 + s * ROWS;
+            const int rows = min(ROWS, it.lq - base[s]);
+            const int keys = rows <= 0 ? 0 : causal ? max(0, min(it.lk, base[s] + rows + ahead)) : it.lk;
+            tiles[s] = (keys + KEYS - 1) / KEYS;
+            clean[s] = (causal ? max(0, min(it.lk, base[s] + 1 + ahead)) : it.lk) / KEYS;
+        }
+        n = max(tiles[0], tiles[1]);
+        cut = tiles[1] > 0 ? min(clean[0], clean[1]) : clean[0];
+    }
+};
+
+// Byte of column `col` in row r of a swizzled tile.
 __device__ __forceinline__ uint32_t tile_at(int half_bytes, int r, int col) {
     return (uint32_t)((col >> 6) * half_bytes + r * 128 + (((col & 63) * 2) ^ ((r & 7) << 4)));
 }
@@ -64,6 +103,18 @@ __device__ __forceinline__ uint32_t tm_ld1(uint32_t at) {
     uint32_t r;
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(at));
     return r;
+}
+
+// The next item for a whole warp: numbers past the blocks' own, in order.  Every
+// block draws until it is told that there are none, so `total` are drawn in all, and
+// the last one puts the count back to zero.
+__device__ __forceinline__ long long draw(unsigned *next, long long total) {
+    unsigned k = 0;
+    if (lane_id() == 0) {
+        k = atomicAdd(next, 1u);
+        if (k == total - 1) atomicExch(next, 0u);
+    }
+    return (long long)gridDim.x + __shfl_sync(0xffffffffu, k, 0);
 }
 
 template <typename T, int DP>
@@ -83,204 +134,207 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
     const uint32_t sq = smem_addr(smem), skv = sq + 2 * S::TILE;
     const int warp = threadIdx.x >> 5;
     volatile int *stop = &ctl.stop;
+    const opattr_prompt &a = p.a;
+    const uint32_t bar_kv = smem_addr(&ctl.kv_full[0]), bar_free = smem_addr(&ctl.kv_free[0]);
     if (threadIdx.x == 0) {
-        bar_init(smem_addr(&ctl.q_full), 1);
-        for (int i = 0; i < S::STAGES; ++i) bar_init(smem_addr(&ctl.kv_full[i]), 1), bar_init(smem_addr(&ctl.kv_empty[i]), 1);
+        for (int i = 0; i < ITEMS; ++i) bar_init(smem_addr(&ctl.item_full[i]), 1), bar_init(smem_addr(&ctl.item_free[i]), 11);
+        bar_init(smem_addr(&ctl.q_full), 1), bar_init(smem_addr(&ctl.q_free), 1);
+        for (int i = 0; i < S::STAGES; ++i) bar_init(bar_kv + 8 * i, 1), bar_init(bar_free + 8 * i, 1);
         for (int i = 0; i < 2; ++i) {
             bar_init(smem_addr(&ctl.s_full[i]), 1);
+            bar_init(smem_addr(&ctl.p_half[i]), 4);
             bar_init(smem_addr(&ctl.p_full[i]), 4);
             bar_init(smem_addr(&ctl.o_full[i]), 1);
+            bar_init(smem_addr(&ctl.o_free[i]), 4);
         }
-        for (int i = 0; i < MOST_MASKED; ++i)
-            bar_init(smem_addr(&ctl.v_full[i]), 1), bar_init(smem_addr(&ctl.v_ready[i]), 2), ctl.poison[i] = 0;
+        for (int i = 0; i < CUTS; ++i) bar_init(smem_addr(&ctl.v_full[i]), 1), bar_init(smem_addr(&ctl.v_ready[i]), 1);
         bar_init(smem_addr(&ctl.drain), 1);
         ctl.stop = 0;
-        ctl.item[0] = -1;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         map_prefetch(&mq), map_prefetch(&mk), map_prefetch(&mv);
     }
     if (warp == MMA_WARP) tm_alloc(smem_addr(&ctl.tmem), 512);
-    pdl_wait();
-
-    // ---- the item: query tiles run from the last one to the first, so that the
-    // longest of a causal sequence come first; heads side by side share keys in L2
-    const opattr_prompt &a = p.a;
-    const int per = p.pair ? ROWS : 2 * ROWS;
-    const int hx = blockIdx.x % p.heads_x;
-    {
-        const int want = p.tiles - 1 - (int)(blockIdx.x / p.heads_x);
-        int before = 0;
-        bool bad = threadIdx.x == 0 && (a.q_offsets[0] != 0 || a.q_offsets[a.n_seqs] != a.q_tokens || a.k_offsets[0] != 0 ||
-                                        a.k_offsets[a.n_seqs] != a.k_tokens);
-        for (int b0 = 0; b0 < a.n_seqs; b0 += THREADS) {
-            const int b = b0 + threadIdx.x;
-            int mine = 0;
-            if (b < a.n_seqs) {
-                const int q0 = a.q_offsets[b], q1 = a.q_offsets[b + 1], k0 = a.k_offsets[b], k1 = a.k_offsets[b + 1];
-                if (q0 < 0 || q1 < q0 || q1 > a.q_tokens || k0 < 0 || k1 < k0 || k1 > a.k_tokens) bad = true;
-                else mine = (q1 - q0 + per - 1) / per;
-            }
-            int sum;
-            const int at = before + block_exclusive_scan(mine, ctl.scan, &sum);
-            if (want >= at && want < at + mine) ctl.item[0] = b, ctl.item[1] = want - at;
-            before += sum;
-            if (before > p.tiles) break;                 // only where an offset is wrong
-        }
-        if (bad) atomicOr(err, SERVE_INVALID);
-        // after a wait that gave up nothing more is begun
-        if (threadIdx.x == 0 && (*(volatile unsigned *)err & SERVE_TIMEOUT)) ctl.stop = 2;
-    }
     tm_before();
     __syncthreads();
     tm_after();
-    const uint32_t tm = ctl.tmem;
-    const int b = ctl.item[0];
-    if (b >= 0 && *stop == 0) {
-    const int q0 = a.q_offsets[b], lq = a.q_offsets[b + 1] - q0, k0 = a.k_offsets[b], lk = a.k_offsets[b + 1] - k0;
-    const int t0 = ctl.item[1] * per, ahead = lk - lq;   // query i sees the keys up to i + ahead
-    const int head0 = p.pair ? 2 * hx : hx, g = head0 / (a.q_heads / a.kv_heads);
-    // each sub-tile: its first query, its key tiles, and the first of them that a mask cuts
-    int base[2], n_tiles[2], clean[2];
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-        base[s] = p.pair ? t0 : t0 + s * ROWS;
-        const int rows = min(ROWS, lq - base[s]);
-        const int keys = rows <= 0 ? 0 : a.causal ? max(0, min(lk, base[s] + rows + ahead)) : lk;
-        n_tiles[s] = (keys + KEYS - 1) / KEYS;
-        clean[s] = (a.causal ? max(0, min(lk, base[s] + 1 + ahead)) : lk) / KEYS;
-    }
-    const int n = max(n_tiles[0], n_tiles[1]);
-    const int cut = n_tiles[1] > 0 ? min(clean[0], clean[1]) : clean[0];     // tiles from here on are looked over
-    const uint32_t bar_kv = smem_addr(&ctl.kv_full[0]), bar_free = smem_addr(&ctl.kv_empty[0]);
+    constexpr uint32_t tm = 0;                           // all of the tensor memory: its first column is column 0
+    pdl_wait();
+
+    // the next item, for a whole warp; its slot is given back by item_done
+    Place<ITEMS> slot;
+    auto item_next = [&](Item &it) {
+        if (!warp_wait(smem_addr(&ctl.item_full[slot.at]), slot.ph, stop)) return false;
+        it = ctl.item[slot.at];
+        __syncwarp();
+        if (lane_id() == 0) bar_arrive(smem_addr(&ctl.item_free[slot.at]));
+        slot.step();
+        return it.some != 0;
+    };
 
     if (warp < 8) {
-        regs_more<REGS_SOFTMAX>();
         // ---- softmax: a warpgroup per sub-tile, a thread per query
+        regs_more<REGS_SOFTMAX>();
         const int s = warp >> 2, r = threadIdx.x & 127;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t ts = tm + s * 128 + lanes, to = tm + 256 + s * DP + lanes;
+        const uint32_t b_s = smem_addr(&ctl.s_full[s]), b_half = smem_addr(&ctl.p_half[s]), b_p = smem_addr(&ctl.p_full[s]);
         const float c = a.scale == 0.f ? 1.f : fabsf(a.scale) * LOG2E;
         const float sign = a.scale < 0.f ? -1.f : 0.f;
         const bool turn = !(a.scale > 0.f);
-        const int head = p.pair ? head0 + s : head0, row = base[s] + r;
-        const int seen = a.causal ? min(lk, row + 1 + ahead) : lk;
         const uint64_t c2 = pair(c, c);
-        float m = -INFINITY, l = 0.f;
+        Place<1> turn_s, turn_o;
+        Place<CUTS> over;                                // cut value tiles, of either sub-tile
+        Place<S::STAGES> ring;                           // value tiles
+        ring.step();
+        Item it;
         bool ok = true;
-        for (int j = 0; j < n_tiles[s]; ++j) {
-            if (!(ok = warp_wait(smem_addr(&ctl.s_full[s]), j & 1, stop))) break;
-            tm_after();
-            uint32_t x[KEYS];
+        while (ok && item_next(it)) {
+            const Work w(it, p.pair, a.causal);
+            const int n_tiles = s ? w.tiles[1] : w.tiles[0], clean = s ? w.clean[1] : w.clean[0];
+            const int head = p.pair ? it.head0 + s : it.head0, row = (s ? w.base[1] : w.base[0]) + r;
+            const int seen = a.causal ? min(it.lk, row + 1 + w.ahead) : it.lk;
+            float m = -INFINITY, l = 0.f;
+            for (int j = 0; j < w.n; ++j) {
+                if (j < n_tiles) {
+                    if (!(ok = warp_wait(b_s, turn_s.ph, stop))) break;
+                    turn_s.step();
+                    tm_after();
+                    uint32_t x[KEYS];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) tm_ld32(ts + 32 * q, x + 32 * q);
-            tm_wait_ld();
-            if (turn) {
+                    for (int q = 0; q < 4; ++q) tm_ld32(ts + 32 * q, x + 32 * q);
+                    tm_wait_ld();
+                    if (turn) {
 #pragma unroll
-                for (int i = 0; i < KEYS; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * sign);
-            }
-            if (j >= clean[s]) {
-                const int left = seen - j * KEYS;
-#pragma unroll
-                for (int i = 0; i < KEYS; ++i) x[i] = i < left ? x[i] : 0xff800000u;
-            }
-            float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-            for (int i = 0; i < KEYS; i += 8)
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    t[q] = fmaxf(t[q], fmaxf(__uint_as_float(x[i + 2 * q]), __uint_as_float(x[i + 2 * q + 1])));
-            const float top = fmaxf(m, fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])));
-            if (__any_sync(0xffffffffu, (top - m) * c > SLACK)) {
-                const float keep = top == m ? 1.f : exp2_fast((m - top) * c);
-                m = top;
-                l *= keep;
-                if (j > 0) {
-                    const uint64_t keep2 = pair(keep, keep);
-                    for (int d = 0; d < DP; d += 32) {
-                        uint32_t o[32];
-                        tm_ld32(to + d, o);
-                        tm_wait_ld();
-#pragma unroll
-                        for (int i = 0; i < 32; i += 2) {
-                            const float2 y = unpair(mul2(pair(__uint_as_float(o[i]), __uint_as_float(o[i + 1])), keep2));
-                            o[i] = __float_as_uint(y.x), o[i + 1] = __float_as_uint(y.y);
-                        }
-                        tm_st32(to + d, o);
+                        for (int i = 0; i < KEYS; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * sign);
                     }
-                }
-            }
-            const float from = m == -INFINITY ? OFFSET : __fmaf_rn(-m, c, OFFSET);
-            const uint64_t from2 = pair(from, from);
-            uint64_t sum[2] = {0, 0};
+                    if (j >= clean) {
+                        const int left = seen - j * KEYS;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                uint32_t y[16];
+                        for (int i = 0; i < KEYS; ++i) x[i] = i < left ? x[i] : 0xff800000u;
+                    }
+                    float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int e = 32 * q + 2 * i;
-                    const float2 z = unpair(fma2(pair(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), c2, from2));
-                    const float lo = exp2_fast(z.x), hi = exp2_fast(z.y);
-                    sum[i & 1] = add2(sum[i & 1], pair(lo, hi));
-                    y[i] = Type2<T>::down(lo, hi);
-                }
-                tm_st16(ts + 16 * q, y);
-            }
-            const float2 z = unpair(add2(sum[0], sum[1]));
-            l += z.x + z.y;
-            tm_wait_st();
-            if (a.causal && j >= cut) {
-                // a value that is not finite times a weight of zero would reach the rows
-                // that do not see it: such a tile's products are made here, key by key
-                if (!(ok = warp_wait(smem_addr(&ctl.v_ready[j - cut]), 0, stop))) break;
-                if (*(volatile int *)&ctl.poison[j - cut]) {
-                    const unsigned char *v = smem + 2 * S::TILE + (2 * j + 1) % S::STAGES * S::TILE;
-                    const int left = seen - j * KEYS;
-                    for (int d = 0; d < DP; d += 32) {
-                        uint32_t o[32] = {};
+                    for (int i = 0; i < KEYS; i += 8)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+                            t[q] = max3(t[q], __uint_as_float(x[i + 2 * q]), __uint_as_float(x[i + 2 * q + 1]));
+                    const float top = fmaxf(max3(m, t[0], t[1]), fmaxf(t[2], t[3]));
+                    if (__any_sync(0xffffffffu, (top - m) * c > SLACK)) {
+                        const float keep = top == m ? 1.f : exp2_fast((m - top) * c);
+                        m = top;
+                        l *= keep;
                         if (j > 0) {
-                            tm_ld32(to + d, o);
-                            tm_wait_ld();
-                        }
-                        for (int i = 0; i < KEYS; ++i) {
-                            const uint32_t w = tm_ld1(ts + i / 2);
-                            tm_wait_ld();
-                            const float2 w2 = Type2<T>::up(w);
-                            const float weight = i & 1 ? w2.y : w2.x;
+                            // (the scores are there, so the products before them are done)
+                            const uint64_t keep2 = pair(keep, keep);
+                            for (int d = 0; d < DP; d += 32) {
+                                uint32_t o[32];
+                                tm_ld32(to + d, o);
+                                tm_wait_ld();
 #pragma unroll
-                            for (int e = 0; e < 32; e += 8) {
-                                const uint4 u = *reinterpret_cast<const uint4 *>(v + tile_at(S::HALF, i, d + e));
-                                const uint32_t uu[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-                                for (int q = 0; q < 4; ++q) {
-                                    const float2 y = Type2<T>::up(uu[q]);
-                                    uint32_t *z = o + e + 2 * q;
-                                    if (i < left) {
-                                        z[0] = __float_as_uint(__fmaf_rn(weight, y.x, __uint_as_float(z[0])));
-                                        z[1] = __float_as_uint(__fmaf_rn(weight, y.y, __uint_as_float(z[1])));
-                                    }
+                                for (int i = 0; i < 32; i += 2) {
+                                    const float2 y = unpair(mul2(pair(__uint_as_float(o[i]), __uint_as_float(o[i + 1])), keep2));
+                                    o[i] = __float_as_uint(y.x), o[i + 1] = __float_as_uint(y.y);
                                 }
+                                tm_st32(to + d, o);
                             }
                         }
-                        tm_st32(to + d, o);
                     }
+                    const float from = m == -INFINITY ? OFFSET : __fmaf_rn(-m, c, OFFSET);
+                    const uint64_t from2 = pair(from, from);
+                    uint64_t sum[2] = {0, 0};
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        uint32_t y[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int e = 32 * q + 2 * i;
+                            const float2 z = unpair(fma2(pair(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), c2, from2));
+                            const float lo = exp2_fast(z.x), hi = exp2_fast(z.y);
+                            sum[i & 1] = add2(sum[i & 1], pair(lo, hi));
+                            y[i] = Type2<T>::down(lo, hi);
+                        }
+                        tm_st16(ts + 16 * q, y);
+                        if (q == 1) {
+                            // the products with the first half of the keys may begin
+                            tm_wait_st();
+                            tm_before();
+                            __syncwarp();
+                            if (lane_id() == 0) bar_arrive(b_half);
+                        }
+                    }
+                    const float2 z = unpair(add2(sum[0], sum[1]));
+                    l += z.x + z.y;
                     tm_wait_st();
                 }
+                if (j >= w.cut) {
+                    if (a.causal && j < n_tiles) {
+                        // a value that is not finite times a weight of zero would reach the rows
+                        // that do not see it: such a tile's products are made here, key by key
+                        if (!(ok = warp_wait(smem_addr(&ctl.v_ready[over.at]), over.ph, stop))) break;
+                        if (*(volatile int *)&ctl.poison[over.at]) {
+                            const unsigned char *v = smem + 2 * S::TILE + ring.at * S::TILE;
+                            const int left = seen - j * KEYS;
+                            for (int d = 0; d < DP; d += 32) {
+                                uint32_t o[32] = {};
+                                if (j > 0) {
+                                    tm_ld32(to + d, o);
+                                    tm_wait_ld();
+                                }
+                                for (int i = 0; i < KEYS; ++i) {
+                                    const uint32_t u2 = tm_ld1(ts + i / 2);
+                                    tm_wait_ld();
+                                    const float2 w2 = Type2<T>::up(u2);
+                                    const float weight = i & 1 ? w2.y : w2.x;
+#pragma unroll
+                                    for (int e = 0; e < 32; e += 8) {
+                                        const uint4 u = *reinterpret_cast<const uint4 *>(v + tile_at(S::HALF, i, d + e));
+                                        const uint32_t uu[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                                        for (int q = 0; q < 4; ++q) {
+                                            const float2 y = Type2<T>::up(uu[q]);
+                                            uint32_t *z = o + e + 2 * q;
+                                            if (i < left) {
+                                                z[0] = __float_as_uint(__fmaf_rn(weight, y.x, __uint_as_float(z[0])));
+                                                z[1] = __float_as_uint(__fmaf_rn(weight, y.y, __uint_as_float(z[1])));
+                                            }
+                                        }
+                                    }
+                                }
+                                tm_st32(to + d, o);
+                            }
+                            tm_wait_st();
+                        }
+                    }
+                    over.step();
+                }
+                ring.step(), ring.step();
+                if (j < n_tiles) {
+                    tm_before();
+                    __syncwarp();
+                    if (lane_id() == 0) bar_arrive(b_p);
+                }
             }
-            tm_before();
-            __syncwarp();
-            if (lane_id() == 0) bar_arrive(smem_addr(&ctl.p_full[s]));
-        }
-        if (n_tiles[s] > 0 && ok) ok = warp_wait(smem_addr(&ctl.o_full[s]), 0, stop);
-        tm_after();
-        if (ok) {
-            const bool live = row < lq;
+            if (!ok) break;
+            if (n_tiles > 0) {
+                if (!(ok = warp_wait(smem_addr(&ctl.o_full[s]), turn_o.ph, stop))) break;
+                turn_o.step();
+                tm_after();
+            }
+            const bool live = row < it.lq;
             const float share = l == 0.f ? 0.f : 1.f / l;
-            T *out = (T *)a.out.data + (int64_t)(q0 + row) * a.out.token_stride + head * a.out.head_stride;
+            T *out = (T *)a.out.data + (int64_t)(it.q0 + row) * a.out.token_stride + head * a.out.head_stride;
+#pragma unroll
             for (int d = 0; d < DP; d += 32) {
                 uint32_t o[32] = {};
-                if (n_tiles[s] > 0) {
+                if (n_tiles > 0) {
                     tm_ld32(to + d, o);
                     tm_wait_ld();
+                    if (d + 32 == DP) {
+                        // the next item's products may go there
+                        tm_before();
+                        __syncwarp();
+                        if (lane_id() == 0) bar_arrive(smem_addr(&ctl.o_free[s]));
+                    }
                 }
 #pragma unroll
                 for (int e = 0; e < 32; e += 8) {
@@ -295,129 +349,260 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                 }
             }
             if (live && a.lse)
-                a.lse[(int64_t)(q0 + row) * a.q_heads + head] =
+                a.lse[(int64_t)(it.q0 + row) * a.q_heads + head] =
                     l == 0.f ? -INFINITY : (__fmaf_rn(m == -INFINITY ? 0.f : m, c, -OFFSET) + log2f(l)) * LN2;
         }
     } else {
-    regs_fewer<REGS_OTHERS>();
-    if (warp == MMA_WARP) {
-        // ---- products: one thread
-        if (lane_id() == 0 && n > 0) {
+        regs_fewer<REGS_OTHERS>();
+        if (warp == MMA_WARP) {
+            // ---- products: one thread issues them, but the whole warp walks along, so that
+            // descriptors stay in uniform registers (from one lane's branch each operand
+            // would be moved there anew: 75 cycles a product instead of the 64 that it takes)
             constexpr uint32_t DS = mma_desc(BF, ROWS, KEYS, false), DO = mma_desc(BF, ROWS, DP, true);
-            auto scores = [&](int s, int j) {
-                const uint32_t qa = sq + s * S::TILE, ka = skv + (j == 0 ? 0 : 2 * j) % S::STAGES * S::TILE;
+            const bool lead = elect();
+            // descriptors count in 16 bytes: a tile's is its first one's and an offset
+            const uint64_t qdesc = tile_desc(sq, 16), kdesc = tile_desc(skv, 16), vdesc = tile_desc(skv, S::HALF);
+            Place<S::STAGES> keys, values;
+            Place<CUTS> over;
+            Place<1> q_turn, s_turn[2], o_turn[2];
+            auto scores = [&](int s, int st) {
+                const uint64_t qd = qdesc + s * (S::TILE >> 4), kd = kdesc + st * (S::TILE >> 4);
+                if (lead) {
 #pragma unroll
-                for (int k = 0; k < DP / 16; ++k) {
-                    const uint32_t off = (k / 4) * S::HALF + (k % 4) * 32;
-                    mma_ss(tm + s * 128, tile_desc(qa + off, 16), tile_desc(ka + off, 16), DS, k > 0);
-                }
-                mma_commit(smem_addr(&ctl.s_full[s]));
-            };
-            auto full = [&](int load) { return bar_wait(bar_kv + load % S::STAGES * 8, load / S::STAGES & 1, stop); };
-            auto release = [&](int load) { mma_commit(bar_free + load % S::STAGES * 8); };
-            bool ok = bar_wait(smem_addr(&ctl.q_full), 0, stop) && full(0);
-            if (ok) {
-                tm_after();
-                for (int s = 0; s < 2; ++s)
-                    if (n_tiles[s] > 0) scores(s, 0);
-                release(0);
-            }
-            for (int j = 0; ok && j < n; ++j) {
-                const bool more = j + 1 < n;
-                if (!(ok = full(2 * j + 1))) break;
-                if (j >= cut && !(ok = bar_wait(smem_addr(&ctl.v_ready[j - cut]), 0, stop))) break;
-                if (more && !(ok = full(2 * j + 2))) break;
-                const bool by_hand = a.causal && j >= cut && *(volatile int *)&ctl.poison[j - cut];
-                const uint32_t va = skv + (2 * j + 1) % S::STAGES * S::TILE;
-                for (int s = 0; s < 2; ++s) {
-                    if (j >= n_tiles[s]) continue;
-                    if (!(ok = bar_wait(smem_addr(&ctl.p_full[s]), j & 1, stop))) break;
-                    tm_after();
-                    if (!by_hand) {
-#pragma unroll
-                        for (int k = 0; k < KEYS / 16; ++k)
-                            mma_ts(tm + 256 + s * DP, tm + s * 128 + 8 * k, tile_desc(va + k * 2048, S::HALF), DO, j > 0 || k > 0);
+                    for (int k = 0; k < DP / 16; ++k) {
+                        const int off = (k / 4) * (S::HALF >> 4) + (k % 4) * 2;
+                        mma_ss(tm + s * 128, qd + off, kd + off, DS, k > 0);
                     }
-                    if (j + 1 < n_tiles[s]) scores(s, j + 1);
-                    else mma_commit(smem_addr(&ctl.o_full[s]));
+                    mma_commit(smem_addr(&ctl.s_full[s]));
                 }
-                if (!ok) break;
-                release(2 * j + 1);
-                if (more) release(2 * j + 2);
+            };
+            auto full = [&](const Place<S::STAGES> &x) { return warp_wait(bar_kv + x.at * 8, x.ph, stop); };
+            auto release = [&](int st) {
+                if (lead) mma_commit(bar_free + st * 8);
+            };
+            bool ok = true;
+            Item it;
+            while (ok && item_next(it)) {
+                const Work w(it, p.pair, a.causal);
+                const int nt = uniform(w.n), nt0 = uniform(w.tiles[0]), nt1 = uniform(w.tiles[1]), from = uniform(w.cut);
+                if (nt == 0) continue;
+                bool by_hand = false;
+                // values of tile j and keys of tile j + 1
+                auto next = [&](int j) {
+                    values = keys;
+                    values.step();
+                    keys = values;
+                    keys.step();
+                    if (!full(values) || (j + 1 < nt && !full(keys))) return false;
+                    by_hand = false;
+                    if (j >= from) {
+                        if (!warp_wait(smem_addr(&ctl.v_ready[over.at]), over.ph, stop)) return false;
+                        by_hand = a.causal && uniform(*(volatile int *)&ctl.poison[over.at]);
+                        over.step();
+                    }
+                    return true;
+                };
+                if (!(ok = warp_wait(smem_addr(&ctl.q_full), q_turn.ph, stop) && full(keys))) break;
+                q_turn.step();
+                tm_after();
+                if (nt0 > 0) scores(0, keys.at);
+                if (nt1 > 0) scores(1, keys.at);
+                release(keys.at);
+                if (nt == 1 && lead) mma_commit(smem_addr(&ctl.q_free));
+                if (!(ok = next(0))) break;
+                for (int j = 0; ok && j < nt; ++j) {
+                    const int vst = values.at, kst = keys.at;
+                    const uint64_t vd = vdesc + vst * (S::TILE >> 4);
+                    const bool hand = by_hand;
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        const int mine = s ? nt1 : nt0;
+                        if (j < mine) {
+                            if (!(ok = warp_wait(smem_addr(&ctl.p_half[s]), s_turn[s].ph, stop))) break;
+                            if (j == 0) {
+                                // the results before these have been read (a new barrier's parity 1 is over)
+                                if (!(ok = warp_wait(smem_addr(&ctl.o_free[s]), o_turn[s].ph ^ 1, stop))) break;
+                                o_turn[s].step();
+                            }
+                            tm_after();
+                            if (!hand && lead) {
+#pragma unroll
+                                for (int k = 0; k < KEYS / 32; ++k)
+                                    mma_ts(tm + 256 + s * DP, tm + s * 128 + 8 * k, vd + k * 128, DO, k > 0 || j > 0);
+                            }
+                            if (!(ok = warp_wait(smem_addr(&ctl.p_full[s]), s_turn[s].ph, stop))) break;
+                            s_turn[s].step();
+                            tm_after();
+                            if (!hand && lead) {
+#pragma unroll
+                                for (int k = KEYS / 32; k < KEYS / 16; ++k)
+                                    mma_ts(tm + 256 + s * DP, tm + s * 128 + 8 * k, vd + k * 128, DO, true);
+                            }
+                            if (j + 1 < mine) scores(s, kst);
+                            else if (lead) mma_commit(smem_addr(&ctl.o_full[s]));
+                        }
+                        // while the tensor cores have the first sub-tile's products to do
+                        if (s == 0 && j + 1 < nt && !(ok = next(j + 1))) break;
+                    }
+                    if (!ok) break;
+                    release(vst);
+                    if (j + 1 < nt) release(kst);
+                    if (j + 2 == nt && lead) mma_commit(smem_addr(&ctl.q_free));
+                }
+                // (after the last tile `keys` is the place of the next item's first)
             }
             // nothing of this thread's is under way when the block ends
-            mma_commit(smem_addr(&ctl.drain));
+            if (lead) mma_commit(smem_addr(&ctl.drain));
             int never = 0;
             bar_wait(smem_addr(&ctl.drain), 0, &never);
-        }
-    } else if (warp == LOAD_WARP) {
-        // ---- tile copies: one thread
-        if (lane_id() == 0 && n > 0) {
+        } else if (warp == LOAD_WARP) {
+            // ---- tile copies: one thread
+            const bool lead = elect();
             const uint32_t bq = smem_addr(&ctl.q_full);
-            const int subs = n_tiles[1] > 0 ? 2 : 1;
-            bar_expect(bq, subs * S::TILE);
-            for (int s = 0; s < subs; ++s)
-                for (int d = 0; d < DP / 64; ++d)
-                    tile_load(sq + s * S::TILE + d * S::HALF, &mq, 64 * d, (p.pair ? head0 + s : head0) * p.q_mul, q0 + base[s], bq);
-            int load = 0;
-            for (; load < 2 * n; ++load) {
-                const int st = load % S::STAGES;
-                if (load >= S::STAGES && !bar_wait(bar_free + 8 * st, (load / S::STAGES - 1) & 1, stop)) break;
-                // K0, V0, K1, V1, ..
-                const bool keys = load % 2 == 0;
-                const int j = load / 2;
-                // values that are looked over have a barrier of their own: the stage's may
-                // have gone round several times before the tail's warps see it
-                const bool over = !keys && j >= cut;
-                const uint32_t bar = over ? smem_addr(&ctl.v_full[j - cut]) : bar_kv + 8 * st;
-                bar_expect(bar, S::TILE);
-                for (int d = 0; d < DP / 64; ++d)
-                    tile_load(skv + st * S::TILE + d * S::HALF, keys ? &mk : &mv, 64 * d, keys ? g * p.k_mul : g * p.v_mul,
-                              k0 + j * KEYS, bar);
-                if (over) bar_arrive(bar_kv + 8 * st);
+            Place<S::STAGES> ring;
+            Place<CUTS> over;
+            Place<1> q_turn;
+            uint32_t bars[S::STAGES];                    // barrier of the last copy into each stage, and its parity
+            int pars[S::STAGES];
+            for (int i = 0; i < S::STAGES; ++i) bars[i] = 0;
+            bool ok = true;
+            int q_out = 0;
+            Item it;
+            while (ok && item_next(it)) {
+                const Work w(it, p.pair, a.causal);
+                if (w.n == 0) continue;
+                const int g = it.head0 / (a.q_heads / a.kv_heads), subs = w.tiles[1] > 0 ? 2 : 1;
+                if (!(ok = warp_wait(smem_addr(&ctl.q_free), q_turn.ph ^ 1, stop))) break;
+                q_turn.step();
+                if (lead) {
+                    bar_expect(bq, subs * S::TILE);
+                    for (int s = 0; s < subs; ++s)
+                        for (int d = 0; d < DP / 64; ++d)
+                            tile_load(sq + s * S::TILE + d * S::HALF, &mq, 64 * d, (p.pair ? it.head0 + s : it.head0) * p.q_mul,
+                                      it.q0 + (s ? w.base[1] : w.base[0]), bq);
+                }
+                q_out = 1;
+                for (int load = 0; load < 2 * w.n; ++load) {
+                    if (!(ok = warp_wait(bar_free + 8 * ring.at, ring.ph ^ 1, stop))) break;
+                    // K0, V0, K1, V1, ..; values that are looked over have a barrier of their own: the
+                    // stage's may have gone round several times before the tail's warp sees it
+                    const bool keys = load % 2 == 0, cut = !keys && load / 2 >= w.cut;
+                    const uint32_t bar = cut ? smem_addr(&ctl.v_full[over.at]) : bar_kv + 8 * ring.at;
+                    if (lead) {
+                        bar_expect(bar, S::TILE);
+                        for (int d = 0; d < DP / 64; ++d)
+                            tile_load(skv + ring.at * S::TILE + d * S::HALF, keys ? &mk : &mv, 64 * d, g * (keys ? p.k_mul : p.v_mul),
+                                      it.k0 + load / 2 * KEYS, bar);
+                        if (cut) bar_arrive(bar_kv + 8 * ring.at);
+                    }
+                    bars[ring.at] = bar;
+                    pars[ring.at] = cut ? over.ph : ring.ph;
+                    if (cut) over.step();
+                    ring.step();
+                }
             }
-            // copies that nobody waited for any more
+            // copies that nobody waits for any more
             int never = 0;
-            if (*stop)
-                for (int i = max(0, load - S::STAGES); i < load; ++i) {
-                    const bool over = i % 2 && i / 2 >= cut;
-                    bar_wait(over ? smem_addr(&ctl.v_full[i / 2 - cut]) : bar_kv + i % S::STAGES * 8, over ? 0 : i / S::STAGES & 1,
-                             &never);
-                }
-            if (*stop) bar_wait(bq, 0, &never);
-        }
-    } else {
-        // ---- tiles that a mask cuts, two warps: rows past the sequence's keys become
-        // zeros, and, causal, the others are looked over for values that are not finite
-        const int w = threadIdx.x - 32 * TAIL_WARP;
-        for (int j = cut; j < n; ++j) {
-            const int load = 2 * j + 1, keys = min(KEYS, lk - j * KEYS);
-            if (!warp_wait(smem_addr(&ctl.v_full[j - cut]), 0, stop)) break;
-            unsigned char *v = smem + 2 * S::TILE + load % S::STAGES * S::TILE;
-            unsigned most = 0;
-            for (int i = w; i < S::TILE / 16; i += 64) {
-                uint4 *u = reinterpret_cast<uint4 *>(v) + i;
-                if ((i * 16 % S::HALF) / 128 >= keys) *u = make_uint4(0, 0, 0, 0);
-                else if (a.causal) {
-                    const uint4 y = *u;
-                    most = __vmaxu2(most, __vmaxu2(__vmaxu2(y.x & 0x7fff7fffu, y.y & 0x7fff7fffu),
-                                                   __vmaxu2(y.z & 0x7fff7fffu, y.w & 0x7fff7fffu)));
+            if (*stop) {
+                for (int i = 0; i < S::STAGES; ++i)
+                    if (bars[i]) bar_wait(bars[i], pars[i], &never);
+                if (q_out) bar_wait(bq, q_turn.ph ^ 1, &never);
+            }
+        } else if (warp == TAIL_WARP) {
+            // ---- value tiles that a mask cuts: rows past the sequence's keys become zeros, and,
+            // causal, the others are looked over for values that are not finite
+            constexpr unsigned INF = BF ? 0x7f80u : 0x7c00u;
+            Place<CUTS> over;
+            Place<S::STAGES> ring;
+            ring.step();
+            bool ok = true;
+            Item it;
+            while (ok && item_next(it)) {
+                const Work w(it, p.pair, a.causal);
+                for (int j = 0; j < w.n; ++j, ring.step(), ring.step()) {
+                    if (j < w.cut) continue;
+                    if (!(ok = warp_wait(smem_addr(&ctl.v_full[over.at]), over.ph, stop))) break;
+                    uint4 *v = reinterpret_cast<uint4 *>(smem + 2 * S::TILE + ring.at * S::TILE);
+                    const int keys = min(KEYS, it.lk - j * KEYS);
+                    unsigned most = 0;
+                    for (int d = 0; d < DP / 64; ++d) {
+                        if (a.causal) {
+#pragma unroll 8
+                            for (int i = lane_id(); i < keys * 8; i += 32) {
+                                const uint4 y = v[d * (S::HALF / 16) + i];
+                                most = __vmaxu2(most, __vmaxu2(__vmaxu2(y.x & 0x7fff7fffu, y.y & 0x7fff7fffu),
+                                                               __vmaxu2(y.z & 0x7fff7fffu, y.w & 0x7fff7fffu)));
+                            }
+                        }
+                        for (int i = keys * 8 + lane_id(); i < S::HALF / 16; i += 32) v[d * (S::HALF / 16) + i] = make_uint4(0, 0, 0, 0);
+                    }
+                    const bool found = __any_sync(0xffffffffu, (most >> 16) >= INF || (most & 0xffffu) >= INF);
+                    fence_smem_async();
+                    __syncwarp();
+                    if (lane_id() == 0) {
+                        ctl.poison[over.at] = found;
+                        bar_arrive(smem_addr(&ctl.v_ready[over.at]));
+                    }
+                    over.step();
                 }
             }
-            constexpr unsigned INF = BF ? 0x7f80u : 0x7c00u;
-            if ((most >> 16) >= INF || (most & 0xffffu) >= INF) ctl.poison[j - cut] = 1;
-            fence_smem_async();
-            __syncwarp();
-            if (lane_id() == 0) bar_arrive(smem_addr(&ctl.v_ready[j - cut]));
+        } else {
+            // ---- work items, the longest of a causal sequence first: place x of the query
+            // tiles counts from the end.  Sequence b has the places from q_offsets[b] / per + b
+            // on, enough for its tiles whatever comes before it; those it does not need are
+            // passed over.  A block's first item is its number, others are drawn.
+            const int per = p.pair ? ROWS : 2 * ROWS;
+            const long long total = (long long)p.heads_x * p.tiles;
+            if (blockIdx.x == 0) {
+                bool bad = lane_id() == 0 && (a.q_offsets[0] != 0 || a.q_offsets[a.n_seqs] != a.q_tokens ||
+                                              a.k_offsets[0] != 0 || a.k_offsets[a.n_seqs] != a.k_tokens);
+                for (int b = lane_id(); b < a.n_seqs; b += 32)
+                    bad = bad || a.q_offsets[b + 1] < a.q_offsets[b] || a.k_offsets[b + 1] < a.k_offsets[b];
+                if (bad) atomicOr(err, SERVE_INVALID);
+            }
+            // after a wait that gave up nothing more is begun
+            bool none = uniform(*(volatile unsigned *)err & SERVE_TIMEOUT);
+            long long i = blockIdx.x;
+            for (bool more = true; more;) {
+                Item it{};
+                for (; i < total && !none;) {
+                    const int x = p.tiles - 1 - (int)(i / p.heads_x), hx = (int)(i % p.heads_x);
+                    // the last sequence whose places begin at x or before it, 32 at a time
+                    int lo = 0, n = a.n_seqs;
+                    while (n > 1) {
+                        const int step = (n + 31) / 32, b = lo + step * (int)lane_id();
+                        const bool le = step * (int)lane_id() < n && a.q_offsets[b] / per + b <= x;
+                        const int k = max(0, 31 - __clz(__ballot_sync(0xffffffffu, le)));
+                        lo += k * step;
+                        n = min(step, n - k * step);
+                    }
+                    int v = 0;
+                    if (lane_id() < 4) v = (lane_id() < 2 ? a.q_offsets : a.k_offsets)[lo + (lane_id() & 1)];
+                    const int q0 = uniform(v), q1 = __shfl_sync(0xffffffffu, v, 1);
+                    const int k0 = __shfl_sync(0xffffffffu, v, 2), k1 = __shfl_sync(0xffffffffu, v, 3);
+                    const int t0 = (x - q0 / per - lo) * per;
+                    if (q0 >= 0 && q1 >= q0 && q1 <= a.q_tokens && k0 >= 0 && k1 >= k0 && k1 <= a.k_tokens && t0 >= 0 && t0 < q1 - q0) {
+                        it = Item{q0, q1 - q0, k0, k1 - k0, t0, p.pair ? 2 * hx : hx, 1};
+                        break;
+                    }
+                    i = draw(p.next, total);
+                }
+                more = it.some != 0;
+                if (!warp_wait(smem_addr(&ctl.item_free[slot.at]), slot.ph ^ 1, stop)) break;
+                if (lane_id() == 0) {
+                    ctl.item[slot.at] = it;
+                    bar_arrive(smem_addr(&ctl.item_full[slot.at]));
+                }
+                slot.step();
+                if (more) i = draw(p.next, total);
+            }
         }
-    }
-    }
     }
     tm_before();
     __syncthreads();
-    if (threadIdx.x == 0 && *stop == 1) atomicOr(err, SERVE_TIMEOUT);
+    if (threadIdx.x == 0 && *stop) atomicOr(err, SERVE_TIMEOUT);
     __syncwarp();
-    if (warp == MMA_WARP) tm_free(tm, 512);
+    if (warp == MMA_WARP) tm_free(ctl.tmem, 512);
 }
 
 // ---------------------------------------------------------------- host
@@ -455,8 +640,9 @@ static opattr_status run_prompt(Ctx &c, Serve &s, const PromptArgs &p, const CUt
     using S = Shape<DP>;
     const cudaError_t e = cudaFuncSetAttribute(k_prompt<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
     if (e != cudaSuccess) return cuda_status(c, e);
-    launch(c, "prompt", k_prompt<T, DP>, dim3((unsigned)((int64_t)p.heads_x * p.tiles)), dim3(THREADS), S::SMEM, p, m[0], m[1],
-           m[2], s.err);
+    const int64_t items = (int64_t)p.heads_x * p.tiles;
+    launch(c, "prompt", k_prompt<T, DP>, dim3((unsigned)std::min<int64_t>(items, sm_count(c))), dim3(THREADS), S::SMEM, p, m[0],
+           m[1], m[2], s.err);
     return cuda_status(c, c.last_error);
 }
 
@@ -482,6 +668,7 @@ opattr_status do_attention(Ctx &c, Serve &s, const opattr_prompt *a) {
     if (tiles * p.heads_x > INT32_MAX) return OPATTR_E_INVALID_ARG;
     p.tiles = (int)tiles;
     p.q_mul = a->q_heads > 1 && a->q.head_stride != 0;
+    p.next = s.err + 16;                                 // its own line
     p.k_mul = a->kv_heads > 1 && a->k.head_stride != 0;
     p.v_mul = a->kv_heads > 1 && a->v.head_stride != 0;
     if (!encode_tiled()) return OPATTR_E_CUDA;

@@ -107,6 +107,15 @@ __device__ __forceinline__ void regs_more() { asm volatile("setmaxnreg.inc.sync.
 template <int N>
 __device__ __forceinline__ void regs_fewer() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
+// A value that all lanes of the warp have, told to the compiler as such.
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
+// One lane of the whole warp.
+__device__ __forceinline__ bool elect() {
+    unsigned one;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(one));
+    return one;
+}
+
 // ---------------------------------------------------------------- products
 // A tile in shared memory as a tile copy with 128-byte swizzle leaves it: rows
 // of 64 two-byte elements, eight rows to a 1,024-byte block, blocks of rows one
@@ -132,6 +141,12 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
 // The barrier's arrival once every product this thread issued so far is complete.
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
 }
 
 // ---------------------------------------------------------------- pairs of 32-bit values
