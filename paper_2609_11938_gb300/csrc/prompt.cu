@@ -47,6 +47,7 @@ struct PromptArgs {
     int pair;                            // 1: an item's sub-tiles are two heads of one key head; 0: 256 queries of one
     int tiles;                           // places of query tiles
     int q_mul, k_mul, v_mul;             // 0 where all heads read the same rows
+    int wide;                            // 1: rows of the output are 32-byte aligned and DP wide
     unsigned *next;                      // items given out past each block's first; zero between launches
 };
 
@@ -103,6 +104,12 @@ __device__ __forceinline__ uint32_t tm_ld1(uint32_t at) {
     uint32_t r;
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(at));
     return r;
+}
+
+// 32 bytes of a thread in one store: whole sectors, where rows lie far apart.
+__device__ __forceinline__ void store32(void *p, const uint32_t *r) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
 
 // The next item for a whole warp: numbers past the blocks' own, in order.  Every
@@ -178,9 +185,8 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t ts = tm + s * 128 + lanes, to = tm + 256 + s * DP + lanes;
         const uint32_t b_s = smem_addr(&ctl.s_full[s]), b_half = smem_addr(&ctl.p_half[s]), b_p = smem_addr(&ctl.p_full[s]);
-        const float c = a.scale == 0.f ? 1.f : fabsf(a.scale) * LOG2E;
-        const float sign = a.scale < 0.f ? -1.f : 0.f;
-        const bool turn = !(a.scale > 0.f);
+        // (a negative scale's sign is the products'; for none, the least that keeps -inf what it is)
+        const float c = a.scale == 0.f ? __uint_as_float(1) : fabsf(a.scale) * LOG2E;
         const uint64_t c2 = pair(c, c);
         Place<1> turn_s, turn_o;
         Place<CUTS> over;                                // cut value tiles, of either sub-tile
@@ -203,14 +209,15 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
 #pragma unroll
                     for (int q = 0; q < 4; ++q) tm_ld32(ts + 32 * q, x + 32 * q);
                     tm_wait_ld();
-                    if (turn) {
-#pragma unroll
-                        for (int i = 0; i < KEYS; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * sign);
-                    }
                     if (j >= clean) {
+                        // of the 32s of keys that a mask cuts, most are seen by all of the warp's rows
                         const int left = seen - j * KEYS;
 #pragma unroll
-                        for (int i = 0; i < KEYS; ++i) x[i] = i < left ? x[i] : 0xff800000u;
+                        for (int q = 0; q < KEYS; q += 32) {
+                            if (__all_sync(0xffffffffu, left >= q + 32)) continue;
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) x[q + i] = i < left - q ? x[q + i] : 0xff800000u;
+                        }
                     }
                     float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -226,6 +233,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                         if (j > 0) {
                             // (the scores are there, so the products before them are done)
                             const uint64_t keep2 = pair(keep, keep);
+#pragma unroll 1
                             for (int d = 0; d < DP; d += 32) {
                                 uint32_t o[32];
                                 tm_ld32(to + d, o);
@@ -274,12 +282,14 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                         if (*(volatile int *)&ctl.poison[over.at]) {
                             const unsigned char *v = smem + 2 * S::TILE + ring.at * S::TILE;
                             const int left = seen - j * KEYS;
+#pragma unroll 1
                             for (int d = 0; d < DP; d += 32) {
                                 uint32_t o[32] = {};
                                 if (j > 0) {
                                     tm_ld32(to + d, o);
                                     tm_wait_ld();
                                 }
+#pragma unroll 1
                                 for (int i = 0; i < KEYS; ++i) {
                                     const uint32_t u2 = tm_ld1(ts + i / 2);
                                     tm_wait_ld();
@@ -320,10 +330,10 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                 turn_o.step();
                 tm_after();
             }
-            const bool live = row < it.lq;
+            const bool live = row < it.lq, wide = p.wide;
             const float share = l == 0.f ? 0.f : 1.f / l;
             T *out = (T *)a.out.data + (int64_t)(it.q0 + row) * a.out.token_stride + head * a.out.head_stride;
-#pragma unroll
+#pragma unroll 1
             for (int d = 0; d < DP; d += 32) {
                 uint32_t o[32] = {};
                 if (n_tiles > 0) {
@@ -337,15 +347,17 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                     }
                 }
 #pragma unroll
-                for (int e = 0; e < 32; e += 8) {
-                    uint4 y;
-                    uint32_t *yy = reinterpret_cast<uint32_t *>(&y);
+                for (int e = 0; e < 16; ++e)
+                    o[e] = l == 0.f ? 0u : Type2<T>::down(__uint_as_float(o[2 * e]) * share, __uint_as_float(o[2 * e + 1]) * share);
+                if (live) {
+                    if (wide) {
+                        store32(out + d, o);
+                        store32(out + d + 16, o + 8);
+                    } else {
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const float lo = __uint_as_float(o[e + 2 * q]) * share, hi = __uint_as_float(o[e + 2 * q + 1]) * share;
-                        yy[q] = l == 0.f ? 0u : Type2<T>::down(lo, hi);
+                        for (int e = 0; e < 4; ++e)
+                            if (d + 8 * e < a.head_dim) *reinterpret_cast<uint4 *>(out + d + 8 * e) = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
                     }
-                    if (live && d + e < a.head_dim) *reinterpret_cast<uint4 *>(out + d + e) = y;
                 }
             }
             if (live && a.lse)
@@ -358,7 +370,8 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
             // ---- products: one thread issues them, but the whole warp walks along, so that
             // descriptors stay in uniform registers (from one lane's branch each operand
             // would be moved there anew: 75 cycles a product instead of the 64 that it takes)
-            constexpr uint32_t DS = mma_desc(BF, ROWS, KEYS, false), DO = mma_desc(BF, ROWS, DP, true);
+            const uint32_t DS = mma_desc(BF, ROWS, KEYS, false) | (a.scale < 0.f ? MMA_NEGATE : 0u);
+            constexpr uint32_t DO = mma_desc(BF, ROWS, DP, true);
             const bool lead = elect();
             // descriptors count in 16 bytes: a tile's is its first one's and an offset
             const uint64_t qdesc = tile_desc(sq, 16), kdesc = tile_desc(skv, 16), vdesc = tile_desc(skv, S::HALF);
@@ -669,6 +682,8 @@ opattr_status do_attention(Ctx &c, Serve &s, const opattr_prompt *a) {
     p.tiles = (int)tiles;
     p.q_mul = a->q_heads > 1 && a->q.head_stride != 0;
     p.next = s.err + 16;                                 // its own line
+    p.wide = a->head_dim % 64 == 0 && (reinterpret_cast<uintptr_t>(a->out.data) & 31) == 0 &&
+             (a->q_tokens == 1 || a->out.token_stride % 16 == 0) && (a->q_heads == 1 || a->out.head_stride % 16 == 0);
     p.k_mul = a->kv_heads > 1 && a->k.head_stride != 0;
     p.v_mul = a->kv_heads > 1 && a->v.head_stride != 0;
     if (!encode_tiled()) return OPATTR_E_CUDA;

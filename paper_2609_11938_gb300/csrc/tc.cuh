@@ -130,6 +130,7 @@ __host__ __device__ constexpr uint32_t mma_desc(bool bf16, int m, int n, bool b_
     return 1u << 4 | (bf16 ? 1u : 0u) << 7 | (bf16 ? 1u : 0u) << 10 | (b_rows_n ? 1u : 0u) << 16 | (uint32_t)(n >> 3) << 17 |
            (uint32_t)(m >> 4) << 24;
 }
+constexpr uint32_t MMA_NEGATE = 1u << 13;                // with -A in the place of A
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, bool add) {
     asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
                  ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"((unsigned)add) : "memory");
