@@ -14,6 +14,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 import threading
 from dataclasses import dataclass
 
@@ -187,12 +188,13 @@ def library():
             lib.opattr_match_noalloc.argtypes = [P(Kernels), P(Ncu), ctypes.c_int, _vp, _vp, P(MatchSummary), _vp]
             lib.opattr_match_noalloc.restype = ctypes.c_int
             i32, i64, f32 = ctypes.c_int32, ctypes.c_int64, ctypes.c_float
-            lib.opattr_attention.argtypes = [_vp, P(Prompt)]
-            lib.opattr_cache_attention.argtypes = [_vp, P(Cache), _vp, i32, i32, P(Rows), P(Rows), _vp, f32]
-            lib.opattr_cache_append.argtypes = [_vp, P(Cache), _vp, i32, _vp, i64, P(Rows), P(Rows)]
-            lib.opattr_cache_fork.argtypes = [_vp, P(Cache), _vp, _vp, i32]
-            lib.opattr_cache_trim.argtypes = [_vp, P(Cache), _vp, _vp, i32]
-            lib.opattr_cache_compact.argtypes = [_vp, P(Cache), _vp]
+            # (structs of these calls go by reference, or packed into bytes)
+            lib.opattr_attention.argtypes = [_vp, _vp]
+            lib.opattr_cache_attention.argtypes = [_vp, _vp, _vp, i32, i32, _vp, _vp, _vp, f32]
+            lib.opattr_cache_append.argtypes = [_vp, _vp, _vp, i32, _vp, i64, _vp, _vp]
+            lib.opattr_cache_fork.argtypes = [_vp, _vp, _vp, _vp, i32]
+            lib.opattr_cache_trim.argtypes = [_vp, _vp, _vp, _vp, i32]
+            lib.opattr_cache_compact.argtypes = [_vp, _vp, _vp]
             lib.opattr_check.argtypes = [_vp]
             for f in ("opattr_create", "opattr_enclose", "opattr_match", "opattr_aggregate", "opattr_attribute",
                       "opattr_rollup", "opattr_set_timing", "opattr_timing_report", "opattr_attention",
@@ -323,32 +325,31 @@ def opattr_match_noalloc(kernels: Kernels, ncu: Ncu, mismatch: str, idx_ptr: int
                                           _vp(idx_ptr), _vp(kind_ptr or 0), ctypes.byref(summary), _vp(stream or 0))
 
 
-def opattr_attention(handle, args: Prompt) -> int:
-    return (_lib or library()).opattr_attention(handle, ctypes.byref(args))
+def opattr_attention(handle, args) -> int:
+    """args: a Prompt (by reference) or its bytes."""
+    return (_lib or library()).opattr_attention(handle, args)
 
 
-def opattr_cache_attention(handle, cache: Cache, seqs_ptr: int | None, n: int, q_heads: int, q: Rows, out: Rows,
-                           lse_ptr: int | None, scale: float) -> int:
-    return (_lib or library()).opattr_cache_attention(handle, ctypes.byref(cache), seqs_ptr, n, q_heads,
-                                                      ctypes.byref(q), ctypes.byref(out), lse_ptr, scale)
+def opattr_cache_attention(handle, cache, seqs_ptr: int | None, n: int, q_heads: int, q, out, lse_ptr: int | None,
+                           scale: float) -> int:
+    """cache: a Cache by reference; q, out: Rows by reference, or their bytes."""
+    return (_lib or library()).opattr_cache_attention(handle, cache, seqs_ptr, n, q_heads, q, out, lse_ptr, scale)
 
 
-def opattr_cache_append(handle, cache: Cache, seqs_ptr: int, n: int, offsets_ptr: int, tokens: int, k: Rows,
-                        v: Rows) -> int:
-    return (_lib or library()).opattr_cache_append(handle, ctypes.byref(cache), seqs_ptr, n, offsets_ptr, tokens,
-                                                   ctypes.byref(k), ctypes.byref(v))
+def opattr_cache_append(handle, cache, seqs_ptr: int, n: int, offsets_ptr: int, tokens: int, k, v) -> int:
+    return (_lib or library()).opattr_cache_append(handle, cache, seqs_ptr, n, offsets_ptr, tokens, k, v)
 
 
-def opattr_cache_fork(handle, cache: Cache, src_ptr: int, dst_ptr: int, n: int) -> int:
-    return (_lib or library()).opattr_cache_fork(handle, ctypes.byref(cache), src_ptr, dst_ptr, n)
+def opattr_cache_fork(handle, cache, src_ptr: int, dst_ptr: int, n: int) -> int:
+    return (_lib or library()).opattr_cache_fork(handle, cache, src_ptr, dst_ptr, n)
 
 
-def opattr_cache_trim(handle, cache: Cache, seqs_ptr: int, lengths_ptr: int | None, n: int) -> int:
-    return (_lib or library()).opattr_cache_trim(handle, ctypes.byref(cache), seqs_ptr, lengths_ptr, n)
+def opattr_cache_trim(handle, cache, seqs_ptr: int, lengths_ptr: int | None, n: int) -> int:
+    return (_lib or library()).opattr_cache_trim(handle, cache, seqs_ptr, lengths_ptr, n)
 
 
-def opattr_cache_compact(handle, cache: Cache, live_ptr: int | None) -> int:
-    return (_lib or library()).opattr_cache_compact(handle, ctypes.byref(cache), live_ptr)
+def opattr_cache_compact(handle, cache, live_ptr: int | None) -> int:
+    return (_lib or library()).opattr_cache_compact(handle, cache, live_ptr)
 
 
 def opattr_check(handle) -> int:
@@ -452,24 +453,34 @@ def _dtype(t, name) -> int:
     raise TypeError(f"{name}: expected torch.bfloat16 or torch.float16, got {t.dtype}")
 
 
-def _rows(t, heads: int | None, dim: int, like, name, device) -> Rows:
-    """[tokens, heads, dim] of `like`'s type as opattr_rows; a view whose heads
-    are contiguous and whose rows lie 16 bytes apart or a multiple of that."""
-    if t.dim() != 3 or (heads is not None and t.shape[1] != heads) or t.shape[2] != dim:
+# Rows and Prompt as bytes: one call in the place of an object and its fields
+_ROWS = struct.Struct("@Pqq")
+_PROMPT = struct.Struct("@6ifi2q" + "Pqq" * 4 + "3P")
+
+
+def _rows(t, heads: int | None, dim: int, like, name, device):
+    """[tokens, heads, dim] of `like`'s type as the fields of opattr_rows; a view
+    whose rows are contiguous and start 16 bytes apart or a multiple of that."""
+    shape = t.shape
+    if len(shape) != 3 or (heads is not None and shape[1] != heads) or shape[2] != dim:
         raise ValueError(f"{name}: expected [tokens, {heads if heads is not None else 'heads'}, {dim}], "
-                         f"got {list(t.shape)}")
+                         f"got {list(shape)}")
     if t.dtype is not like:
         raise TypeError(f"{name}: expected {like}, got {t.dtype}")
     if t.get_device() != device:
         raise ValueError(f"{name}: must live on cuda:{device}")
-    if t.numel() == 0:
-        return Rows(None, 0, 0)
     st, sh, se = t.stride()
-    n, h, _ = t.shape
+    n, h, _ = shape
     p = t.data_ptr()
-    if (se != 1 and dim > 1) or p % 16 or (n > 1 and (st % 8 or st < 8)) or (h > 1 and (sh % 8 or sh < 0)):
+    if n == 0 or h == 0:
+        return None, 0, 0
+    if n == 1:
+        st = h * dim
+    if h == 1:
+        sh = dim
+    if se != 1 or p & 15 or st & 7 or sh & 7 or st < 8 or sh < 0:
         raise ValueError(f"{name}: a row's elements must be contiguous and rows 16-byte aligned")
-    return Rows(p, st if n > 1 else h * dim, sh if h > 1 else dim)
+    return p, st, sh
 
 
 def _distinct(t, name):
@@ -508,6 +519,7 @@ class KVCache:
                             _ptr(self.v_pages, self.k_pages.dtype, "v_pages", dv),
                             _ptr(self.table, torch.int32, "table", dv), _ptr(self.length, torch.int32, "length", dv),
                             _ptr(self.refs, torch.int32, "refs", dv), _ptr(self.low, torch.int32, "low", dv))
+        self.device, self.by_ref = dv, ctypes.byref(self.struct)
 
 
 class Context:
@@ -521,6 +533,7 @@ class Context:
         if stream is None:
             stream = torch.cuda.current_stream(device)
         self.stream = stream
+        self._raw_stream = stream.cuda_stream
         st, self.handle = opattr_create(device, stream.cuda_stream, mismatch, dedup, spin_limit)
         if st != OK:
             raise OpattrError(st, "opattr_create")
@@ -734,9 +747,9 @@ class Context:
     # -- attention, and the paged cache under it.  These calls do not wait; on
     # another stream than the context's they are ordered as calls on that stream
     def _enter(self):
-        cur = _torch().cuda.current_stream(self.device)
-        if cur == self.stream:
+        if _torch()._C._cuda_getCurrentRawStream(self.device) == self._raw_stream:
             return None
+        cur = _torch().cuda.current_stream(self.device)
         self.stream.wait_stream(cur)
         return cur
 
@@ -762,42 +775,52 @@ class Context:
         default 1 / sqrt(dim).  Returns (status, out, lse or None)."""
         torch = _torch()
         dv = self.device
-        if q.dim() != 3 or k.dim() != 3:
+        qs, ks = q.shape, k.shape
+        if len(qs) != 3 or len(ks) != 3:
             raise ValueError("q, k: expected [tokens, heads, dim]")
-        dim, dt = q.shape[2], q.dtype
+        tokens, heads, dim = qs
+        k_tokens, kv_heads, _ = ks
+        dt = q.dtype
         dtype = _dtype(q, "q")
         if dim < 8 or dim > 128 or dim % 8:
             raise ValueError(f"dim: expected a multiple of 8 from 8 to 128, got {dim}")
-        if k.shape[1] < 1 or q.shape[1] < 1 or q.shape[1] % k.shape[1]:
-            raise ValueError(f"heads: {q.shape[1]} of q are no multiple of {k.shape[1]} of k")
-        if v.shape[0] != k.shape[0]:
-            raise ValueError(f"v: expected {k.shape[0]} rows, got {v.shape[0]}")
-        rq, rk, rv = (_rows(t, h, dim, dt, nm, dv) for t, h, nm in ((q, None, "q"), (k, None, "k"), (v, k.shape[1], "v")))
+        if kv_heads < 1 or heads < 1 or heads % kv_heads:
+            raise ValueError(f"heads: {heads} of q are no multiple of {kv_heads} of k")
+        if v.shape[0] != k_tokens:
+            raise ValueError(f"v: expected {k_tokens} rows, got {v.shape[0]}")
+        rows = *_rows(q, heads, dim, dt, "q", dv), *_rows(k, kv_heads, dim, dt, "k", dv), *_rows(v, kv_heads, dim, dt, "v", dv)
         if q_offsets is None:
             if k_offsets is not None:
                 raise ValueError("k_offsets: needs q_offsets")
-            q_offsets = torch.tensor([0, q.shape[0]], dtype=torch.int32, device=self._dev)
-            if k.shape[0] != q.shape[0]:
-                k_offsets = torch.tensor([0, k.shape[0]], dtype=torch.int32, device=self._dev)
+            q_offsets = torch.tensor([0, tokens], dtype=torch.int32, device=self._dev)
+            if k_tokens != tokens:
+                k_offsets = torch.tensor([0, k_tokens], dtype=torch.int32, device=self._dev)
         if q_offsets.dim() != 1 or q_offsets.shape[0] < 1:
             raise ValueError("q_offsets: expected [n_seqs + 1]")
         n_seqs = q_offsets.shape[0] - 1
-        if k_offsets is None and k.shape[0] != q.shape[0]:
+        if k_offsets is None and k_tokens != tokens:
             raise ValueError("k_offsets: k has other rows than q")
-        if out is None:
-            out = torch.empty(q.shape, dtype=dt, device=self._dev)
-        elif out.shape != q.shape:
-            raise ValueError(f"out: expected {list(q.shape)}, got {list(out.shape)}")
-        _distinct(out, "out")
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=self._dev) if need_lse else None
+        out, ro = self._out(out, q, heads, dim, dt)
+        lse = p_lse = None
+        if need_lse:
+            lse = torch.empty((tokens, heads), dtype=torch.float32, device=self._dev)
+            p_lse = lse.data_ptr()
         p_qo = self._i32(q_offsets, None, "q_offsets")
-        args = Prompt(dtype, n_seqs, q.shape[1], k.shape[1], dim, int(bool(causal)),
-                      dim ** -0.5 if scale is None else scale, 0, q.shape[0], k.shape[0], rq, rk, rv,
-                      _rows(out, q.shape[1], dim, dt, "out", dv), p_qo,
-                      p_qo if k_offsets is None else self._i32(k_offsets, n_seqs + 1, "k_offsets"),
-                      _ptr(lse, torch.float32, "lse", dv))
+        args = _PROMPT.pack(dtype, n_seqs, heads, kv_heads, dim, 1 if causal else 0, dim ** -0.5 if scale is None else scale,
+                            0, tokens, k_tokens, *(x or 0 for x in rows), *(x or 0 for x in ro), p_qo or 0,
+                            (p_qo if k_offsets is None else self._i32(k_offsets, n_seqs + 1, "k_offsets")) or 0, p_lse or 0)
         cur = self._enter()
         return self._leave(cur, opattr_attention(self.handle, args), "opattr_attention"), out, lse
+
+    def _out(self, out, q, heads, dim, dt):
+        """An output of q's shape, and its rows."""
+        if out is None:
+            out = _torch().empty(q.shape, dtype=dt, device=self._dev)
+        else:
+            if out.shape != q.shape:
+                raise ValueError(f"out: expected {list(q.shape)}, got {list(out.shape)}")
+            _distinct(out, "out")
+        return out, _rows(out, heads, dim, dt, "out", self.device)
 
     def cache(self, n_pages: int, page_size: int, kv_heads: int, head_dim: int, n_seqs: int, pages_per_seq: int,
               dtype=None) -> KVCache:
@@ -810,7 +833,7 @@ class Context:
         return KVCache(*pool, new((n_seqs, pages_per_seq), -1), new((n_seqs,), 0), new((n_pages,), 0), new((1,), 0))
 
     def _cache(self, cache: KVCache) -> Cache:
-        if cache.k_pages.get_device() != self.device:
+        if cache.device != self.device:
             raise ValueError(f"cache: must live on cuda:{self.device}")
         return cache.struct
 
@@ -819,68 +842,69 @@ class Context:
         (opattr_cache_attention): q [n, heads, dim], row i of sequence seqs[i]
         (int32 [n], or None: sequence i).  Returns (status, out, lse or None)."""
         torch = _torch()
-        dv = self.device
         kv = self._cache(cache)
         dim, dt = kv.head_dim, cache.k_pages.dtype
-        rq = _rows(q, None, dim, dt, "q", dv)
-        n, heads = q.shape[:2]
+        rq = _rows(q, None, dim, dt, "q", self.device)
+        n, heads, _ = q.shape
         if heads < 1 or heads % kv.kv_heads:
             raise ValueError(f"heads: {heads} of q are no multiple of {kv.kv_heads} of the cache")
         if seqs is None and n > kv.n_seqs:
             raise ValueError(f"q: {n} rows for {kv.n_seqs} sequences")
-        if out is None:
-            out = torch.empty(q.shape, dtype=dt, device=self._dev)
-        elif out.shape != q.shape:
-            raise ValueError(f"out: expected {list(q.shape)}, got {list(out.shape)}")
-        _distinct(out, "out")
-        lse = torch.empty((n, heads), dtype=torch.float32, device=self._dev) if need_lse else None
-        ro = _rows(out, heads, dim, dt, "out", dv)
-        p_seqs, p_lse = self._i32(seqs, n, "seqs"), _ptr(lse, torch.float32, "lse", dv)
+        out, ro = self._out(out, q, heads, dim, dt)
+        lse = p_lse = None
+        if need_lse:
+            lse = torch.empty((n, heads), dtype=torch.float32, device=self._dev)
+            p_lse = lse.data_ptr()
+        p_seqs = self._i32(seqs, n, "seqs")
         cur = self._enter()
-        st = opattr_cache_attention(self.handle, kv, p_seqs, n, heads, rq, ro, p_lse,
-                                    dim ** -0.5 if scale is None else scale)
+        st = opattr_cache_attention(self.handle, cache.by_ref, p_seqs, n, heads, _ROWS.pack(rq[0] or 0, rq[1], rq[2]),
+                                    _ROWS.pack(ro[0] or 0, ro[1], ro[2]), p_lse, dim ** -0.5 if scale is None else scale)
         return self._leave(cur, st, "opattr_cache_attention"), out, lse
 
     def cache_append(self, cache: KVCache, seqs, offsets, k, v) -> int:
         """Rows offsets[i] .. offsets[i + 1] of k and v ([tokens, kv_heads, dim])
         to the end of sequence seqs[i], each sequence once (opattr_cache_append)."""
-        dv = self.device
         kv = self._cache(cache)
         if v.shape != k.shape:
             raise ValueError(f"v: expected {list(k.shape)}, got {list(v.shape)}")
-        rk, rv = (_rows(t, kv.kv_heads, kv.head_dim, cache.k_pages.dtype, nm, dv) for t, nm in ((k, "k"), (v, "v")))
+        dt = cache.k_pages.dtype
+        rk = _rows(k, kv.kv_heads, kv.head_dim, dt, "k", self.device)
+        rv = _rows(v, kv.kv_heads, kv.head_dim, dt, "v", self.device)
         p_seqs = self._i32(seqs, None, "seqs")
-        p_off = self._i32(offsets, seqs.shape[0] + 1, "offsets")
+        n = seqs.shape[0]
+        p_off = self._i32(offsets, n + 1, "offsets")
         cur = self._enter()
-        st = opattr_cache_append(self.handle, kv, p_seqs, seqs.shape[0], p_off, k.shape[0], rk, rv)
+        st = opattr_cache_append(self.handle, cache.by_ref, p_seqs, n, p_off, k.shape[0],
+                                 _ROWS.pack(rk[0] or 0, rk[1], rk[2]), _ROWS.pack(rv[0] or 0, rv[1], rv[2]))
         return self._leave(cur, st, "opattr_cache_append")
 
     def cache_fork(self, cache: KVCache, src, dst) -> int:
         """The empty sequences dst[i] share the pages of src[i] (opattr_cache_fork)."""
-        kv = self._cache(cache)
+        self._cache(cache)
         p_dst = self._i32(dst, None, "dst")
-        p_src = self._i32(src, dst.shape[0], "src")
+        n = dst.shape[0]
+        p_src = self._i32(src, n, "src")
         cur = self._enter()
-        return self._leave(cur, opattr_cache_fork(self.handle, kv, p_src, p_dst, dst.shape[0]), "opattr_cache_fork")
+        return self._leave(cur, opattr_cache_fork(self.handle, cache.by_ref, p_src, p_dst, n), "opattr_cache_fork")
 
     def cache_trim(self, cache: KVCache, seqs, lengths=None) -> int:
         """Sequence seqs[i] keeps its first lengths[i] tokens (none: it is
         freed), and the pages past them are let go (opattr_cache_trim)."""
-        kv = self._cache(cache)
+        self._cache(cache)
         p_seqs = self._i32(seqs, None, "seqs")
-        p_len = self._i32(lengths, seqs.shape[0], "lengths")
+        n = seqs.shape[0]
+        p_len = self._i32(lengths, n, "lengths")
         cur = self._enter()
-        st = opattr_cache_trim(self.handle, kv, p_seqs, p_len, seqs.shape[0])
-        return self._leave(cur, st, "opattr_cache_trim")
+        return self._leave(cur, opattr_cache_trim(self.handle, cache.by_ref, p_seqs, p_len, n), "opattr_cache_trim")
 
     def cache_compact(self, cache: KVCache):
         """The pages in use become the cache's first ones (opattr_cache_compact).
         Returns (status, int32 [1] tensor of how many those are)."""
         torch = _torch()
-        kv = self._cache(cache)
+        self._cache(cache)
         live = torch.empty(1, dtype=torch.int32, device=self._dev)
         cur = self._enter()
-        st = opattr_cache_compact(self.handle, kv, live.data_ptr())
+        st = opattr_cache_compact(self.handle, cache.by_ref, live.data_ptr())
         return self._leave(cur, st, "opattr_cache_compact"), live
 
     def check(self) -> None:

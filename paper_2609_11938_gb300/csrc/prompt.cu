@@ -31,7 +31,7 @@ constexpr int CUTS = 4;                  // value tiles cut by a mask that can b
 constexpr int ITEMS = 3;                 // work items looked up ahead
 
 // Shapes by the padded head width DP (64 or 128; the copies fill what a head
-// lacks with zeros).
+// lacks with zeros).  The products take DV of its columns (64; 96 or 128).
 template <int DP>
 struct Shape {
     static constexpr int HALF = 128 * 128;                 // bytes of 128 rows of 64 elements
@@ -124,7 +124,7 @@ __device__ __forceinline__ long long draw(unsigned *next, long long total) {
     return (long long)gridDim.x + __shfl_sync(0xffffffffu, k, 0);
 }
 
-template <typename T, int DP>
+template <typename T, int DP, int DV>
 __global__ void __launch_bounds__(THREADS, 1)
 k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorMap mq,
          const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, unsigned *err) {
@@ -371,7 +371,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
             // descriptors stay in uniform registers (from one lane's branch each operand
             // would be moved there anew: 75 cycles a product instead of the 64 that it takes)
             const uint32_t DS = mma_desc(BF, ROWS, KEYS, false) | (a.scale < 0.f ? MMA_NEGATE : 0u);
-            constexpr uint32_t DO = mma_desc(BF, ROWS, DP, true);
+            constexpr uint32_t DO = mma_desc(BF, ROWS, DV, true);
             const bool lead = elect();
             // descriptors count in 16 bytes: a tile's is its first one's and an offset
             const uint64_t qdesc = tile_desc(sq, 16), kdesc = tile_desc(skv, 16), vdesc = tile_desc(skv, S::HALF);
@@ -382,7 +382,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                 const uint64_t qd = qdesc + s * (S::TILE >> 4), kd = kdesc + st * (S::TILE >> 4);
                 if (lead) {
 #pragma unroll
-                    for (int k = 0; k < DP / 16; ++k) {
+                    for (int k = 0; k < DV / 16; ++k) {
                         const int off = (k / 4) * (S::HALF >> 4) + (k % 4) * 2;
                         mma_ss(tm + s * 128, qd + off, kd + off, DS, k > 0);
                     }
@@ -485,17 +485,24 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                 const Work w(it, p.pair, a.causal);
                 if (w.n == 0) continue;
                 const int g = it.head0 / (a.q_heads / a.kv_heads), subs = w.tiles[1] > 0 ? 2 : 1;
-                if (!(ok = warp_wait(smem_addr(&ctl.q_free), q_turn.ph ^ 1, stop))) break;
-                q_turn.step();
-                if (lead) {
-                    bar_expect(bq, subs * S::TILE);
-                    for (int s = 0; s < subs; ++s)
-                        for (int d = 0; d < DP / 64; ++d)
-                            tile_load(sq + s * S::TILE + d * S::HALF, &mq, 64 * d, (p.pair ? it.head0 + s : it.head0) * p.q_mul,
-                                      it.q0 + (s ? w.base[1] : w.base[0]), bq);
-                }
-                q_out = 1;
+                // the queries as soon as those before them are done with; until then the first keys
+                // and values go ahead, as far as the item before this one leaves stages free
+                bool q_due = true;
                 for (int load = 0; load < 2 * w.n; ++load) {
+                    if (q_due && (load == S::STAGES - 2 || load == 2 * w.n - 1 ||
+                                  __all_sync(0xffffffffu, bar_is_done(smem_addr(&ctl.q_free), q_turn.ph ^ 1)))) {
+                        if (!(ok = warp_wait(smem_addr(&ctl.q_free), q_turn.ph ^ 1, stop))) break;
+                        q_turn.step();
+                        q_due = false;
+                        if (lead) {
+                            bar_expect(bq, subs * S::TILE);
+                            for (int s = 0; s < subs; ++s)
+                                for (int d = 0; d < DP / 64; ++d)
+                                    tile_load(sq + s * S::TILE + d * S::HALF, &mq, 64 * d,
+                                              (p.pair ? it.head0 + s : it.head0) * p.q_mul, it.q0 + (s ? w.base[1] : w.base[0]), bq);
+                        }
+                        q_out = 1;
+                    }
                     if (!(ok = warp_wait(bar_free + 8 * ring.at, ring.ph ^ 1, stop))) break;
                     // K0, V0, K1, V1, ..; values that are looked over have a barrier of their own: the
                     // stage's may have gone round several times before the tail's warp sees it
@@ -566,35 +573,33 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
             // passed over.  A block's first item is its number, others are drawn.
             const int per = p.pair ? ROWS : 2 * ROWS;
             const long long total = (long long)p.heads_x * p.tiles;
-            if (blockIdx.x == 0) {
-                bool bad = lane_id() == 0 && (a.q_offsets[0] != 0 || a.q_offsets[a.n_seqs] != a.q_tokens ||
-                                              a.k_offsets[0] != 0 || a.k_offsets[a.n_seqs] != a.k_tokens);
-                for (int b = lane_id(); b < a.n_seqs; b += 32)
-                    bad = bad || a.q_offsets[b + 1] < a.q_offsets[b] || a.k_offsets[b + 1] < a.k_offsets[b];
-                if (bad) atomicOr(err, SERVE_INVALID);
-            }
             // after a wait that gave up nothing more is begun
-            bool none = uniform(*(volatile unsigned *)err & SERVE_TIMEOUT);
+            const unsigned gave_up = *(volatile unsigned *)err & SERVE_TIMEOUT;
+            bool none = false;
             long long i = blockIdx.x;
             for (bool more = true; more;) {
                 Item it{};
                 for (; i < total && !none;) {
                     const int x = p.tiles - 1 - (int)(i / p.heads_x), hx = (int)(i % p.heads_x);
-                    // the last sequence whose places begin at x or before it, 32 at a time
+                    // the last sequence whose places begin at x or before it, 32 at a time;
+                    // the last 32 with all that there is to know about them
                     int lo = 0, n = a.n_seqs;
-                    while (n > 1) {
+                    while (n > 32) {
                         const int step = (n + 31) / 32, b = lo + step * (int)lane_id();
                         const bool le = step * (int)lane_id() < n && a.q_offsets[b] / per + b <= x;
                         const int k = max(0, 31 - __clz(__ballot_sync(0xffffffffu, le)));
                         lo += k * step;
                         n = min(step, n - k * step);
                     }
-                    int v = 0;
-                    if (lane_id() < 4) v = (lane_id() < 2 ? a.q_offsets : a.k_offsets)[lo + (lane_id() & 1)];
-                    const int q0 = uniform(v), q1 = __shfl_sync(0xffffffffu, v, 1);
-                    const int k0 = __shfl_sync(0xffffffffu, v, 2), k1 = __shfl_sync(0xffffffffu, v, 3);
-                    const int t0 = (x - q0 / per - lo) * per;
-                    if (q0 >= 0 && q1 >= q0 && q1 <= a.q_tokens && k0 >= 0 && k1 >= k0 && k1 <= a.k_tokens && t0 >= 0 && t0 < q1 - q0) {
+                    const int b = lo + min((int)lane_id(), n - 1);
+                    const int vq0 = a.q_offsets[b], vq1 = a.q_offsets[b + 1], vk0 = a.k_offsets[b], vk1 = a.k_offsets[b + 1];
+                    const int k = max(0, 31 - __clz(__ballot_sync(0xffffffffu, (int)lane_id() < n && vq0 / per + b <= x)));
+                    const int q0 = __shfl_sync(0xffffffffu, vq0, k), q1 = __shfl_sync(0xffffffffu, vq1, k);
+                    const int k0 = __shfl_sync(0xffffffffu, vk0, k), k1 = __shfl_sync(0xffffffffu, vk1, k);
+                    const int t0 = (x - q0 / per - (lo + k)) * per;
+                    none = uniform(gave_up) != 0;
+                    if (!none && q0 >= 0 && q1 >= q0 && q1 <= a.q_tokens && k0 >= 0 && k1 >= k0 && k1 <= a.k_tokens && t0 >= 0 &&
+                        t0 < q1 - q0) {
                         it = Item{q0, q1 - q0, k0, k1 - k0, t0, p.pair ? 2 * hx : hx, 1};
                         break;
                     }
@@ -608,6 +613,13 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                 }
                 slot.step();
                 if (more) i = draw(p.next, total);
+            }
+            if (blockIdx.x == 0) {
+                bool bad = lane_id() == 0 && (a.q_offsets[0] != 0 || a.q_offsets[a.n_seqs] != a.q_tokens ||
+                                              a.k_offsets[0] != 0 || a.k_offsets[a.n_seqs] != a.k_tokens);
+                for (int b = lane_id(); b < a.n_seqs; b += 32)
+                    bad = bad || a.q_offsets[b + 1] < a.q_offsets[b] || a.k_offsets[b + 1] < a.k_offsets[b];
+                if (bad) atomicOr(err, SERVE_INVALID);
             }
         }
     }
@@ -648,15 +660,21 @@ static bool row_map(CUtensorMap *m, int dtype, const opattr_rows &r, int64_t tok
                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename T, int DP>
+template <typename T, int DP, int DV>
 static opattr_status run_prompt(Ctx &c, Serve &s, const PromptArgs &p, const CUtensorMap *m) {
     using S = Shape<DP>;
-    const cudaError_t e = cudaFuncSetAttribute(k_prompt<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
+    const cudaError_t e = cudaFuncSetAttribute(k_prompt<T, DP, DV>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
     if (e != cudaSuccess) return cuda_status(c, e);
     const int64_t items = (int64_t)p.heads_x * p.tiles;
-    launch(c, "prompt", k_prompt<T, DP>, dim3((unsigned)std::min<int64_t>(items, sm_count(c))), dim3(THREADS), S::SMEM, p, m[0],
+    launch(c, "prompt", k_prompt<T, DP, DV>, dim3((unsigned)std::min<int64_t>(items, sm_count(c))), dim3(THREADS), S::SMEM, p, m[0],
            m[1], m[2], s.err);
     return cuda_status(c, c.last_error);
+}
+
+template <typename T>
+static opattr_status prompt_of(Ctx &c, Serve &s, const PromptArgs &p, const CUtensorMap *m) {
+    if (p.a.head_dim <= 64) return run_prompt<T, 64, 64>(c, s, p, m);
+    return p.a.head_dim <= 96 ? run_prompt<T, 128, 96>(c, s, p, m) : run_prompt<T, 128, 128>(c, s, p, m);
 }
 
 opattr_status do_attention(Ctx &c, Serve &s, const opattr_prompt *a) {
@@ -693,9 +711,7 @@ opattr_status do_attention(Ctx &c, Serve &s, const opattr_prompt *a) {
         !row_map(&m[1], a->dtype, a->k_tokens ? a->k : a->q, a->k_tokens ? a->k_tokens : 1, a->kv_heads, a->head_dim) ||
         !row_map(&m[2], a->dtype, a->k_tokens ? a->v : a->q, a->k_tokens ? a->k_tokens : 1, a->kv_heads, a->head_dim))
         return OPATTR_E_INVALID_ARG;
-    if (a->dtype == OPATTR_BF16)
-        return a->head_dim <= 64 ? run_prompt<__nv_bfloat16, 64>(c, s, p, m) : run_prompt<__nv_bfloat16, 128>(c, s, p, m);
-    return a->head_dim <= 64 ? run_prompt<__half, 64>(c, s, p, m) : run_prompt<__half, 128>(c, s, p, m);
+    return a->dtype == OPATTR_BF16 ? prompt_of<__nv_bfloat16>(c, s, p, m) : prompt_of<__half>(c, s, p, m);
 }
 
 }  // namespace opattr

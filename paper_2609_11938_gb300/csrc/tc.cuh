@@ -19,28 +19,39 @@ __device__ __forceinline__ void bar_arrive(uint32_t bar) {
 __device__ __forceinline__ void bar_expect(uint32_t bar, unsigned bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ bool bar_done(uint32_t bar, unsigned phase) {
+// Whether the barrier's phase of this parity is over; a thread that finds that it
+// is not sleeps until it is, for `ns` at most.
+__device__ __forceinline__ bool bar_done(uint32_t bar, unsigned phase, unsigned ns) {
     unsigned ok;
-    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+    asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n selp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(ok) : "r"(bar), "r"(phase), "r"(ns) : "memory");
+    return ok;
+}
+__device__ __forceinline__ bool bar_is_done(uint32_t bar, unsigned phase) {
+    unsigned ok;
+    asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
                  : "=r"(ok) : "r"(bar), "r"(phase) : "memory");
     return ok;
 }
-// Waits until the barrier's phase of this parity is over; gives up after WAIT_NS
-// of waiting, or once another warp of the block gave up.
+// Waits until the phase is over; gives up after WAIT_NS of waiting, or once another
+// warp of the block gave up.  The sleeps are long: warps that poll take issue slots
+// from those that compute.
 constexpr unsigned long long WAIT_NS = 4000000000ull;
+constexpr unsigned SLEEP_NS = 1000000;
 __device__ __forceinline__ unsigned long long clock_ns() {
     unsigned long long t;
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
     return t;
 }
-__device__ __forceinline__ bool bar_wait(uint32_t bar, unsigned phase, volatile int *stop) {
-    for (int i = 0; i < 32; ++i)
-        if (bar_done(bar, phase)) return true;
+__device__ __forceinline__ bool bar_wait_on(uint32_t bar, unsigned phase, volatile int *stop) {
     const unsigned long long t0 = clock_ns();
     while (!*stop && clock_ns() - t0 < WAIT_NS)
-        if (bar_done(bar, phase)) return true;
+        if (bar_done(bar, phase, SLEEP_NS)) return true;
     *stop = 1;
     return false;
+}
+__device__ __forceinline__ bool bar_wait(uint32_t bar, unsigned phase, volatile int *stop) {
+    return bar_done(bar, phase, SLEEP_NS) || bar_wait_on(bar, phase, stop);
 }
 // The same for a whole warp that goes on together.
 __device__ __forceinline__ bool warp_wait(uint32_t bar, unsigned phase, volatile int *stop) {

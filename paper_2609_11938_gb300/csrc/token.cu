@@ -4,9 +4,11 @@
 // The cache is read once and there is little to compute on it, so what counts is
 // that every SM has enough loads under way until the last one is done.  All
 // (sequence, key head) pairs' tokens are laid end to end and cut into equal runs,
-// one per block, whatever the lengths; a pair that is cut is joined by the block
-// that finishes its part last, over the parts in order (so the bits do not depend
-// on who that is).
+// one per block, whatever the lengths (a pair counts one step more than it has,
+// for what beginning and ending it costs: without that, a block whose run is of
+// many short sequences ended 25 us after the others at 64 sequences of 1 .. 16,000
+// tokens); a pair that is cut is joined by the block that finishes its part last,
+// over the parts in order (so the bits do not depend on who that is).
 //
 // A warp takes 16 keys at a time straight from memory into the registers that
 // the products want them in, without shared memory: the products' inner
@@ -28,7 +30,10 @@ namespace opattr {
 bool cache_ok(const opattr_cache *k);
 
 constexpr int TOKEN_WARPS = 4, TOKEN_THREADS = 32 * TOKEN_WARPS;
-constexpr int MIN_STEPS = 2;                  // steps of a run at least: a cut costs a join
+// A cut costs a join, about 3 us where nothing else is to be done meanwhile; a step
+// of a block by itself 0.45 us.  So pairs of few steps are not cut, and others are
+// cut down to two steps as far as there are blocks.
+constexpr int UNCUT_STEPS = 8, MIN_STEPS = 2;
 
 struct TokenArgs {
     opattr_cache kv;
@@ -90,22 +95,24 @@ __global__ void __launch_bounds__(TOKEN_THREADS, NT == 1 ? 3 : 2) k_token(const 
         return len > kv.pages_per_seq << p.shift ? -1 : len;
     };
     auto steps_of = [](int len) { return len <= 0 ? 1 : (len + STEP - 1) / STEP; };
+    auto cost_of = [](int steps) { return steps + 1; };        // place 0 of a pair stands for no keys
     const int per = (p.n + TOKEN_THREADS - 1) / TOKEN_THREADS, b0 = min(p.n, (int)threadIdx.x * per), b1 = min(p.n, b0 + per);
     long long mine = 0;
     for (int b = b0; b < b1; ++b) {
         const int len = len_of(seq_of(b));
         if (len < 0 && blockIdx.x == 0) atomicOr(err, SERVE_INVALID);
-        mine += (long long)steps_of(len) * units;
+        mine += (long long)cost_of(steps_of(len)) * units;
     }
     long long total;
     long long at = block_exclusive_scan(mine, warp_buf, &total);
-    const long long W = min((long long)gridDim.x, (total + MIN_STEPS - 1) / MIN_STEPS);
+    const long long pairs = (long long)p.n * units;
+    const long long W = min((long long)gridDim.x, total <= (UNCUT_STEPS + 1) * pairs ? pairs : max(1ll, total / MIN_STEPS));
     if (blockIdx.x >= W) return;
     const long long s0 = blockIdx.x * total / W, s1 = (blockIdx.x + 1) * total / W;
     if (s0 >= at && s0 < at + mine) {
         int b = b0;
         for (;; ++b) {
-            const long long of = (long long)steps_of(len_of(seq_of(b))) * units;
+            const long long of = (long long)cost_of(steps_of(len_of(seq_of(b)))) * units;
             if (s0 < at + of) break;
             at += of;
         }
@@ -119,15 +126,17 @@ __global__ void __launch_bounds__(TOKEN_THREADS, NT == 1 ? 3 : 2) k_token(const 
     long long base = first_at;                    // where sequence b's steps begin
     const float c = p.scale * LOG2E;
     for (long long s = s0; s < s1;) {
-        const int seq = seq_of(b), len = max(0, len_of(seq)), steps = steps_of(len);
-        if (s >= base + (long long)steps * units) {
-            base += (long long)steps * units;
+        const int seq = seq_of(b), len = max(0, len_of(seq)), steps = steps_of(len), cost = cost_of(steps);
+        if (s >= base + (long long)cost * units) {
+            base += (long long)cost * units;
             ++b;
             continue;
         }
-        const int unit = (int)((s - base) / steps), g = unit / p.blocks_of_heads, hb = unit % p.blocks_of_heads;
-        const long long unit_at = base + (long long)unit * steps;
-        const int from = (int)(s - unit_at), to = (int)min((long long)steps, s1 - unit_at);
+        const int unit = (int)((s - base) / cost), g = unit / p.blocks_of_heads, hb = unit % p.blocks_of_heads;
+        const long long unit_at = base + (long long)unit * cost + 1;   // of its first step
+        const int from = (int)max(0ll, s - unit_at), to = (int)min((long long)steps, s1 - unit_at);
+        s = unit_at + to;
+        if (from >= to) continue;
         const int heads = min(NQ, p.group - hb * NQ), head0 = g * p.group + hb * NQ;
         const int32_t *table = kv.table + (long long)seq * kv.pages_per_seq;
 
@@ -357,7 +366,6 @@ __global__ void __launch_bounds__(TOKEN_THREADS, NT == 1 ? 3 : 2) k_token(const 
             }
         }
         __syncthreads();
-        s = unit_at + to;
     }
 }
 
