@@ -28,7 +28,8 @@ constexpr int MMA_WARP = 8, LOAD_WARP = 9, TAIL_WARP = 10;   // and the last one
 // registers: 384 x 168 at launch = 256 x 208 + 128 x 88
 constexpr int REGS_SOFTMAX = 208, REGS_OTHERS = 88;
 constexpr int CUTS = 4;                  // value tiles cut by a mask that can be under way: half the ring's stages
-constexpr int ITEMS = 3;                 // work items looked up ahead
+constexpr int SHORT = 4;                 // key tiles of an item that is over before the next one is looked up
+constexpr int ITEMS = 2;                 // slots of work items: the one being computed, and the one whose tiles are fetched
 
 // Shapes by the padded head width DP (64 or 128; the copies fill what a head
 // lacks with zeros).  The products take DV of its columns (64; 96 or 128).
@@ -49,21 +50,34 @@ struct PromptArgs {
     int q_mul, k_mul, v_mul;             // 0 where all heads read the same rows
     int wide;                            // 1: rows of the output are 32-byte aligned and DP wide
     unsigned *next;                      // items given out past each block's first; zero between launches
+    // where keys are cut, else NULL
+    const struct Piece *plan;
+    const int *n_pieces;
+    float *parts;                        // [piece][head][sub-tile] partial results, four columns of every row side by side; then the rows' maxima and sums
+    uint32_t *tickets;                   // [place][head][sub-tile] arrivals
 };
 
-// A work item: two sub-tiles of queries of one sequence.
+// A work item: two sub-tiles of queries of one sequence, and keys of it.
 struct Item {
-    int q0, lq, k0, lk;                  // the sequence's rows
-    int t0, head0;                       // first query within it, (first) head
+    int q0, lq, k0, lk;                  // the sequence's queries; the keys taken here
+    int t0, head0, hx;                   // first query within it, (first) head, and its place among heads_x
+    int ahead;                           // query i sees the keys up to i + ahead
+    int place, first, piece, pieces;     // its query tile; the tile's first piece, which of them this is, and how many there are
     int some;                            // 0: there are no more
 };
 
+// Pieces of keys of a query tile, as the plan lists them.
+struct Piece {
+    int q0, lq, k0, lk, t0, ahead, place, first, piece, pieces;
+};
+
 struct Ctrl {
-    uint64_t item_full[ITEMS], item_free[ITEMS], q_full, q_free, kv_full[8], kv_free[8];
+    uint64_t item_full[ITEMS], item_free[ITEMS], item_want, q_full, q_free, kv_full[8], kv_free[8];
     uint64_t s_full[2], p_half[2], p_full[2], o_full[2], o_free[2], v_full[CUTS], v_ready[CUTS], drain;
     uint32_t tmem;
     int stop;
     int poison[CUTS];
+    int last[2];
     Item item[ITEMS];
 };
 
@@ -79,9 +93,9 @@ struct Place {
 // What an item's sub-tiles have to do.
 struct Work {
     int base[2], tiles[2], clean[2];     // first query; key tiles; the first of them that a mask cuts
-    int n, cut, ahead;                   // key tiles of either; the first that is looked over; query i sees keys up to i + ahead
+    int n, cut;                          // key tiles of either; the first that is looked over
     __device__ __forceinline__ Work(const Item &it, int pair, int causal) {
-        ahead = it.lk - it.lq;
+        const int ahead = it.ahead;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             base[s] = pair ? it.t0 : it.t0 + s * ROWS;
@@ -105,6 +119,9 @@ __device__ __forceinline__ uint32_t tm_ld1(uint32_t at) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(at));
     return r;
 }
+
+// The four warps of sub-tile s.
+__device__ __forceinline__ void group_sync(int s) { asm volatile("bar.sync %0, 128;" ::"r"(s + 1) : "memory"); }
 
 // 32 bytes of a thread in one store: whole sectors, where rows lie far apart.
 __device__ __forceinline__ void store32(void *p, const uint32_t *r) {
@@ -145,6 +162,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
     const uint32_t bar_kv = smem_addr(&ctl.kv_full[0]), bar_free = smem_addr(&ctl.kv_free[0]);
     if (threadIdx.x == 0) {
         for (int i = 0; i < ITEMS; ++i) bar_init(smem_addr(&ctl.item_full[i]), 1), bar_init(smem_addr(&ctl.item_free[i]), 11);
+        bar_init(smem_addr(&ctl.item_want), 1);
         bar_init(smem_addr(&ctl.q_full), 1), bar_init(smem_addr(&ctl.q_free), 1);
         for (int i = 0; i < S::STAGES; ++i) bar_init(bar_kv + 8 * i, 1), bar_init(bar_free + 8 * i, 1);
         for (int i = 0; i < 2; ++i) {
@@ -198,7 +216,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
             const Work w(it, p.pair, a.causal);
             const int n_tiles = s ? w.tiles[1] : w.tiles[0], clean = s ? w.clean[1] : w.clean[0];
             const int head = p.pair ? it.head0 + s : it.head0, row = (s ? w.base[1] : w.base[0]) + r;
-            const int seen = a.causal ? min(it.lk, row + 1 + w.ahead) : it.lk;
+            const int seen = a.causal ? min(it.lk, row + 1 + it.ahead) : it.lk;
             float m = -INFINITY, l = 0.f;
             for (int j = 0; j < w.n; ++j) {
                 if (j < n_tiles) {
@@ -331,20 +349,81 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                 tm_after();
             }
             const bool live = row < it.lq, wide = p.wide;
+            float ref = m == -INFINITY ? m : m * c;      // the row's sum counts in 2^(ref - OFFSET)
+            bool mine = true, joined = false;
+            const float *parts = nullptr;
+            auto o_read = [&] {                          // the next item's products may go there
+                tm_before();
+                __syncwarp();
+                if (lane_id() == 0) bar_arrive(smem_addr(&ctl.o_free[s]));
+            };
+            constexpr int PART = ROWS * (DP + 2);
+            const long long stride = (long long)p.heads_x * 2 * PART;
+            if (it.pieces > 1) {
+                // a part of the keys: the result so far goes to memory, and whoever brings the
+                // last part of the tile puts them together, in order
+                parts = p.parts + ((long long)it.first * p.heads_x + it.hx) * 2 * PART + s * PART;
+                float *part = const_cast<float *>(parts) + it.piece * stride;
+#pragma unroll 1
+                for (int d = 0; d < DP; d += 32) {
+                    uint32_t o[32] = {};
+                    if (n_tiles > 0) {
+                        tm_ld32(to + d, o);
+                        tm_wait_ld();
+                        if (d + 32 == DP) o_read();
+                    }
+                    if (live) {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4)
+                            __stcg(reinterpret_cast<uint4 *>(part + (d + e) * ROWS + 4 * r), make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]));
+                    }
+                }
+                if (live) *reinterpret_cast<float2 *>(part + ROWS * DP + 2 * r) = make_float2(ref, l);
+                __threadfence();
+                group_sync(s);
+                if (r == 0) {
+                    uint32_t *t = p.tickets + ((long long)it.place * p.heads_x + it.hx) * 2 + s;
+                    const bool all = atomicAdd(t, 1u) == (unsigned)it.pieces - 1;
+                    if (all) atomicExch(t, 0u);
+                    ctl.last[s] = all;
+                }
+                group_sync(s);
+                mine = joined = *(volatile int *)&ctl.last[s];
+                if (joined) {
+                    __threadfence();
+                    ref = -INFINITY;
+                    for (int k = 0; live && k < it.pieces; ++k) ref = fmaxf(ref, __ldcg(parts + k * stride + ROWS * DP + 2 * r));
+                    l = 0.f;
+                    for (int k = 0; live && k < it.pieces; ++k) {
+                        const float2 y = __ldcg(reinterpret_cast<const float2 *>(parts + k * stride + ROWS * DP + 2 * r));
+                        l = __fmaf_rn(y.y, y.x == ref ? 1.f : exp2_fast(y.x - ref), l);
+                    }
+                }
+            }
             const float share = l == 0.f ? 0.f : 1.f / l;
             T *out = (T *)a.out.data + (int64_t)(it.q0 + row) * a.out.token_stride + head * a.out.head_stride;
 #pragma unroll 1
-            for (int d = 0; d < DP; d += 32) {
+            for (int d = 0; d < DP && mine; d += 32) {
                 uint32_t o[32] = {};
-                if (n_tiles > 0) {
+                if (joined && live) {
+#pragma unroll 4
+                    for (int k = 0; k < it.pieces; ++k) {
+                        const float *part = parts + k * stride;
+                        const float y = __ldcg(part + ROWS * DP + 2 * r), f = y == ref ? 1.f : exp2_fast(y - ref);
+#pragma unroll
+                        for (int e = 0; e < 32; e += 4) {
+                            const float4 z = __ldcg(reinterpret_cast<const float4 *>(part + (d + e) * ROWS + 4 * r));
+                            o[e] = __float_as_uint(__fmaf_rn(z.x, f, __uint_as_float(o[e])));
+                            o[e + 1] = __float_as_uint(__fmaf_rn(z.y, f, __uint_as_float(o[e + 1])));
+                            o[e + 2] = __float_as_uint(__fmaf_rn(z.z, f, __uint_as_float(o[e + 2])));
+                            o[e + 3] = __float_as_uint(__fmaf_rn(z.w, f, __uint_as_float(o[e + 3])));
+                        }
+                    }
+                }
+                if (n_tiles > 0 && !joined) {
                     tm_ld32(to + d, o);
                     tm_wait_ld();
-                    if (d + 32 == DP) {
-                        // the next item's products may go there
-                        tm_before();
-                        __syncwarp();
-                        if (lane_id() == 0) bar_arrive(smem_addr(&ctl.o_free[s]));
-                    }
+                    if (d + 32 == DP) o_read();
                 }
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
@@ -360,9 +439,9 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                     }
                 }
             }
-            if (live && a.lse)
+            if (live && mine && a.lse)
                 a.lse[(int64_t)(it.q0 + row) * a.q_heads + head] =
-                    l == 0.f ? -INFINITY : (__fmaf_rn(m == -INFINITY ? 0.f : m, c, -OFFSET) + log2f(l)) * LN2;
+                    l == 0.f ? -INFINITY : ((ref == -INFINITY ? 0.f : ref) - OFFSET + log2f(l)) * LN2;
         }
     } else {
         regs_fewer<REGS_OTHERS>();
@@ -483,7 +562,11 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
             Item it;
             while (ok && item_next(it)) {
                 const Work w(it, p.pair, a.causal);
-                if (w.n == 0) continue;
+                // A block draws its next item when this one's tiles are all on their way: drawn three
+                // ahead, the last items went to the blocks that asked first (8,192 causal tokens, 8
+                // heads of 128: 133 us, so 103).  Short ones it draws at once, as the lookup takes as
+                // long as they do (64 x 512 tokens, 8 heads of 64: 57 us, after their tiles 61).
+                if (lead && w.n <= SHORT) bar_arrive(smem_addr(&ctl.item_want));
                 const int g = it.head0 / (a.q_heads / a.kv_heads), subs = w.tiles[1] > 0 ? 2 : 1;
                 // the queries as soon as those before them are done with; until then the first keys
                 // and values go ahead, as far as the item before this one leaves stages free
@@ -520,6 +603,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                     if (cut) over.step();
                     ring.step();
                 }
+                if (lead && w.n > SHORT) bar_arrive(smem_addr(&ctl.item_want));
             }
             // copies that nobody waits for any more
             int never = 0;
@@ -572,14 +656,22 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
             // on, enough for its tiles whatever comes before it; those it does not need are
             // passed over.  A block's first item is its number, others are drawn.
             const int per = p.pair ? ROWS : 2 * ROWS;
-            const long long total = (long long)p.heads_x * p.tiles;
+            const long long total = (long long)p.heads_x * (p.plan ? *p.n_pieces : p.tiles);
             // after a wait that gave up nothing more is begun
             const unsigned gave_up = *(volatile unsigned *)err & SERVE_TIMEOUT;
             bool none = false;
+            Place<1> wanted;
             long long i = blockIdx.x;
             for (bool more = true; more;) {
                 Item it{};
                 for (; i < total && !none;) {
+                    if (p.plan) {
+                        none = uniform(gave_up) != 0;
+                        const Piece y = p.plan[i / p.heads_x];
+                        const int hx = (int)(i % p.heads_x);
+                        if (!none) it = Item{y.q0, y.lq, y.k0, y.lk, y.t0, p.pair ? 2 * hx : hx, hx, y.ahead, y.place, y.first, y.piece, y.pieces, 1};
+                        break;
+                    }
                     const int x = p.tiles - 1 - (int)(i / p.heads_x), hx = (int)(i % p.heads_x);
                     // the last sequence whose places begin at x or before it, 32 at a time;
                     // the last 32 with all that there is to know about them
@@ -600,7 +692,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                     none = uniform(gave_up) != 0;
                     if (!none && q0 >= 0 && q1 >= q0 && q1 <= a.q_tokens && k0 >= 0 && k1 >= k0 && k1 <= a.k_tokens && t0 >= 0 &&
                         t0 < q1 - q0) {
-                        it = Item{q0, q1 - q0, k0, k1 - k0, t0, p.pair ? 2 * hx : hx, 1};
+                        it = Item{q0, q1 - q0, k0, k1 - k0, t0, p.pair ? 2 * hx : hx, hx, (k1 - k0) - (q1 - q0), 0, 0, 0, 1, 1};
                         break;
                     }
                     i = draw(p.next, total);
@@ -612,7 +704,11 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                     bar_arrive(smem_addr(&ctl.item_full[slot.at]));
                 }
                 slot.step();
-                if (more) i = draw(p.next, total);
+                if (more) {
+                    if (!warp_wait(smem_addr(&ctl.item_want), wanted.ph, stop)) break;
+                    wanted.step();
+                    i = draw(p.next, total);
+                }
             }
             if (blockIdx.x == 0) {
                 bool bad = lane_id() == 0 && (a.q_offsets[0] != 0 || a.q_offsets[a.n_seqs] != a.q_tokens ||
@@ -628,6 +724,58 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
     if (threadIdx.x == 0 && *stop) atomicOr(err, SERVE_TIMEOUT);
     __syncwarp();
     if (warp == MMA_WARP) tm_free(ctl.tmem, 512);
+}
+
+// ---------------------------------------------------------------- the plan where keys are cut
+// Few query tiles with many keys would leave SMs idle: then each tile's keys are cut
+// into pieces of about half of what an SM has to do (PIECE_TILES at least, and no
+// more than PIECES_PER_TILE to a tile: a piece costs a way to memory and back of 128 x
+// DP sums; a quarter was slower throughout).  One block; there are few tiles.
+constexpr int PIECE_TILES = 8, PIECES_PER_SM = 2, PIECES_PER_TILE = 32;
+
+__global__ void __launch_bounds__(1024) k_prompt_plan(PromptArgs p, int sms, Piece *plan, int *n_pieces) {
+    __shared__ int warp_buf[33];
+    __shared__ long long wide_buf[33];
+    pdl_wait();
+    const opattr_prompt &a = p.a;
+    const int per = p.pair ? ROWS : 2 * ROWS;
+    Item it{};
+    auto look = [&](int x) {                             // key tiles of place x; 0: it has no queries
+        const int b = [&] {
+            int lo = 0, hi = a.n_seqs;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (a.q_offsets[mid] / per + mid <= x) lo = mid;
+                else hi = mid;
+            }
+            return lo;
+        }();
+        const int q0 = a.q_offsets[b], q1 = a.q_offsets[b + 1], k0 = a.k_offsets[b], k1 = a.k_offsets[b + 1];
+        const int t0 = (x - q0 / per - b) * per;
+        if (q0 < 0 || q1 < q0 || q1 > a.q_tokens || k0 < 0 || k1 < k0 || k1 > a.k_tokens || t0 < 0 || t0 >= q1 - q0) return 0;
+        it = Item{q0, q1 - q0, k0, k1 - k0, t0, 0, 0, (k1 - k0) - (q1 - q0), x, 0, 0, 1, 1};
+        return max(1, Work(it, p.pair, a.causal).n);
+    };
+    long long all = 0;
+    for (int x = threadIdx.x; x < p.tiles; x += 1024) all += look(x);
+    all = block_sum(all, wide_buf);
+    const int most = (int)max((long long)PIECE_TILES, (all * p.heads_x + PIECES_PER_SM * sms - 1) / (PIECES_PER_SM * sms));
+    int at = 0;
+    for (int x0 = 0; x0 < p.tiles; x0 += 1024) {
+        // (as the items without a plan: from the last place to the first)
+        const int x = p.tiles - 1 - (x0 + (int)threadIdx.x);
+        const int n = x >= 0 ? look(x) : 0, pieces = min(PIECES_PER_TILE, (n + most - 1) / most);
+        int sum;
+        const int first = at + block_exclusive_scan(pieces, warp_buf, &sum);
+        for (int k = 0; k < pieces; ++k) {
+            const int j0 = (int)((long long)n * k / pieces), j1 = (int)((long long)n * (k + 1) / pieces);
+            // the last piece has what is left of the keys, and with them the masks
+            const int k1 = k + 1 == pieces ? it.lk : min(it.lk, j1 * KEYS);
+            plan[first + k] = Piece{it.q0, it.lq, it.k0 + j0 * KEYS, k1 - j0 * KEYS, it.t0, it.ahead - j0 * KEYS, x, first, k, pieces};
+        }
+        at += sum;
+    }
+    if (threadIdx.x == 0) *n_pieces = at;
 }
 
 // ---------------------------------------------------------------- host
@@ -661,18 +809,38 @@ static bool row_map(CUtensorMap *m, int dtype, const opattr_rows &r, int64_t tok
 }
 
 template <typename T, int DP, int DV>
-static opattr_status run_prompt(Ctx &c, Serve &s, const PromptArgs &p, const CUtensorMap *m) {
+static opattr_status run_prompt(Ctx &c, Serve &s, PromptArgs &p, const CUtensorMap *m) {
     using S = Shape<DP>;
+    const int64_t items = (int64_t)p.heads_x * p.tiles;
+    const int sms = sm_count(c);
+    // Keys are cut where there are no more items than SMs and 2,048 keys to a sequence
+    // (uncut, then cut, us: 1 query over 100,000 keys, 8 heads of 128: 945, 119; 512 over
+    // 8,192, 32 heads: 102, 89; 4,096 over as many, 8 heads: 56, 55; with more items than
+    // that, 8,192 causal, 8 heads: 103, 128)
+    if (items <= sms && p.a.k_tokens / p.a.n_seqs >= 2048) {
+        const int64_t most = p.tiles + ((int64_t)PIECES_PER_SM * sms + p.heads_x - 1) / p.heads_x + 1;
+        const int64_t parts = most * p.heads_x * 2 * ROWS * (DP + 2);
+        opattr_status st = serve_ready(c, s, 2 * items);
+        if (st) return st;
+        if ((st = ensure_arena(c, Need().add<int>(1).add<Piece>(most).add<float>(parts).bytes))) return st;
+        Arena ar(c);
+        int *n = ar.take<int>(1);
+        Piece *plan = ar.take<Piece>(most);
+        p.n_pieces = n;
+        p.plan = plan;
+        p.parts = ar.take<float>(parts);
+        p.tickets = s.tickets;
+        launch(c, "prompt_plan", k_prompt_plan, dim3(1), dim3(1024), 0, p, sms, plan, n);
+    }
     const cudaError_t e = cudaFuncSetAttribute(k_prompt<T, DP, DV>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
     if (e != cudaSuccess) return cuda_status(c, e);
-    const int64_t items = (int64_t)p.heads_x * p.tiles;
-    launch(c, "prompt", k_prompt<T, DP, DV>, dim3((unsigned)std::min<int64_t>(items, sm_count(c))), dim3(THREADS), S::SMEM, p, m[0],
+    launch(c, "prompt", k_prompt<T, DP, DV>, dim3((unsigned)(p.plan ? sms : std::min<int64_t>(items, sms))), dim3(THREADS), S::SMEM, p, m[0],
            m[1], m[2], s.err);
     return cuda_status(c, c.last_error);
 }
 
 template <typename T>
-static opattr_status prompt_of(Ctx &c, Serve &s, const PromptArgs &p, const CUtensorMap *m) {
+static opattr_status prompt_of(Ctx &c, Serve &s, PromptArgs &p, const CUtensorMap *m) {
     if (p.a.head_dim <= 64) return run_prompt<T, 64, 64>(c, s, p, m);
     return p.a.head_dim <= 96 ? run_prompt<T, 128, 96>(c, s, p, m) : run_prompt<T, 128, 128>(c, s, p, m);
 }

@@ -93,6 +93,18 @@ def test_prompt_long(ctx):
     check_prompt(ctx, q, k, v, [n], None, True)
 
 
+@pytest.mark.parametrize("dtype,dim,heads,kv", [(BF, 128, 4, 2), (HF, 64, 3, 1), (BF, 96, 5, 5)])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("lq,lk", [([1], [20_000]), ([300, 1, 40], [9001, 30, 5000]), ([0, 257], [3, 4999]), ([200], [4100])])
+def test_prompt_few_queries_many_keys(ctx, dtype, dim, heads, kv, causal, lq, lk):
+    """Keys cut into pieces, their parts joined; twice, for the counts left behind."""
+    g = gen(sum(lk) + dim)
+    q = randn(g, (sum(lq), heads, dim), dtype)
+    k, v = (randn(g, (sum(lk), kv, dim), dtype) for _ in range(2))
+    first, _ = check_prompt(ctx, q, k, v, lq, lk, causal)
+    assert torch.equal(check_prompt(ctx, q, k, v, lq, lk, causal)[0], first)
+
+
 def test_prompt_rising_scores(ctx):
     """Scores that rise along the keys: the running maximum moves at every tile,
     by more and by less than what the accumulator is rescaled for."""
