@@ -473,7 +473,7 @@ def _rows(t, heads: int | None, dim: int, like, name, device):
     n, h, _ = shape
     p = t.data_ptr()
     if n == 0 or h == 0:
-        return None, 0, 0
+        return 0, 0, 0
     if n == 1:
         st = h * dim
     if h == 1:
@@ -762,10 +762,11 @@ class Context:
 
     def _i32(self, t, n: int | None, name):
         if t is None:
-            return None
-        if t.dim() != 1 or (n is not None and t.shape[0] != n):
-            raise ValueError(f"{name}: expected [{n if n is not None else 'n'}], got {list(t.shape)}")
-        return _ptr(t, _torch().int32, name, self.device)
+            return 0
+        shape = t.shape
+        if len(shape) != 1 or (n is not None and shape[0] != n):
+            raise ValueError(f"{name}: expected [{n if n is not None else 'n'}], got {list(shape)}")
+        return _ptr(t, _torch().int32, name, self.device) or 0
 
     def attention(self, q, k, v, q_offsets=None, k_offsets=None, causal: bool = True, scale: float | None = None,
                   out=None, need_lse: bool = False):
@@ -788,38 +789,40 @@ class Context:
             raise ValueError(f"heads: {heads} of q are no multiple of {kv_heads} of k")
         if v.shape[0] != k_tokens:
             raise ValueError(f"v: expected {k_tokens} rows, got {v.shape[0]}")
-        rows = *_rows(q, heads, dim, dt, "q", dv), *_rows(k, kv_heads, dim, dt, "k", dv), *_rows(v, kv_heads, dim, dt, "v", dv)
+        rq, rk, rv = _rows(q, heads, dim, dt, "q", dv), _rows(k, kv_heads, dim, dt, "k", dv), _rows(v, kv_heads, dim, dt, "v", dv)
         if q_offsets is None:
             if k_offsets is not None:
                 raise ValueError("k_offsets: needs q_offsets")
             q_offsets = torch.tensor([0, tokens], dtype=torch.int32, device=self._dev)
             if k_tokens != tokens:
                 k_offsets = torch.tensor([0, k_tokens], dtype=torch.int32, device=self._dev)
-        if q_offsets.dim() != 1 or q_offsets.shape[0] < 1:
+        n_seqs = q_offsets.numel() - 1
+        if n_seqs < 0:
             raise ValueError("q_offsets: expected [n_seqs + 1]")
-        n_seqs = q_offsets.shape[0] - 1
         if k_offsets is None and k_tokens != tokens:
             raise ValueError("k_offsets: k has other rows than q")
         out, ro = self._out(out, q, heads, dim, dt)
-        lse = p_lse = None
+        lse, p_lse = None, 0
         if need_lse:
             lse = torch.empty((tokens, heads), dtype=torch.float32, device=self._dev)
             p_lse = lse.data_ptr()
-        p_qo = self._i32(q_offsets, None, "q_offsets")
+        p_qo = p_ko = self._i32(q_offsets, n_seqs + 1, "q_offsets")
+        if k_offsets is not None and k_offsets is not q_offsets:
+            p_ko = self._i32(k_offsets, n_seqs + 1, "k_offsets")
         args = _PROMPT.pack(dtype, n_seqs, heads, kv_heads, dim, 1 if causal else 0, dim ** -0.5 if scale is None else scale,
-                            0, tokens, k_tokens, *(x or 0 for x in rows), *(x or 0 for x in ro), p_qo or 0,
-                            (p_qo if k_offsets is None else self._i32(k_offsets, n_seqs + 1, "k_offsets")) or 0, p_lse or 0)
+                            0, tokens, k_tokens, *rq, *rk, *rv, *ro, p_qo, p_ko, p_lse)
         cur = self._enter()
         return self._leave(cur, opattr_attention(self.handle, args), "opattr_attention"), out, lse
 
     def _out(self, out, q, heads, dim, dt):
         """An output of q's shape, and its rows."""
         if out is None:
-            out = _torch().empty(q.shape, dtype=dt, device=self._dev)
-        else:
-            if out.shape != q.shape:
-                raise ValueError(f"out: expected {list(q.shape)}, got {list(out.shape)}")
-            _distinct(out, "out")
+            torch = _torch()
+            out = torch.empty_like(q) if q.is_contiguous() else torch.empty(q.shape, dtype=dt, device=self._dev)
+            return out, (out.data_ptr(), heads * dim, dim)
+        if out.shape != q.shape:
+            raise ValueError(f"out: expected {list(q.shape)}, got {list(out.shape)}")
+        _distinct(out, "out")
         return out, _rows(out, heads, dim, dt, "out", self.device)
 
     def cache(self, n_pages: int, page_size: int, kv_heads: int, head_dim: int, n_seqs: int, pages_per_seq: int,
@@ -851,14 +854,13 @@ class Context:
         if seqs is None and n > kv.n_seqs:
             raise ValueError(f"q: {n} rows for {kv.n_seqs} sequences")
         out, ro = self._out(out, q, heads, dim, dt)
-        lse = p_lse = None
+        lse, p_lse = None, 0
         if need_lse:
             lse = torch.empty((n, heads), dtype=torch.float32, device=self._dev)
             p_lse = lse.data_ptr()
         p_seqs = self._i32(seqs, n, "seqs")
         cur = self._enter()
-        st = opattr_cache_attention(self.handle, cache.by_ref, p_seqs, n, heads, _ROWS.pack(rq[0] or 0, rq[1], rq[2]),
-                                    _ROWS.pack(ro[0] or 0, ro[1], ro[2]), p_lse, dim ** -0.5 if scale is None else scale)
+        st = opattr_cache_attention(self.handle, cache.by_ref, p_seqs, n, heads, _ROWS.pack(*rq), _ROWS.pack(*ro), p_lse, dim ** -0.5 if scale is None else scale)
         return self._leave(cur, st, "opattr_cache_attention"), out, lse
 
     def cache_append(self, cache: KVCache, seqs, offsets, k, v) -> int:
@@ -875,7 +877,7 @@ class Context:
         p_off = self._i32(offsets, n + 1, "offsets")
         cur = self._enter()
         st = opattr_cache_append(self.handle, cache.by_ref, p_seqs, n, p_off, k.shape[0],
-                                 _ROWS.pack(rk[0] or 0, rk[1], rk[2]), _ROWS.pack(rv[0] or 0, rv[1], rv[2]))
+                                 _ROWS.pack(*rk), _ROWS.pack(*rv))
         return self._leave(cur, st, "opattr_cache_append")
 
     def cache_fork(self, cache: KVCache, src, dst) -> int:

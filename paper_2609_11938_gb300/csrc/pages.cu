@@ -14,7 +14,7 @@
 
 namespace opattr {
 
-constexpr int PLAN_THREADS = 1024;
+constexpr int PLAN_THREADS = 1024;         // at most: a plan of few sequences has fewer
 constexpr int COPY_THREADS = 256;
 
 bool cache_ok(const opattr_cache *k) {
@@ -107,8 +107,8 @@ struct AppendPlan {
 };
 
 // One block: a call has few sequences, and their new pages are found where the
-// lowest free ones are (`low`: none below it is free), a thousand times four
-// reference counts at a time.
+// lowest free ones are (`low`: none below it is free), four reference counts to a
+// thread at a time.
 __global__ void __launch_bounds__(PLAN_THREADS)
 k_append_plan(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offsets, int tokens, AppendPlan p,
               unsigned *err) {
@@ -139,7 +139,7 @@ k_append_plan(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offset
     }
     if (any_bad(bad, SERVE_INVALID, err)) return;
     int total = 0;
-    for (int i0 = 0; i0 < n; i0 += PLAN_THREADS) {
+    for (int i0 = 0; i0 < n; i0 += blockDim.x) {
         const int i = i0 + threadIdx.x;
         int need = 0;
         if (i < n) {
@@ -166,7 +166,7 @@ k_append_plan(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offset
     // the lowest `total` free pages
     int found = 0;
     const int64_t low = max(0, *kv.low);
-    for (int64_t at = low; found < total && at < kv.n_pages; at += 4 * PLAN_THREADS) {
+    for (int64_t at = low; found < total && at < kv.n_pages; at += 4 * blockDim.x) {
         const int64_t i = at + 4 * threadIdx.x;
         int r[4], mine = 0;
 #pragma unroll
@@ -239,6 +239,7 @@ k_append_rows(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offset
     }
 }
 
+static unsigned plan_threads(int64_t n) { return n <= 256 ? 256 : PLAN_THREADS; }
 static opattr_status seqs_ok(const opattr_cache *kv, const int32_t *seqs, int32_t n) {
     return cache_ok(kv) && n >= 0 && n <= kv->n_seqs && (n == 0 || seqs) ? OPATTR_OK : OPATTR_E_INVALID_ARG;
 }
@@ -267,7 +268,7 @@ opattr_status do_cache_append(Ctx &c, Serve &s, const opattr_cache *kv, const in
     p.mark = a.take<int32_t>(kv->n_seqs);
     p.fresh = a.take<int32_t>(most);
     p.room = (int32_t)most;
-    launch(c, "append_plan", k_append_plan, dim3(1), dim3(PLAN_THREADS), 0, *kv, seqs, n, offsets, (int)tokens, p, s.err);
+    launch(c, "append_plan", k_append_plan, dim3(1), dim3(plan_threads(n)), 0, *kv, seqs, n, offsets, (int)tokens, p, s.err);
     const int64_t pieces = tokens * kv->kv_heads * (kv->head_dim / 8);
     const unsigned rows = grid_for(pieces, COPY_THREADS, 8u * sm_count(c)), shared = std::min<unsigned>(n, sm_count(c));
     launch(c, "append_rows", k_append_rows, dim3(rows + shared), dim3(COPY_THREADS), 0, *kv, seqs, n, offsets, (int)tokens,
@@ -275,9 +276,25 @@ opattr_status do_cache_append(Ctx &c, Serve &s, const opattr_cache *kv, const in
     return cuda_status(c, c.last_error);
 }
 
-// ---------------------------------------------------------------- fork
+// ---------------------------------------------------------------- fork and trim
+// The plan's block makes the change itself where the sequences' tables have few
+// entries, a warp to a sequence; a second launch costs 2.5 us.
+constexpr int64_t SMALL_ENTRIES = 16384;
+
+// Of sequence d: the pages of s, by the threads first, first + step, ..
+__device__ __forceinline__ void fork_pages(const opattr_cache &kv, int s, int d, int first, int step) {
+    const int held = pages_for(kv.length[s], kv.page_size);
+    for (int j = first; j < held; j += step) {
+        const int page = kv.table[(int64_t)s * kv.pages_per_seq + j];
+        kv.table[(int64_t)d * kv.pages_per_seq + j] = page;
+        if (page >= 0 && page < kv.n_pages) atomicAdd(&kv.refs[page], 1);
+    }
+    // (a source is no destination here: its length stands)
+    if (first == 0 && kv.length[s] > 0) kv.length[d] = kv.length[s];
+}
 __global__ void __launch_bounds__(PLAN_THREADS)
-k_fork_plan(opattr_cache kv, const int32_t *src, const int32_t *dst, int n, int32_t *mark, int32_t *go, unsigned *err) {
+k_fork_plan(opattr_cache kv, const int32_t *src, const int32_t *dst, int n, int32_t *mark, int32_t *go, int small,
+            unsigned *err) {
     pdl_wait();
     if (threadIdx.x == 0) *go = 0;
     if (seqs_bad(dst, n, kv.n_seqs, mark, err)) return;
@@ -291,20 +308,15 @@ k_fork_plan(opattr_cache kv, const int32_t *src, const int32_t *dst, int n, int3
         bad = m >= 0 && m < n && dst[m] == s;
     }
     if (any_bad(bad, SERVE_INVALID, err)) return;
-    if (threadIdx.x == 0) *go = 1;
+    if (small)
+        for (int i = threadIdx.x >> 5; i < n; i += blockDim.x >> 5) fork_pages(kv, src[i], dst[i], lane_id(), 32);
+    else if (threadIdx.x == 0) *go = 1;
 }
 __global__ void __launch_bounds__(COPY_THREADS)
 k_fork(opattr_cache kv, const int32_t *src, const int32_t *dst, const int32_t *go) {
     pdl_wait();
     if (*go == 0) return;
-    const int s = src[blockIdx.x], d = dst[blockIdx.x], len = kv.length[s], held = pages_for(len, kv.page_size);
-    for (int j = blockIdx.y * COPY_THREADS + threadIdx.x; j < held; j += gridDim.y * COPY_THREADS) {
-        const int page = kv.table[(int64_t)s * kv.pages_per_seq + j];
-        kv.table[(int64_t)d * kv.pages_per_seq + j] = page;
-        if (page >= 0 && page < kv.n_pages) atomicAdd(&kv.refs[page], 1);
-    }
-    // (a source is no destination here: its length stands)
-    if (blockIdx.y == 0 && threadIdx.x == 0 && len > 0) kv.length[d] = len;
+    fork_pages(kv, src[blockIdx.x], dst[blockIdx.x], blockIdx.y * COPY_THREADS + threadIdx.x, gridDim.y * COPY_THREADS);
 }
 
 opattr_status do_cache_fork(Ctx &c, Serve &s, const opattr_cache *kv, const int32_t *src, const int32_t *dst, int32_t n) {
@@ -315,16 +327,33 @@ opattr_status do_cache_fork(Ctx &c, Serve &s, const opattr_cache *kv, const int3
     if ((st = ensure_arena(c, Need().add<int32_t>(1).add<int32_t>(kv->n_seqs).bytes))) return st;
     Arena a(c);
     int32_t *go = a.take<int32_t>(1), *mark = a.take<int32_t>(kv->n_seqs);
-    launch(c, "fork_plan", k_fork_plan, dim3(1), dim3(PLAN_THREADS), 0, *kv, src, dst, n, mark, go, s.err);
-    launch(c, "fork", k_fork, dim3(n, grid_for(kv->pages_per_seq, 4 * COPY_THREADS, 64)), dim3(COPY_THREADS), 0, *kv, src,
-           dst, (const int32_t *)go);
+    const int64_t entries = (int64_t)n * kv->pages_per_seq;
+    const bool small = entries <= SMALL_ENTRIES;
+    launch(c, "fork_plan", k_fork_plan, dim3(1), dim3(plan_threads(small ? entries / 8 : n)), 0, *kv, src, dst, n, mark, go,
+           (int)small, s.err);
+    if (!small)
+        launch(c, "fork", k_fork, dim3(n, grid_for(kv->pages_per_seq, 4 * COPY_THREADS, 64)), dim3(COPY_THREADS), 0, *kv, src,
+               dst, (const int32_t *)go);
     return cuda_status(c, c.last_error);
 }
 
-// ---------------------------------------------------------------- trim
+// The pages of sequence s from its length `to` on, of `old`.
+__device__ __forceinline__ void trim_pages(const opattr_cache &kv, int s, int old, int to, int first, int step) {
+    const int held = pages_for(old, kv.page_size), keep = pages_for(to, kv.page_size);
+    int low = INT32_MAX;
+    for (int j = keep + first; j < held; j += step) {
+        int32_t *e = &kv.table[(int64_t)s * kv.pages_per_seq + j];
+        const int page = *e;
+        *e = -1;
+        if (page >= 0 && page < kv.n_pages && atomicSub(&kv.refs[page], 1) == 1) low = min(low, page);
+    }
+    __syncwarp();
+    low = __reduce_min_sync(0xffffffffu, low);
+    if (lane_id() == 0 && low < INT32_MAX) atomicMin(kv.low, low);
+}
 __global__ void __launch_bounds__(PLAN_THREADS)
 k_trim_plan(opattr_cache kv, const int32_t *seqs, const int32_t *lengths, int n, int32_t *mark, int32_t *old,
-            int32_t *go, unsigned *err) {
+            int32_t *go, int small, unsigned *err) {
     pdl_wait();
     if (threadIdx.x == 0) *go = 0;
     if (seqs_bad(seqs, n, kv.n_seqs, mark, err)) return;
@@ -336,23 +365,17 @@ k_trim_plan(opattr_cache kv, const int32_t *seqs, const int32_t *lengths, int n,
     }
     if (any_bad(bad, SERVE_INVALID, err)) return;
     for (int i = threadIdx.x; i < n; i += blockDim.x) kv.length[seqs[i]] = lengths ? lengths[i] : 0;
-    if (threadIdx.x == 0) *go = 1;
+    if (small)
+        for (int i = threadIdx.x >> 5; i < n; i += blockDim.x >> 5)
+            trim_pages(kv, seqs[i], old[i], lengths ? lengths[i] : 0, lane_id(), 32);
+    else if (threadIdx.x == 0) *go = 1;
 }
 __global__ void __launch_bounds__(COPY_THREADS)
 k_trim(opattr_cache kv, const int32_t *seqs, const int32_t *lengths, const int32_t *old, const int32_t *go) {
     pdl_wait();
     if (*go == 0) return;
-    const int i = blockIdx.x, s = seqs[i], held = pages_for(old[i], kv.page_size);
-    const int keep = pages_for(lengths ? lengths[i] : 0, kv.page_size);
-    int low = INT32_MAX;
-    for (int j = keep + blockIdx.y * COPY_THREADS + threadIdx.x; j < held; j += gridDim.y * COPY_THREADS) {
-        int32_t *e = &kv.table[(int64_t)s * kv.pages_per_seq + j];
-        const int page = *e;
-        *e = -1;
-        if (page >= 0 && page < kv.n_pages && atomicSub(&kv.refs[page], 1) == 1) low = min(low, page);
-    }
-    low = __reduce_min_sync(0xffffffffu, low);
-    if (lane_id() == 0 && low < INT32_MAX) atomicMin(kv.low, low);
+    const int i = blockIdx.x;
+    trim_pages(kv, seqs[i], old[i], lengths ? lengths[i] : 0, blockIdx.y * COPY_THREADS + threadIdx.x, gridDim.y * COPY_THREADS);
 }
 
 opattr_status do_cache_trim(Ctx &c, Serve &s, const opattr_cache *kv, const int32_t *seqs, const int32_t *lengths,
@@ -363,9 +386,13 @@ opattr_status do_cache_trim(Ctx &c, Serve &s, const opattr_cache *kv, const int3
     if ((st = ensure_arena(c, Need().add<int32_t>(1).add<int32_t>(n).add<int32_t>(kv->n_seqs).bytes))) return st;
     Arena a(c);
     int32_t *go = a.take<int32_t>(1), *old = a.take<int32_t>(n), *mark = a.take<int32_t>(kv->n_seqs);
-    launch(c, "trim_plan", k_trim_plan, dim3(1), dim3(PLAN_THREADS), 0, *kv, seqs, lengths, n, mark, old, go, s.err);
-    launch(c, "trim", k_trim, dim3(n, grid_for(kv->pages_per_seq, 4 * COPY_THREADS, 64)), dim3(COPY_THREADS), 0, *kv, seqs,
-           lengths, (const int32_t *)old, (const int32_t *)go);
+    const int64_t entries = (int64_t)n * kv->pages_per_seq;
+    const bool small = entries <= SMALL_ENTRIES;
+    launch(c, "trim_plan", k_trim_plan, dim3(1), dim3(plan_threads(small ? entries / 8 : n)), 0, *kv, seqs, lengths, n, mark,
+           old, go, (int)small, s.err);
+    if (!small)
+        launch(c, "trim", k_trim, dim3(n, grid_for(kv->pages_per_seq, 4 * COPY_THREADS, 64)), dim3(COPY_THREADS), 0, *kv, seqs,
+               lengths, (const int32_t *)old, (const int32_t *)go);
     return cuda_status(c, c.last_error);
 }
 
@@ -388,6 +415,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_compact_count(opattr_cache kv,
     if (threadIdx.x == 0) tile_live[blockIdx.x] = live;
 }
 // rank[page] of the pages that move, hole[rank] where they go.
+// A pool of one tile counts it here; others' counts come from k_compact_count.
 __global__ void __launch_bounds__(PLAN_THREADS)
 k_compact_place(opattr_cache kv, const int32_t *tile_live, int tiles, int32_t *rank, int32_t *hole, int32_t *mover,
                 int32_t *counts, int32_t *out_live) {
@@ -395,14 +423,14 @@ k_compact_place(opattr_cache kv, const int32_t *tile_live, int tiles, int32_t *r
     pdl_wait();
     const int tile = blockIdx.x;
     int all = 0, before = 0;
-    for (int t = threadIdx.x; t < tiles; t += blockDim.x) {
+    for (int t = threadIdx.x; tiles > 1 && t < tiles; t += blockDim.x) {
         all += tile_live[t];
         if (t < tile) before += tile_live[t];
     }
-    const int L = block_sum(all, warp_buf);
+    const int L = tiles > 1 ? block_sum(all, warp_buf) : live_in(kv, 0, kv.n_pages, warp_buf);
     before = block_sum(before, warp_buf);
     // live pages below L
-    const int edge = L / TILE_PAGES;
+    const int edge = tiles > 1 ? L / TILE_PAGES : 0;
     int below = 0;
     for (int t = threadIdx.x; t < edge; t += blockDim.x) below += tile_live[t];
     below = block_sum(below, warp_buf) + live_in(kv, (int64_t)edge * TILE_PAGES, L, warp_buf);
@@ -469,7 +497,7 @@ opattr_status do_cache_compact(Ctx &c, Serve &s, const opattr_cache *kv, int32_t
     Arena a(c);
     int32_t *counts = a.take<int32_t>(2), *tile_live = a.take<int32_t>(tiles), *rank = a.take<int32_t>(kv->n_pages);
     int32_t *hole = a.take<int32_t>(kv->n_pages), *mover = a.take<int32_t>(kv->n_pages);
-    launch(c, "compact_count", k_compact_count, dim3(tiles), dim3(PLAN_THREADS), 0, *kv, tile_live);
+    if (tiles > 1) launch(c, "compact_count", k_compact_count, dim3(tiles), dim3(PLAN_THREADS), 0, *kv, tile_live);
     launch(c, "compact_place", k_compact_place, dim3(tiles), dim3(PLAN_THREADS), 0, *kv, (const int32_t *)tile_live, tiles,
            rank, hole, mover, counts, live);
     launch(c, "compact_move", k_compact_move, dim3(8 * sm_count(c)), dim3(COPY_THREADS), 0, *kv, (const int32_t *)rank,

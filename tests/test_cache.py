@@ -203,6 +203,25 @@ def test_many_pages(ctx):
     assert c.refs.tolist() == [1] * len(old) + [0] * (n_pages - len(old))
 
 
+@pytest.mark.parametrize("n_pages", [4096, 4097])
+def test_compact_at_a_tile(ctx, n_pages):
+    """Pools of one tile of pages and of one page more, full but for a gap, and full."""
+    c = ctx.cache(n_pages, 16, 1, 8, 3, 4096)
+    counts = [1600, 160, 16 * n_pages - 1760]
+    k, v = rows([1] * counts[0] + [2] * counts[1] + [3] * counts[2], 1, 8, torch.bfloat16)
+    ctx.cache_append(c, i32([0, 1, 2]), i32([0, 1600, 1760, 16 * n_pages]), k, v)
+    _, live = ctx.cache_compact(c)
+    ctx.check()
+    assert int(live) == n_pages and c.table[1].tolist()[:10] == list(range(100, 110))
+    ctx.cache_trim(c, i32([1]))
+    _, live = ctx.cache_compact(c)
+    ctx.check()
+    last = n_pages - 110
+    assert int(live) == n_pages - 10
+    assert c.table[2].tolist()[:last] == list(range(110, n_pages - 10)) + list(range(100, 110))
+    assert (c.k_pages[100:110] == 3).all() and c.refs.tolist() == [1] * (n_pages - 10) + [0] * 10
+
+
 def test_strided_rows(ctx):
     """Keys and values as parts of one projection."""
     c = ctx.cache(8, 16, 2, 64, 2, 4)
