@@ -132,13 +132,13 @@ __device__ __forceinline__ void store32(void *p, const uint32_t *r) {
 // The next item for a whole warp: numbers past the blocks' own, in order.  Every
 // block draws until it is told that there are none, so `total` are drawn in all, and
 // the last one puts the count back to zero.
-__device__ __forceinline__ long long draw(unsigned *next, long long total) {
+__device__ __forceinline__ unsigned draw(unsigned *next, unsigned total) {
     unsigned k = 0;
     if (lane_id() == 0) {
         k = atomicAdd(next, 1u);
         if (k == total - 1) atomicExch(next, 0u);
     }
-    return (long long)gridDim.x + __shfl_sync(0xffffffffu, k, 0);
+    return gridDim.x + __shfl_sync(0xffffffffu, k, 0);
 }
 
 template <typename T, int DP, int DV>
@@ -297,7 +297,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                         // a value that is not finite times a weight of zero would reach the rows
                         // that do not see it: such a tile's products are made here, key by key
                         if (!(ok = warp_wait(smem_addr(&ctl.v_ready[over.at]), over.ph, stop))) break;
-                        if (*(volatile int *)&ctl.poison[over.at]) {
+                        if (seldom(*(volatile int *)&ctl.poison[over.at])) {
                             const unsigned char *v = smem + 2 * S::TILE + ring.at * S::TILE;
                             const int left = seen - j * KEYS;
 #pragma unroll 1
@@ -359,7 +359,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
             };
             constexpr int PART = ROWS * (DP + 2);
             const long long stride = (long long)p.heads_x * 2 * PART;
-            if (it.pieces > 1) {
+            if (seldom(it.pieces > 1)) {
                 // a part of the keys: the result so far goes to memory, and whoever brings the
                 // last part of the tile puts them together, in order
                 parts = p.parts + ((long long)it.first * p.heads_x + it.hx) * 2 * PART + s * PART;
@@ -651,48 +651,69 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                 }
             }
         } else {
-            // ---- work items, the longest of a causal sequence first: place x of the query
-            // tiles counts from the end.  Sequence b has the places from q_offsets[b] / per + b
-            // on, enough for its tiles whatever comes before it; those it does not need are
-            // passed over.  A block's first item is its number, others are drawn.
-            const int per = p.pair ? ROWS : 2 * ROWS;
-            const long long total = (long long)p.heads_x * (p.plan ? *p.n_pieces : p.tiles);
+            // ---- work items, the longest of a causal sequence first: query tiles count from the
+            // last one.  Up to 32 sequences' tiles are numbered as they are, from what each lane
+            // keeps of one of them.  Of more, sequence b has the places from q_offsets[b] / per + b
+            // on, enough for its tiles whatever comes before it; those it does not need are passed
+            // over.  A block's first item is its number, others are drawn.
+            const int per = p.pair ? 7 : 8;              // queries of an item, as a shift
+            const bool few = !p.plan && a.n_seqs <= 32;
             // after a wait that gave up nothing more is begun
             const unsigned gave_up = *(volatile unsigned *)err & SERVE_TIMEOUT;
-            bool none = false;
+            int vq0 = 0, vq1 = 0, vk0 = 0, vk1 = 0;
+            auto fetch = [&](int b) {
+                vq0 = a.q_offsets[b], vq1 = a.q_offsets[b + 1], vk0 = a.k_offsets[b], vk1 = a.k_offsets[b + 1];
+            };
+            auto good = [&] {
+                return vq0 >= 0 && vq1 >= vq0 && vq1 <= a.q_tokens && vk0 >= 0 && vk1 >= vk0 && vk1 <= a.k_tokens;
+            };
+            int mine = 0, upto = 0, tiles = p.tiles;
+            if (few) {
+                fetch(min((int)lane_id(), a.n_seqs - 1));
+                mine = (int)lane_id() < a.n_seqs && good() ? (vq1 - vq0 + (1 << per) - 1) >> per : 0;
+                upto = warp_inclusive_scan(mine);
+                tiles = min(tiles, __shfl_sync(0xffffffffu, upto, 31));
+            } else if (p.plan) {
+                tiles = *p.n_pieces;
+            }
+            const unsigned heads_x = p.heads_x, total = heads_x * (unsigned)tiles;
+            const bool none = uniform(gave_up) != 0;
             Place<1> wanted;
-            long long i = blockIdx.x;
+            unsigned i = blockIdx.x;
             for (bool more = true; more;) {
                 Item it{};
-                for (; i < total && !none;) {
+                while (i < total && !none) {
+                    const unsigned back = i / heads_x;
+                    const int hx = (int)(i - back * heads_x), head0 = p.pair ? 2 * hx : hx;
                     if (p.plan) {
-                        none = uniform(gave_up) != 0;
-                        const Piece y = p.plan[i / p.heads_x];
-                        const int hx = (int)(i % p.heads_x);
-                        if (!none) it = Item{y.q0, y.lq, y.k0, y.lk, y.t0, p.pair ? 2 * hx : hx, hx, y.ahead, y.place, y.first, y.piece, y.pieces, 1};
+                        const Piece y = p.plan[back];
+                        it = Item{y.q0, y.lq, y.k0, y.lk, y.t0, head0, hx, y.ahead, y.place, y.first, y.piece, y.pieces, 1};
                         break;
                     }
-                    const int x = p.tiles - 1 - (int)(i / p.heads_x), hx = (int)(i % p.heads_x);
-                    // the last sequence whose places begin at x or before it, 32 at a time;
-                    // the last 32 with all that there is to know about them
-                    int lo = 0, n = a.n_seqs;
-                    while (n > 32) {
-                        const int step = (n + 31) / 32, b = lo + step * (int)lane_id();
-                        const bool le = step * (int)lane_id() < n && a.q_offsets[b] / per + b <= x;
-                        const int k = max(0, 31 - __clz(__ballot_sync(0xffffffffu, le)));
-                        lo += k * step;
-                        n = min(step, n - k * step);
+                    const int x = tiles - 1 - (int)back;
+                    int k, t0;
+                    if (few) {
+                        k = max(0, __ffs(__ballot_sync(0xffffffffu, upto > x)) - 1);
+                        t0 = (x - __shfl_sync(0xffffffffu, upto - mine, k)) << per;
+                    } else {
+                        // the last sequence whose places begin at x or before it, 32 at a time
+                        int lo = 0, n = a.n_seqs;
+                        while (n > 32) {
+                            const int step = (n + 31) / 32, b = lo + step * (int)lane_id();
+                            const bool le = step * (int)lane_id() < n && (a.q_offsets[b] >> per) + b <= x;
+                            const int at = max(0, 31 - __clz(__ballot_sync(0xffffffffu, le)));
+                            lo += at * step;
+                            n = min(step, n - at * step);
+                        }
+                        const int b = lo + min((int)lane_id(), n - 1);
+                        fetch(b);
+                        k = max(0, 31 - __clz(__ballot_sync(0xffffffffu, (int)lane_id() < n && (vq0 >> per) + b <= x)));
+                        t0 = (x - (__shfl_sync(0xffffffffu, vq0, k) >> per) - (lo + k)) << per;
                     }
-                    const int b = lo + min((int)lane_id(), n - 1);
-                    const int vq0 = a.q_offsets[b], vq1 = a.q_offsets[b + 1], vk0 = a.k_offsets[b], vk1 = a.k_offsets[b + 1];
-                    const int k = max(0, 31 - __clz(__ballot_sync(0xffffffffu, (int)lane_id() < n && vq0 / per + b <= x)));
-                    const int q0 = __shfl_sync(0xffffffffu, vq0, k), q1 = __shfl_sync(0xffffffffu, vq1, k);
-                    const int k0 = __shfl_sync(0xffffffffu, vk0, k), k1 = __shfl_sync(0xffffffffu, vk1, k);
-                    const int t0 = (x - q0 / per - (lo + k)) * per;
-                    none = uniform(gave_up) != 0;
-                    if (!none && q0 >= 0 && q1 >= q0 && q1 <= a.q_tokens && k0 >= 0 && k1 >= k0 && k1 <= a.k_tokens && t0 >= 0 &&
-                        t0 < q1 - q0) {
-                        it = Item{q0, q1 - q0, k0, k1 - k0, t0, p.pair ? 2 * hx : hx, hx, (k1 - k0) - (q1 - q0), 0, 0, 0, 1, 1};
+                    const int q0 = __shfl_sync(0xffffffffu, vq0, k), lq = __shfl_sync(0xffffffffu, vq1, k) - q0;
+                    const int k0 = __shfl_sync(0xffffffffu, vk0, k), lk = __shfl_sync(0xffffffffu, vk1, k) - k0;
+                    if (__shfl_sync(0xffffffffu, (int)good(), k) && t0 >= 0 && t0 < lq) {
+                        it = Item{q0, lq, k0, lk, t0, head0, hx, lk - lq, 0, 0, 0, 1, 1};
                         break;
                     }
                     i = draw(p.next, total);

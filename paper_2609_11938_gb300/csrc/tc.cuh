@@ -9,6 +9,9 @@ namespace opattr {
 
 __device__ __forceinline__ uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
+// A condition whose code is to lie out of the way of the instructions fetched ahead.
+__device__ __forceinline__ bool seldom(bool x) { return __builtin_expect(x, 0); }
+
 // ---------------------------------------------------------------- barriers
 __device__ __forceinline__ void bar_init(uint32_t bar, unsigned count) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
@@ -51,7 +54,8 @@ __device__ __forceinline__ bool bar_wait_on(uint32_t bar, unsigned phase, volati
     return false;
 }
 __device__ __forceinline__ bool bar_wait(uint32_t bar, unsigned phase, volatile int *stop) {
-    return bar_done(bar, phase, SLEEP_NS) || bar_wait_on(bar, phase, stop);
+    if (seldom(!bar_done(bar, phase, SLEEP_NS))) return bar_wait_on(bar, phase, stop);
+    return true;
 }
 // The same for a whole warp that goes on together.
 __device__ __forceinline__ bool warp_wait(uint32_t bar, unsigned phase, volatile int *stop) {
