@@ -112,7 +112,8 @@ struct AppendPlan {
 __global__ void __launch_bounds__(PLAN_THREADS)
 k_append_plan(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offsets, int tokens, AppendPlan p,
               unsigned *err) {
-    __shared__ int warp_buf[33];
+    constexpr int HELD = 2048;
+    __shared__ int warp_buf[33], held_page[HELD];
     pdl_wait();
     if (threadIdx.x == 0) *p.go = 0;
     if (seqs_bad(seqs, n, kv.n_seqs, p.mark, err)) return;
@@ -136,6 +137,7 @@ k_append_plan(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offset
         }
         p.old[i] = old;
         p.to[i] = last;
+        if (i < HELD) held_page[i] = last;
     }
     if (any_bad(bad, SERVE_INVALID, err)) return;
     int total = 0;
@@ -149,7 +151,10 @@ k_append_plan(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offset
             if (last >= 0 && kv.refs[last] > 1) {
                 // one after another: those before it have copied theirs and let go
                 int held = kv.refs[last];
-                for (int k = 0; k < i && held > 1; ++k) held -= p.to[k] == last;
+                const int near = min(i, HELD);
+#pragma unroll 8
+                for (int k = 0; k < near; ++k) held -= held_page[k] == last;
+                for (int k = HELD; k < i; ++k) held -= p.to[k] == last;
                 if (held > 1) from = last;
             }
             p.from[i] = from;
@@ -213,16 +218,17 @@ k_append_rows(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offset
     const int per = kv.head_dim / 8;                              // pieces of a head's row
     uint4 *kp = reinterpret_cast<uint4 *>(kv.k_pages), *vp = reinterpret_cast<uint4 *>(kv.v_pages);
     if (blockIdx.x >= row_blocks) {
-        for (int i = blockIdx.x - row_blocks; i < n; i += gridDim.x - row_blocks) {
+        // a sequence's head at a time, as many threads as its filled rows have pieces
+        const int64_t all = (int64_t)n * kv.kv_heads, block = (int64_t)kv.page_size * per;
+        for (int64_t x = blockIdx.x - row_blocks; x < all; x += gridDim.x - row_blocks) {
+            const int i = (int)(x / kv.kv_heads), g = (int)(x % kv.kv_heads);
             if (p.from[i] < 0) continue;
             const int live = (p.old[i] % kv.page_size) * per;
-            const int64_t block = (int64_t)kv.page_size * per;
-            for (int x = threadIdx.x; x < live * kv.kv_heads; x += COPY_THREADS) {
-                const int64_t g = x / live, e = x % live;
-                const int64_t src = (p.from[i] * (int64_t)kv.kv_heads + g) * block + e;
-                const int64_t dst = (p.to[i] * (int64_t)kv.kv_heads + g) * block + e;
-                kp[dst] = kp[src];
-                vp[dst] = vp[src];
+            const int64_t src = (p.from[i] * (int64_t)kv.kv_heads + g) * block, dst = (p.to[i] * (int64_t)kv.kv_heads + g) * block;
+            for (int e = threadIdx.x; e < live; e += COPY_THREADS) {
+                const uint4 k4 = kp[src + e], v4 = vp[src + e];
+                kp[dst + e] = k4;
+                vp[dst + e] = v4;
             }
         }
         return;
@@ -270,7 +276,8 @@ opattr_status do_cache_append(Ctx &c, Serve &s, const opattr_cache *kv, const in
     p.room = (int32_t)most;
     launch(c, "append_plan", k_append_plan, dim3(1), dim3(plan_threads(n)), 0, *kv, seqs, n, offsets, (int)tokens, p, s.err);
     const int64_t pieces = tokens * kv->kv_heads * (kv->head_dim / 8);
-    const unsigned rows = grid_for(pieces, COPY_THREADS, 8u * sm_count(c)), shared = std::min<unsigned>(n, sm_count(c));
+    const unsigned rows = grid_for(pieces, COPY_THREADS, 8u * sm_count(c));
+    const unsigned shared = (unsigned)std::min<int64_t>((int64_t)n * kv->kv_heads, 2 * sm_count(c));
     launch(c, "append_rows", k_append_rows, dim3(rows + shared), dim3(COPY_THREADS), 0, *kv, seqs, n, offsets, (int)tokens,
            *k, *v, p, rows);
     return cuda_status(c, c.last_error);

@@ -28,7 +28,7 @@ constexpr int MMA_WARP = 8, LOAD_WARP = 9, TAIL_WARP = 10;   // and the last one
 // registers: 384 x 168 at launch = 256 x 208 + 128 x 88
 constexpr int REGS_SOFTMAX = 208, REGS_OTHERS = 88;
 constexpr int CUTS = 4;                  // value tiles cut by a mask that can be under way: half the ring's stages
-constexpr int SHORT = 4;                 // key tiles of an item that is over before the next one is looked up
+constexpr int SHORT = 4;                 // key tiles that take as long as the lookup of an item
 constexpr int ITEMS = 2;                 // slots of work items: the one being computed, and the one whose tiles are fetched
 
 // Shapes by the padded head width DP (64 or 128; the copies fill what a head
@@ -562,16 +562,17 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
             Item it;
             while (ok && item_next(it)) {
                 const Work w(it, p.pair, a.causal);
-                // A block draws its next item when this one's tiles are all on their way: drawn three
-                // ahead, the last items went to the blocks that asked first (8,192 causal tokens, 8
-                // heads of 128: 133 us, so 103).  Short ones it draws at once, as the lookup takes as
-                // long as they do (64 x 512 tokens, 8 heads of 64: 57 us, after their tiles 61).
-                if (lead && w.n <= SHORT) bar_arrive(smem_addr(&ctl.item_want));
+                // A block draws its next item when no more than SHORT of this one's tiles are left to
+                // fetch, which hides the lookup: drawn three ahead, the last items went to the blocks
+                // that asked first (8,192 causal tokens, 8 heads of 128: 133 us, so 103).
+                const int ask = max(0, 2 * (w.n - SHORT));
+                if (lead && w.n == 0) bar_arrive(smem_addr(&ctl.item_want));
                 const int g = it.head0 / (a.q_heads / a.kv_heads), subs = w.tiles[1] > 0 ? 2 : 1;
                 // the queries as soon as those before them are done with; until then the first keys
                 // and values go ahead, as far as the item before this one leaves stages free
                 bool q_due = true;
                 for (int load = 0; load < 2 * w.n; ++load) {
+                    if (lead && load == ask) bar_arrive(smem_addr(&ctl.item_want));
                     if (q_due && (load == S::STAGES - 2 || load == 2 * w.n - 1 ||
                                   __all_sync(0xffffffffu, bar_is_done(smem_addr(&ctl.q_free), q_turn.ph ^ 1)))) {
                         if (!(ok = warp_wait(smem_addr(&ctl.q_free), q_turn.ph ^ 1, stop))) break;
@@ -603,7 +604,6 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                     if (cut) over.step();
                     ring.step();
                 }
-                if (lead && w.n > SHORT) bar_arrive(smem_addr(&ctl.item_want));
             }
             // copies that nobody waits for any more
             int never = 0;
