@@ -16,6 +16,10 @@ namespace opattr {
 
 constexpr int PLAN_THREADS = 1024;         // at most: a plan of few sequences has fewer
 constexpr int COPY_THREADS = 256;
+// tokens whose pieces a thread has under way (four, with half the threads, took 97 us for
+// 55,000 tokens of 8 heads of 128, two 70)
+constexpr int ROWS_AHEAD = 2;
+constexpr int FIRST_TICKETS = 4096;
 
 bool cache_ok(const opattr_cache *k) {
     if (k->dtype != OPATTR_BF16 && k->dtype != OPATTR_F16) return false;
@@ -29,33 +33,38 @@ bool cache_ok(const opattr_cache *k) {
 
 opattr_status serve_ready(Ctx &c, Serve &s, int64_t tickets) {
     if (!s.err) {
-        cudaError_t e = cudaMalloc(&s.err, 256);
+        // with the first tickets behind it
+        cudaError_t e = cudaMalloc(&s.err, 256 + sizeof(uint32_t) * FIRST_TICKETS);
         if (e == cudaErrorMemoryAllocation) {
             cudaGetLastError();
             s.err = nullptr;
             return OPATTR_E_OOM;
         }
-        if (e == cudaSuccess) e = cudaMemsetAsync(s.err, 0, 256, c.stream);
+        if (e == cudaSuccess) e = cudaMemsetAsync(s.err, 0, 256 + sizeof(uint32_t) * FIRST_TICKETS, c.stream);
         if (e != cudaSuccess) return cuda_status(c, e);
+        s.tickets = s.err + 64;
+        s.n_tickets = FIRST_TICKETS;
     }
     if (tickets > s.n_tickets) {
         // launches before this one may still count in the old tickets
-        if (s.tickets) {
+        if (s.more) {
             const cudaError_t e = cudaStreamSynchronize(c.stream);
             if (e != cudaSuccess) return cuda_status(c, e);
-            cudaFree(s.tickets);
-            s.tickets = nullptr;
-            s.n_tickets = 0;
+            cudaFree(s.more);
         }
-        const int64_t n = tickets < 4096 ? 4096 : 2 * tickets;
-        cudaError_t e = cudaMalloc(&s.tickets, sizeof(uint32_t) * n);
+        s.more = nullptr;
+        s.tickets = s.err + 64;
+        s.n_tickets = FIRST_TICKETS;
+        const int64_t n = 2 * tickets;
+        cudaError_t e = cudaMalloc(&s.more, sizeof(uint32_t) * n);
         if (e == cudaErrorMemoryAllocation) {
             cudaGetLastError();
-            s.tickets = nullptr;
+            s.more = nullptr;
             return OPATTR_E_OOM;
         }
-        if (e == cudaSuccess) e = cudaMemsetAsync(s.tickets, 0, sizeof(uint32_t) * n, c.stream);
+        if (e == cudaSuccess) e = cudaMemsetAsync(s.more, 0, sizeof(uint32_t) * n, c.stream);
         if (e != cudaSuccess) return cuda_status(c, e);
+        s.tickets = s.more;
         s.n_tickets = n;
     }
     return OPATTR_OK;
@@ -63,7 +72,7 @@ opattr_status serve_ready(Ctx &c, Serve &s, int64_t tickets) {
 
 void serve_free(Serve &s) {
     if (s.err) cudaFree(s.err);
-    if (s.tickets) cudaFree(s.tickets);
+    if (s.more) cudaFree(s.more);
     s = Serve{};
 }
 
@@ -188,10 +197,16 @@ k_append_plan(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offset
     __syncthreads();
     if (any_bad(found < total, SERVE_PAGES, err)) return;
     // it holds: the tables change
+    const int32_t *first = p.first;
+    if (n < HELD) {                      // (the shared pages have been ranked)
+        for (int i = threadIdx.x; i <= n; i += blockDim.x) held_page[i] = p.first[i];
+        __syncthreads();
+        first = held_page;
+    }
     for (int k = threadIdx.x; k < total; k += blockDim.x) {
-        const int i = seq_of_row(p.first, n, k), s = seqs[i], page = p.fresh[k];
+        const int i = seq_of_row(first, n, k), s = seqs[i], page = p.fresh[k];
         const int have = pages_for(p.old[i], kv.page_size), copied = p.from[i] >= 0;
-        kv.table[(int64_t)s * kv.pages_per_seq + have - copied + (k - p.first[i])] = page;
+        kv.table[(int64_t)s * kv.pages_per_seq + have - copied + (k - first[i])] = page;
         kv.refs[page] = 1;
     }
     for (int i = threadIdx.x; i < n; i += blockDim.x) {
@@ -233,15 +248,36 @@ k_append_rows(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offset
         }
         return;
     }
-    const int64_t pieces = (int64_t)tokens * kv.kv_heads * per;
-    for (int64_t x = (int64_t)blockIdx.x * COPY_THREADS + threadIdx.x; x < pieces; x += (int64_t)row_blocks * COPY_THREADS) {
-        const int e = (int)(x % per), g = (int)(x / per % kv.kv_heads), t = (int)(x / per / kv.kv_heads);
-        const int i = seq_of_row(offsets, n, t), pos = p.old[i] + t - offsets[i];
-        const int page = kv.table[(int64_t)seqs[i] * kv.pages_per_seq + pos / kv.page_size];
-        if (page < 0 || page >= kv.n_pages) continue;             // a table that was not consistent before the call
-        const int64_t dst = ((page * (int64_t)kv.kv_heads + g) * kv.page_size + pos % kv.page_size) * per + e;
-        kp[dst] = *reinterpret_cast<const uint4 *>((const uint16_t *)k.data + t * k.token_stride + g * k.head_stride + 8 * e);
-        vp[dst] = *reinterpret_cast<const uint4 *>((const uint16_t *)v.data + t * v.token_stride + g * v.head_stride + 8 * e);
+    // a thread keeps its piece of a row and goes from token to token, so that nothing is divided
+    // on the way (that cost more than the copies)
+    const int row = kv.kv_heads * per, side = max(1, COPY_THREADS / row), sub = threadIdx.x / row;
+    if (sub >= side) return;
+    for (int r = threadIdx.x % row; r < row; r += COPY_THREADS) {
+        const int g = r / per, e = r % per;
+        const uint16_t *kr = (const uint16_t *)k.data + g * k.head_stride + 8 * e;
+        const uint16_t *vr = (const uint16_t *)v.data + g * v.head_stride + 8 * e;
+        const int64_t step = (int64_t)row_blocks * side;
+        for (int64_t t0 = (int64_t)blockIdx.x * side + sub; t0 < tokens; t0 += ROWS_AHEAD * step) {
+            uint4 k4[ROWS_AHEAD], v4[ROWS_AHEAD];
+#pragma unroll
+            for (int q = 0; q < ROWS_AHEAD; ++q) {
+                const int64_t t = t0 + q * step;
+                if (t >= tokens) break;
+                k4[q] = *reinterpret_cast<const uint4 *>(kr + t * k.token_stride);
+                v4[q] = *reinterpret_cast<const uint4 *>(vr + t * v.token_stride);
+            }
+#pragma unroll
+            for (int q = 0; q < ROWS_AHEAD; ++q) {
+                const int64_t t = t0 + q * step;
+                if (t >= tokens) break;
+                const int i = seq_of_row(offsets, n, (int)t), pos = p.old[i] + (int)t - offsets[i];
+                const int page = kv.table[(int64_t)seqs[i] * kv.pages_per_seq + pos / kv.page_size];
+                if (page < 0 || page >= kv.n_pages) continue;     // a table that was not consistent before the call
+                const int64_t dst = ((page * (int64_t)kv.kv_heads + g) * kv.page_size + pos % kv.page_size) * per + e;
+                kp[dst] = k4[q];
+                vp[dst] = v4[q];
+            }
+        }
     }
 }
 
@@ -275,8 +311,8 @@ opattr_status do_cache_append(Ctx &c, Serve &s, const opattr_cache *kv, const in
     p.fresh = a.take<int32_t>(most);
     p.room = (int32_t)most;
     launch(c, "append_plan", k_append_plan, dim3(1), dim3(plan_threads(n)), 0, *kv, seqs, n, offsets, (int)tokens, p, s.err);
-    const int64_t pieces = tokens * kv->kv_heads * (kv->head_dim / 8);
-    const unsigned rows = grid_for(pieces, COPY_THREADS, 8u * sm_count(c));
+    const int row = kv->kv_heads * (kv->head_dim / 8);
+    const unsigned rows = grid_for(tokens, std::max(1, COPY_THREADS / row), 8u * sm_count(c));
     const unsigned shared = (unsigned)std::min<int64_t>((int64_t)n * kv->kv_heads, 2 * sm_count(c));
     launch(c, "append_rows", k_append_rows, dim3(rows + shared), dim3(COPY_THREADS), 0, *kv, seqs, n, offsets, (int)tokens,
            *k, *v, p, rows);
@@ -286,7 +322,7 @@ opattr_status do_cache_append(Ctx &c, Serve &s, const opattr_cache *kv, const in
 // ---------------------------------------------------------------- fork and trim
 // The plan's block makes the change itself where the sequences' tables have few
 // entries, a warp to a sequence; a second launch costs 2.5 us.
-constexpr int64_t SMALL_ENTRIES = 16384;
+constexpr int64_t SMALL_ENTRIES = 4096;
 
 // Of sequence d: the pages of s, by the threads first, first + step, ..
 __device__ __forceinline__ void fork_pages(const opattr_cache &kv, int s, int d, int first, int step) {
@@ -465,18 +501,30 @@ k_compact_place(opattr_cache kv, const int32_t *tile_live, int tiles, int32_t *r
         if (out_live) *out_live = L;
     }
 }
-// Pages over the grid, 16 bytes a thread; then the tables.
+constexpr int MOVE = 4 * COPY_THREADS;          // pieces of 16 bytes of a run
+// Pages over the grid; then the tables.
 __global__ void __launch_bounds__(COPY_THREADS)
 k_compact_move(opattr_cache kv, const int32_t *rank, const int32_t *hole, const int32_t *mover, const int32_t *counts) {
     pdl_wait();
     const int moves = counts[0], L = counts[1];
-    const int64_t page = (int64_t)kv.kv_heads * kv.page_size * (kv.head_dim / 8), all = moves * page;
+    const int page = kv.kv_heads * kv.page_size * (kv.head_dim / 8), runs = (page + MOVE - 1) / MOVE;
     const int64_t t0 = (int64_t)blockIdx.x * COPY_THREADS + threadIdx.x, step = (int64_t)gridDim.x * COPY_THREADS;
     uint4 *kp = reinterpret_cast<uint4 *>(kv.k_pages), *vp = reinterpret_cast<uint4 *>(kv.v_pages);
-    for (int64_t x = t0; x < all; x += step) {
-        const int64_t m = x / page, e = x % page, src = mover[m] * page + e, dst = hole[m] * page + e;
-        kp[dst] = kp[src];
-        vp[dst] = vp[src];
+    // runs of a page's pieces, a block to each: every thread has all its loads under way before it stores
+    for (int64_t u = blockIdx.x; u < (int64_t)moves * runs; u += gridDim.x) {
+        const int m = (int)(u / runs), first = (int)(u % runs) * MOVE + threadIdx.x;
+        const int64_t src = mover[m] * (int64_t)page, dst = hole[m] * (int64_t)page;
+        uint4 k4[MOVE / COPY_THREADS], v4[MOVE / COPY_THREADS];
+#pragma unroll
+        for (int q = 0; q < MOVE / COPY_THREADS; ++q) {
+            const int e = first + q * COPY_THREADS;
+            if (e < page) k4[q] = kp[src + e], v4[q] = vp[src + e];
+        }
+#pragma unroll
+        for (int q = 0; q < MOVE / COPY_THREADS; ++q) {
+            const int e = first + q * COPY_THREADS;
+            if (e < page) kp[dst + e] = k4[q], vp[dst + e] = v4[q];
+        }
     }
     for (int64_t m = t0; m < moves; m += step) {
         kv.refs[hole[m]] = kv.refs[mover[m]];

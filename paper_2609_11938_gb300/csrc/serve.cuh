@@ -18,8 +18,9 @@ enum ServeErr : unsigned {
 
 // Device state of the context's operators, made by the first of their calls.
 struct Serve {
-    unsigned *err = nullptr;         // ServeErr bits, sticky
-    uint32_t *tickets = nullptr;     // arrivals at each joined output row block; zero between launches
+    unsigned *err = nullptr;         // ServeErr bits, sticky; at word 16 the prompts' count of work items drawn
+    uint32_t *tickets = nullptr;     // arrivals at each joined block of results; zero between launches
+    uint32_t *more = nullptr;        // where there are more of them than come with err
     int64_t n_tickets = 0;
 };
 
