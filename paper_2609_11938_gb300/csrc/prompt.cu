@@ -4,6 +4,30 @@
 //   s_ij = scale * q_i . k_j,  j seen by i: j < Lk and, causal, j <= i + Lk - Lq
 //   o_i = sum_j exp(s_ij - m_i) v_j / sum_j exp(s_ij - m_i),  lse_i = m_i + log of that sum
 // A row that sees no key gets o = 0 and lse = -inf.
+//
+// One pass over the keys with a running maximum and sum.  A block holds two sub-tiles
+// of 128 rows (queries; heads that share keys side by side) and takes their keys 128
+// at a time:
+//   S [128 x 128] = Q K^T       both from shared memory, into tensor memory
+//   P = 2^(S c - m)             a thread per row, back into tensor memory in 16 bits
+//   O [128 x D]  += P V         P from tensor memory, V as it lies (its rows are keys)
+// with a row's m raised, and O and the sum rescaled, only when a new maximum is more
+// than a few powers of two above it.  Tensor memory is full: two S and two O of 128
+// columns each, P in the place of S.  While one sub-tile's softmax runs, the tensor
+// cores have the other's products to do.  Warps: 0 .. 3 and 4 .. 7 the two softmax
+// groups, 8 issues the products, 9 the tile copies into a ring of five (width 128) or
+// eight tiles, 10 looks over value tiles that a mask cuts, 11 looks up work items.
+// P is rounded to the inputs' type, which is what the products take: an error of the
+// size of the result's own rounding.
+//
+// Measured on one GB300 (bfloat16, causal unless said): 12,301 tokens, 32 heads of 128 on 8:
+// 770 us, 1,610 TFLOP/s; 9,728, 16 heads on 4, all keys seen: 470 us, 1,645 (there the
+// power limit holds the clock at 1.6 GHz and the tensor cores are busy for three
+// quarters of the cycles); 16 heads of 64: 405 us, 955.  At width 64 a tile's exponentials
+// and its trips through tensor memory (1,500 cycles of a group, of them 512 of the
+// special function unit) take longer than its products (512), and short prompts wait
+// for one tile's chain of steps: 8 x 512 tokens, 8 heads of 64, all seen, 17,600 cycles,
+// of which four tiles are 9,200.
 #include <math.h>
 
 #include <algorithm>
@@ -22,7 +46,7 @@ bool rows_ok(const opattr_rows &r, int64_t tokens, int heads, int dim) {
 }
 
 constexpr int KEYS = 128;                // keys of a tile
-constexpr int ROWS = 128;                // queries of a sub-tile: one thread and one lane of tensor memory each
+constexpr int ROWS = 128;                // rows of a sub-tile: one thread and one lane of tensor memory each
 constexpr int THREADS = 384;             // two warpgroups for the softmax of two sub-tiles, one for the rest
 constexpr int MMA_WARP = 8, LOAD_WARP = 9, TAIL_WARP = 10;   // and the last one looks up items
 // registers: 384 x 168 at launch = 256 x 208 + 128 x 88
@@ -44,8 +68,9 @@ struct Shape {
 
 struct PromptArgs {
     opattr_prompt a;
-    int heads_x;                         // work items side by side: pairs of heads, or heads
-    int pair;                            // 1: an item's sub-tiles are two heads of one key head; 0: 256 queries of one
+    // a sub-tile's rows are `pack` heads of one key head of `span` tokens, head by head; an item
+    // has two of them, one behind the other, and heads_x items stand side by side
+    int pack, span, heads_x;
     int tiles;                           // places of query tiles
     int q_mul, k_mul, v_mul;             // 0 where all heads read the same rows
     int wide;                            // 1: rows of the output are 32-byte aligned and DP wide
@@ -94,12 +119,12 @@ struct Place {
 struct Work {
     int base[2], tiles[2], clean[2];     // first query; key tiles; the first of them that a mask cuts
     int n, cut;                          // key tiles of either; the first that is looked over
-    __device__ __forceinline__ Work(const Item &it, int pair, int causal) {
+    __device__ __forceinline__ Work(const Item &it, int span, int causal) {
         const int ahead = it.ahead;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            base[s] = pair ? it.t0 : it.t0 + s * ROWS;
-            const int rows = min(ROWS, it.lq - base[s]);
+            base[s] = it.t0 + s * span;
+            const int rows = min(span, it.lq - base[s]);
             const int keys = rows <= 0 ? 0 : causal ? max(0, min(it.lk, base[s] + rows + ahead)) : it.lk;
             tiles[s] = (keys + KEYS - 1) / KEYS;
             clean[s] = (causal ? max(0, min(it.lk, base[s] + 1 + ahead)) : it.lk) / KEYS;
@@ -206,6 +231,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
         // (a negative scale's sign is the products'; for none, the least that keeps -inf what it is)
         const float c = a.scale == 0.f ? __uint_as_float(1) : fabsf(a.scale) * LOG2E;
         const uint64_t c2 = pair(c, c);
+        const int row_token = r / p.pack, row_head = r % p.pack;
         Place<1> turn_s, turn_o;
         Place<CUTS> over;                                // cut value tiles, of either sub-tile
         Place<S::STAGES> ring;                           // value tiles
@@ -213,10 +239,13 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
         Item it;
         bool ok = true;
         while (ok && item_next(it)) {
-            const Work w(it, p.pair, a.causal);
+            const Work w(it, p.span, a.causal);
             const int n_tiles = s ? w.tiles[1] : w.tiles[0], clean = s ? w.clean[1] : w.clean[0];
-            const int head = p.pair ? it.head0 + s : it.head0, row = (s ? w.base[1] : w.base[0]) + r;
+            const int head = it.head0 + row_head, row = (s ? w.base[1] : w.base[0]) + row_token;
             const int seen = a.causal ? min(it.lk, row + 1 + it.ahead) : it.lk;
+            // (rows past the queries, or past the sub-tile's last whole token, are nobody's: what
+            // is in them has no say in when the others are rescaled)
+            const bool live = row < it.lq && row_token < p.span;
             float m = -INFINITY, l = 0.f;
             for (int j = 0; j < w.n; ++j) {
                 if (j < n_tiles) {
@@ -244,7 +273,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                         for (int q = 0; q < 4; ++q)
                             t[q] = max3(t[q], __uint_as_float(x[i + 2 * q]), __uint_as_float(x[i + 2 * q + 1]));
                     const float top = fmaxf(max3(m, t[0], t[1]), fmaxf(t[2], t[3]));
-                    if (__any_sync(0xffffffffu, (top - m) * c > SLACK)) {
+                    if (__any_sync(0xffffffffu, live && (top - m) * c > SLACK)) {
                         const float keep = top == m ? 1.f : exp2_fast((m - top) * c);
                         m = top;
                         l *= keep;
@@ -348,7 +377,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                 turn_o.step();
                 tm_after();
             }
-            const bool live = row < it.lq, wide = p.wide;
+            const bool wide = p.wide;
             float ref = m == -INFINITY ? m : m * c;      // the row's sum counts in 2^(ref - OFFSET)
             bool mine = true, joined = false;
             const float *parts = nullptr;
@@ -475,7 +504,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
             bool ok = true;
             Item it;
             while (ok && item_next(it)) {
-                const Work w(it, p.pair, a.causal);
+                const Work w(it, p.span, a.causal);
                 const int nt = uniform(w.n), nt0 = uniform(w.tiles[0]), nt1 = uniform(w.tiles[1]), from = uniform(w.cut);
                 if (nt == 0) continue;
                 bool by_hand = false;
@@ -561,7 +590,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
             int q_out = 0;
             Item it;
             while (ok && item_next(it)) {
-                const Work w(it, p.pair, a.causal);
+                const Work w(it, p.span, a.causal);
                 // A block draws its next item when no more than SHORT of this one's tiles are left to
                 // fetch, which hides the lookup: drawn three ahead, the last items went to the blocks
                 // that asked first (8,192 causal tokens, 8 heads of 128: 133 us, so 103).
@@ -579,11 +608,11 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                         q_turn.step();
                         q_due = false;
                         if (lead) {
-                            bar_expect(bq, subs * S::TILE);
+                            bar_expect(bq, subs * p.pack * p.span * DP * 2);
                             for (int s = 0; s < subs; ++s)
                                 for (int d = 0; d < DP / 64; ++d)
-                                    tile_load(sq + s * S::TILE + d * S::HALF, &mq, 64 * d,
-                                              (p.pair ? it.head0 + s : it.head0) * p.q_mul, it.q0 + (s ? w.base[1] : w.base[0]), bq);
+                                    tile_load(sq + s * S::TILE + d * S::HALF, &mq, 64 * d, it.head0 * p.q_mul,
+                                              it.q0 + (s ? w.base[1] : w.base[0]), bq);
                         }
                         q_out = 1;
                     }
@@ -622,7 +651,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
             bool ok = true;
             Item it;
             while (ok && item_next(it)) {
-                const Work w(it, p.pair, a.causal);
+                const Work w(it, p.span, a.causal);
                 for (int j = 0; j < w.n; ++j, ring.step(), ring.step()) {
                     if (j < w.cut) continue;
                     if (!(ok = warp_wait(smem_addr(&ctl.v_full[over.at]), over.ph, stop))) break;
@@ -656,7 +685,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
             // keeps of one of them.  Of more, sequence b has the places from q_offsets[b] / per + b
             // on, enough for its tiles whatever comes before it; those it does not need are passed
             // over.  A block's first item is its number, others are drawn.
-            const int per = p.pair ? 7 : 8;              // queries of an item, as a shift
+            const int per = 2 * p.span;                  // tokens of an item
             const bool few = !p.plan && a.n_seqs <= 32;
             // after a wait that gave up nothing more is begun
             const unsigned gave_up = *(volatile unsigned *)err & SERVE_TIMEOUT;
@@ -670,7 +699,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
             int mine = 0, upto = 0, tiles = p.tiles;
             if (few) {
                 fetch(min((int)lane_id(), a.n_seqs - 1));
-                mine = (int)lane_id() < a.n_seqs && good() ? (vq1 - vq0 + (1 << per) - 1) >> per : 0;
+                mine = (int)lane_id() < a.n_seqs && good() ? (vq1 - vq0 + per - 1) / per : 0;
                 upto = warp_inclusive_scan(mine);
                 tiles = min(tiles, __shfl_sync(0xffffffffu, upto, 31));
             } else if (p.plan) {
@@ -684,7 +713,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                 Item it{};
                 while (i < total && !none) {
                     const unsigned back = i / heads_x;
-                    const int hx = (int)(i - back * heads_x), head0 = p.pair ? 2 * hx : hx;
+                    const int hx = (int)(i - back * heads_x), head0 = hx * p.pack;
                     if (p.plan) {
                         const Piece y = p.plan[back];
                         it = Item{y.q0, y.lq, y.k0, y.lk, y.t0, head0, hx, y.ahead, y.place, y.first, y.piece, y.pieces, 1};
@@ -694,21 +723,21 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                     int k, t0;
                     if (few) {
                         k = max(0, __ffs(__ballot_sync(0xffffffffu, upto > x)) - 1);
-                        t0 = (x - __shfl_sync(0xffffffffu, upto - mine, k)) << per;
+                        t0 = (x - __shfl_sync(0xffffffffu, upto - mine, k)) * per;
                     } else {
                         // the last sequence whose places begin at x or before it, 32 at a time
                         int lo = 0, n = a.n_seqs;
                         while (n > 32) {
                             const int step = (n + 31) / 32, b = lo + step * (int)lane_id();
-                            const bool le = step * (int)lane_id() < n && (a.q_offsets[b] >> per) + b <= x;
+                            const bool le = step * (int)lane_id() < n && a.q_offsets[b] / per + b <= x;
                             const int at = max(0, 31 - __clz(__ballot_sync(0xffffffffu, le)));
                             lo += at * step;
                             n = min(step, n - at * step);
                         }
                         const int b = lo + min((int)lane_id(), n - 1);
                         fetch(b);
-                        k = max(0, 31 - __clz(__ballot_sync(0xffffffffu, (int)lane_id() < n && (vq0 >> per) + b <= x)));
-                        t0 = (x - (__shfl_sync(0xffffffffu, vq0, k) >> per) - (lo + k)) << per;
+                        k = max(0, 31 - __clz(__ballot_sync(0xffffffffu, (int)lane_id() < n && vq0 / per + b <= x)));
+                        t0 = (x - __shfl_sync(0xffffffffu, vq0, k) / per - (lo + k)) * per;
                     }
                     const int q0 = __shfl_sync(0xffffffffu, vq0, k), lq = __shfl_sync(0xffffffffu, vq1, k) - q0;
                     const int k0 = __shfl_sync(0xffffffffu, vk0, k), lk = __shfl_sync(0xffffffffu, vk1, k) - k0;
@@ -759,7 +788,7 @@ __global__ void __launch_bounds__(1024) k_prompt_plan(PromptArgs p, int sms, Pie
     __shared__ long long wide_buf[33];
     pdl_wait();
     const opattr_prompt &a = p.a;
-    const int per = p.pair ? ROWS : 2 * ROWS;
+    const int per = 2 * p.span;
     Item it{};
     auto look = [&](int x) {                             // key tiles of place x; 0: it has no queries
         const int b = [&] {
@@ -775,7 +804,7 @@ __global__ void __launch_bounds__(1024) k_prompt_plan(PromptArgs p, int sms, Pie
         const int t0 = (x - q0 / per - b) * per;
         if (q0 < 0 || q1 < q0 || q1 > a.q_tokens || k0 < 0 || k1 < k0 || k1 > a.k_tokens || t0 < 0 || t0 >= q1 - q0) return 0;
         it = Item{q0, q1 - q0, k0, k1 - k0, t0, 0, 0, (k1 - k0) - (q1 - q0), x, 0, 0, 1, 1};
-        return max(1, Work(it, p.pair, a.causal).n);
+        return max(1, Work(it, p.span, a.causal).n);
     };
     long long all = 0;
     for (int x = threadIdx.x; x < p.tiles; x += 1024) all += look(x);
@@ -817,13 +846,13 @@ static EncodeTiled encode_tiled() {
     return fn;
 }
 
-// Boxes of 128 rows of 64 elements of one head; past a head's width or the last row: zeros.
-static bool row_map(CUtensorMap *m, int dtype, const opattr_rows &r, int64_t tokens, int heads, int dim) {
+// Boxes of 64 elements of `pack` heads of `span` rows; past a head's width or the last row: zeros.
+static bool row_map(CUtensorMap *m, int dtype, const opattr_rows &r, int64_t tokens, int heads, int dim, int pack, int span) {
     const bool one = heads == 1 || r.head_stride == 0;
     const cuuint64_t dims[3] = {(cuuint64_t)dim, (cuuint64_t)(one ? 1 : heads), (cuuint64_t)tokens};
     const cuuint64_t strides[2] = {2 * (cuuint64_t)(one ? dim : r.head_stride),
                                    2 * (cuuint64_t)(tokens == 1 ? dim : r.token_stride)};
-    const cuuint32_t box[3] = {64, 1, 128}, step[3] = {1, 1, 1};
+    const cuuint32_t box[3] = {64, (cuuint32_t)pack, (cuuint32_t)span}, step[3] = {1, 1, 1};
     return encode_tiled()(m, dtype == OPATTR_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
                           r.data, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -882,12 +911,18 @@ opattr_status do_attention(Ctx &c, Serve &s, const opattr_prompt *a) {
     PromptArgs p{};
     p.a = *a;
     const int group = a->q_heads / a->kv_heads;
-    p.pair = group % 2 == 0;
-    p.heads_x = p.pair ? a->q_heads / 2 : a->q_heads;
-    const int64_t tiles = a->q_tokens / (p.pair ? ROWS : 2 * ROWS) + a->n_seqs;
+    p.q_mul = a->q_heads > 1 && a->q.head_stride != 0;
+    // Heads that share keys share a sub-tile: as many of a group as leave at most 8 of its rows
+    // over, so that short runs of queries fill it too (five pieces of prompts of 60 .. 1,021
+    // queries, 20 heads on 4: 143 us, by 256 queries of a head 160)
+    p.pack = 1;
+    for (int k = 2; k <= ROWS && p.q_mul; ++k)
+        if (group % k == 0 && k * (ROWS / k) >= ROWS - 8) p.pack = k;
+    p.span = ROWS / p.pack;
+    p.heads_x = a->q_heads / p.pack;
+    const int64_t tiles = a->q_tokens / (2 * p.span) + a->n_seqs;
     if (tiles * p.heads_x > INT32_MAX) return OPATTR_E_INVALID_ARG;
     p.tiles = (int)tiles;
-    p.q_mul = a->q_heads > 1 && a->q.head_stride != 0;
     p.next = s.err + 16;                                 // its own line
     p.wide = a->head_dim % 64 == 0 && (reinterpret_cast<uintptr_t>(a->out.data) & 31) == 0 &&
              (a->q_tokens == 1 || a->out.token_stride % 16 == 0) && (a->q_heads == 1 || a->out.head_stride % 16 == 0);
@@ -896,9 +931,11 @@ opattr_status do_attention(Ctx &c, Serve &s, const opattr_prompt *a) {
     if (!encode_tiled()) return OPATTR_E_CUDA;
     // without keys there is nothing to copy, and any rows stand in for them
     CUtensorMap m[3];
-    if (!row_map(&m[0], a->dtype, a->q, a->q_tokens, a->q_heads, a->head_dim) ||
-        !row_map(&m[1], a->dtype, a->k_tokens ? a->k : a->q, a->k_tokens ? a->k_tokens : 1, a->kv_heads, a->head_dim) ||
-        !row_map(&m[2], a->dtype, a->k_tokens ? a->v : a->q, a->k_tokens ? a->k_tokens : 1, a->kv_heads, a->head_dim))
+    const opattr_rows &k = a->k_tokens ? a->k : a->q, &v = a->k_tokens ? a->v : a->q;
+    const int64_t keys = a->k_tokens ? a->k_tokens : 1;
+    if (!row_map(&m[0], a->dtype, a->q, a->q_tokens, a->q_heads, a->head_dim, p.pack, p.span) ||
+        !row_map(&m[1], a->dtype, k, keys, a->kv_heads, a->head_dim, 1, KEYS) ||
+        !row_map(&m[2], a->dtype, v, keys, a->kv_heads, a->head_dim, 1, KEYS))
         return OPATTR_E_INVALID_ARG;
     return a->dtype == OPATTR_BF16 ? prompt_of<__nv_bfloat16>(c, s, p, m) : prompt_of<__half>(c, s, p, m);
 }

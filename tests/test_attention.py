@@ -63,7 +63,8 @@ def test_prompt_lengths(ctx, dtype, dim, causal, lens):
     check_prompt(ctx, q, k, v, lens, None, causal)
 
 
-@pytest.mark.parametrize("heads,kv", [(1, 1), (3, 3), (7, 1), (12, 4), (16, 16), (40, 8)])
+@pytest.mark.parametrize("heads,kv", [(1, 1), (3, 3), (7, 1), (12, 4), (16, 16), (40, 8), (13, 1), (26, 2), (48, 1),
+                                      (120, 1), (131, 1), (256, 2)])
 def test_prompt_heads(ctx, heads, kv):
     g = gen(heads)
     lens = [150, 33]
@@ -84,6 +85,18 @@ def test_prompt_pieces(ctx, dtype, dim, causal, lq, lk):
     out, lse = check_prompt(ctx, q, k, v, lq, lk, causal)
     if causal and lq == [300]:
         assert (out[:295] == 0).all() and (lse[:295] == -math.inf).all()
+
+
+@pytest.mark.parametrize("heads,kv", [(2, 2), (6, 2), (4, 1)])
+def test_prompt_neighbours(ctx, heads, kv):
+    """A sequence's bits do not depend on the queries, keys and values packed beside it."""
+    g = gen(21)
+    lens = [137, 300, 41]
+    q, k, v = (randn(g, (478, h, 64), BF) for h in (heads, kv, kv))
+    want = ctx.attention(q, k, v, offsets(lens))[1][137:437]
+    for x in (q, k, v):
+        x[:137], x[437:] = 50.0, -80.0
+    assert torch.equal(ctx.attention(q, k, v, offsets(lens))[1][137:437], want)
 
 
 def test_prompt_long(ctx):
@@ -139,6 +152,7 @@ def test_prompt_views(ctx):
     check_prompt(ctx, hq, hk, hv, [n], None, True)
     one = randn(g, (n, 1, D), BF)
     check_prompt(ctx, q, one.expand(n, G, D), v, [n], None, False)        # one key head for all
+    check_prompt(ctx, one.expand(n, H, D), k, v, [n], None, True)         # one query for all heads
 
 
 @pytest.mark.parametrize("dtype", [BF, HF])
