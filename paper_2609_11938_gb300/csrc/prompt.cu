@@ -882,8 +882,12 @@ static opattr_status run_prompt(Ctx &c, Serve &s, PromptArgs &p, const CUtensorM
         p.tickets = s.tickets;
         launch(c, "prompt_plan", k_prompt_plan, dim3(1), dim3(1024), 0, p, sms, plan, n);
     }
-    const cudaError_t e = cudaFuncSetAttribute(k_prompt<T, DP, DV>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
-    if (e != cudaSuccess) return cuda_status(c, e);
+    constexpr unsigned bit = 1u << ((std::is_same<T, __half>::value ? 3 : 0) + (DP == 64 ? 0 : DV == 96 ? 1 : 2));
+    if (!(s.prompt_room & bit)) {
+        const cudaError_t e = cudaFuncSetAttribute(k_prompt<T, DP, DV>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
+        if (e != cudaSuccess) return cuda_status(c, e);
+        s.prompt_room |= bit;
+    }
     launch(c, "prompt", k_prompt<T, DP, DV>, dim3((unsigned)(p.plan ? sms : std::min<int64_t>(items, sms))), dim3(THREADS), S::SMEM, p, m[0],
            m[1], m[2], s.err);
     return cuda_status(c, c.last_error);

@@ -22,6 +22,7 @@ struct Serve {
     uint32_t *tickets = nullptr;     // arrivals at each joined block of results; zero between launches
     uint32_t *more = nullptr;        // where there are more of them than come with err
     int64_t n_tickets = 0;
+    unsigned prompt_room = 0;        // variants of the prompt kernel that have their shared memory
 };
 
 opattr_status serve_ready(Ctx &c, Serve &s, int64_t tickets);
