@@ -675,15 +675,20 @@ opattr_status opattr_check(opattr_ctx *ctx) {
     DeviceGuard g(c.device);
     if (!g.ok) return OPATTR_E_CUDA;
     unsigned found = 0;
+    Serve &v = ctx->serve;
     cudaError_t e = cudaSuccess;
-    if (ctx->serve.err) {
-        e = cudaMemcpyAsync(c.h_small, ctx->serve.err, sizeof(unsigned), cudaMemcpyDeviceToHost, c.stream);
-        // (with the count of work items, which a wait that gave up may leave behind)
-        if (e == cudaSuccess) e = cudaMemsetAsync(ctx->serve.err, 0, 256, c.stream);
+    if (v.err) {
+        e = cudaMemcpyAsync(c.h_small, v.err, sizeof(unsigned), cudaMemcpyDeviceToHost, c.stream);
+        if (e == cudaSuccess) e = cudaMemsetAsync(v.err, 0, sizeof(unsigned), c.stream);
     }
     if (e == cudaSuccess) e = cudaStreamSynchronize(c.stream);
+    if (e == cudaSuccess && v.err && (found = c.h_small[0]) & SERVE_TIMEOUT) {
+        // a launch that gave up leaves its counts as they were
+        e = cudaMemsetAsync(v.err, 0, 256, c.stream);
+        if (e == cudaSuccess) e = cudaMemsetAsync(v.tickets, 0, sizeof(uint32_t) * v.n_tickets, c.stream);
+        if (e == cudaSuccess) e = cudaStreamSynchronize(c.stream);
+    }
     if (e != cudaSuccess || c.last_error != cudaSuccess) return finish(c, cuda_status(c, e));
-    if (ctx->serve.err) found = c.h_small[0];
     if (c.timing) timing_collect(c);
     if (found & SERVE_TIMEOUT) return OPATTR_E_TIMEOUT;
     return found & SERVE_INVALID ? OPATTR_E_INVALID_ARG : found & SERVE_PAGES ? OPATTR_E_PAGES : OPATTR_OK;
