@@ -109,6 +109,7 @@ struct AppendPlan {
     int32_t *go;        // [1] 1: the call holds
     int32_t *old;       // [n] lengths before
     int32_t *from, *to; // [n] a partly filled page that is copied first, and where to; -1 none
+    int32_t *late;      // [n] a page that this sequence keeps and shortens for one that copies it; -1 none
     int32_t *mark;      // [n_seqs]
     int32_t *first;     // [n + 1] new pages before this sequence's
     int32_t *fresh;     // new pages in the order they are given out
@@ -123,6 +124,7 @@ k_append_plan(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offset
               unsigned *err) {
     constexpr int HELD = 2048;
     __shared__ int warp_buf[33], held_page[HELD];
+    __shared__ uint16_t held_part[HELD];
     pdl_wait();
     if (threadIdx.x == 0) *p.go = 0;
     if (seqs_bad(seqs, n, kv.n_seqs, p.mark, err)) return;
@@ -146,27 +148,33 @@ k_append_plan(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offset
         }
         p.old[i] = old;
         p.to[i] = last;
-        if (i < HELD) held_page[i] = last;
+        if (i < HELD) held_page[i] = last, held_part[i] = (uint16_t)(old % kv.page_size);
     }
     if (any_bad(bad, SERVE_INVALID, err)) return;
     int total = 0;
+    bool any_late = false;
     for (int i0 = 0; i0 < n; i0 += blockDim.x) {
         const int i = i0 + threadIdx.x;
         int need = 0;
         if (i < n) {
             const int old = p.old[i], more = offsets[i + 1] - offsets[i], last = p.to[i];
             need = pages_for(old + more, kv.page_size) - pages_for(old, kv.page_size);
-            int from = -1;
+            int from = -1, late = -1;
             if (last >= 0 && kv.refs[last] > 1) {
                 // one after another: those before it have copied theirs and let go
-                int held = kv.refs[last];
+                int held = kv.refs[last], longest = 0;
                 const int near = min(i, HELD);
 #pragma unroll 8
-                for (int k = 0; k < near; ++k) held -= held_page[k] == last;
-                for (int k = HELD; k < i; ++k) held -= p.to[k] == last;
+                for (int k = 0; k < near; ++k)
+                    if (held_page[k] == last) --held, longest = max(longest, (int)held_part[k]);
+                for (int k = HELD; k < i; ++k)
+                    if (p.to[k] == last) --held, longest = max(longest, p.old[k] % kv.page_size);
                 if (held > 1) from = last;
+                else if (longest > old % kv.page_size) late = last;
             }
             p.from[i] = from;
+            p.late[i] = late;
+            any_late = any_late || late >= 0;
             need += from >= 0;
         }
         int sum;
@@ -217,6 +225,16 @@ k_append_plan(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offset
         }
         kv.length[seqs[i]] = p.old[i] + (offsets[i + 1] - offsets[i]);
     }
+    if (__syncthreads_or(any_late)) {
+        // the sequence that keeps such a page copies it for the others before it writes there
+        for (int i = threadIdx.x; i < n; i += blockDim.x) {
+            int page = p.late[i];
+            if (p.from[i] >= 0)
+                for (int k = i + 1; k < n && page < 0; ++k)
+                    if (p.late[k] == p.from[i]) page = p.late[k];
+            if (page >= 0) p.from[i] = -2 - page;
+        }
+    }
     if (threadIdx.x == 0) {
         if (total > 0) *kv.low = p.fresh[total - 1] + 1;
         *p.go = 1;
@@ -224,7 +242,9 @@ k_append_plan(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offset
 }
 
 // Rows into their pages, 16 bytes at a time, keys and values side by side; the
-// blocks past `row_blocks` copy the pages that were shared.
+// blocks past `row_blocks` copy the pages that were shared, each sequence its own.
+// Where the one that is left with the page in place begins to write before the end
+// of what another copies (from below -1), it does both, one after the other.
 __global__ void __launch_bounds__(COPY_THREADS)
 k_append_rows(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offsets, int tokens, opattr_rows k,
               opattr_rows v, AppendPlan p, unsigned row_blocks) {
@@ -237,13 +257,28 @@ k_append_rows(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offset
         const int64_t all = (int64_t)n * kv.kv_heads, block = (int64_t)kv.page_size * per;
         for (int64_t x = blockIdx.x - row_blocks; x < all; x += gridDim.x - row_blocks) {
             const int i = (int)(x / kv.kv_heads), g = (int)(x % kv.kv_heads);
-            if (p.from[i] < 0) continue;
-            const int live = (p.old[i] % kv.page_size) * per;
-            const int64_t src = (p.from[i] * (int64_t)kv.kv_heads + g) * block, dst = (p.to[i] * (int64_t)kv.kv_heads + g) * block;
-            for (int e = threadIdx.x; e < live; e += COPY_THREADS) {
-                const uint4 k4 = kp[src + e], v4 = vp[src + e];
-                kp[dst + e] = k4;
-                vp[dst + e] = v4;
+            const int from = p.from[i];
+            auto copy = [&](int entry, int page) {
+                const int live = (p.old[entry] % kv.page_size) * per;
+                const int64_t src = (page * (int64_t)kv.kv_heads + g) * block, dst = (p.to[entry] * (int64_t)kv.kv_heads + g) * block;
+                for (int e = threadIdx.x; e < live; e += COPY_THREADS) {
+                    const uint4 k4 = kp[src + e], v4 = vp[src + e];
+                    kp[dst + e] = k4;
+                    vp[dst + e] = v4;
+                }
+            };
+            if (from >= 0) copy(i, from);
+            if (from >= -1 || p.to[i] >= 0) continue;
+            const int page = -2 - from, part = p.old[i] % kv.page_size;
+#pragma unroll 4
+            for (int e = 0; e < i; ++e)
+                if (p.from[e] == from && p.to[e] >= 0) copy(e, page);
+            __syncthreads();
+            const int rows = min(offsets[i + 1] - offsets[i], kv.page_size - part);
+            for (int e = threadIdx.x; e < rows * per; e += COPY_THREADS) {
+                const int64_t t = offsets[i] + e / per, d = 8 * (e % per), dst = (page * (int64_t)kv.kv_heads + g) * block + part * per + e;
+                kp[dst] = *reinterpret_cast<const uint4 *>((const uint16_t *)k.data + t * k.token_stride + g * k.head_stride + d);
+                vp[dst] = *reinterpret_cast<const uint4 *>((const uint16_t *)v.data + t * v.token_stride + g * v.head_stride + d);
             }
         }
         return;
@@ -273,6 +308,7 @@ k_append_rows(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offset
                 const int i = seq_of_row(offsets, n, (int)t), pos = p.old[i] + (int)t - offsets[i];
                 const int page = kv.table[(int64_t)seqs[i] * kv.pages_per_seq + pos / kv.page_size];
                 if (page < 0 || page >= kv.n_pages) continue;     // a table that was not consistent before the call
+                if (pos - pos % kv.page_size < p.old[i] && p.from[i] < -1 && p.to[i] < 0) continue;
                 const int64_t dst = ((page * (int64_t)kv.kv_heads + g) * kv.page_size + pos % kv.page_size) * per + e;
                 kp[dst] = k4[q];
                 vp[dst] = v4[q];
@@ -297,7 +333,7 @@ opattr_status do_cache_append(Ctx &c, Serve &s, const opattr_cache *kv, const in
     if ((st = serve_ready(c, s, 0))) return st;
     // at most: a page copied and one begun by each sequence, and the full ones
     const int64_t most = std::min<int64_t>(kv->n_pages, 2ll * n + tokens / kv->page_size);
-    if ((st = ensure_arena(c, Need().add<int32_t>(1).add<int32_t>(n).add<int32_t>(n).add<int32_t>(n).add<int32_t>(n + 1)
+    if ((st = ensure_arena(c, Need().add<int32_t>(1).add<int32_t>(n).add<int32_t>(n).add<int32_t>(n).add<int32_t>(n).add<int32_t>(n + 1)
                                   .add<int32_t>(kv->n_seqs).add<int32_t>(most).bytes)))
         return st;
     Arena a(c);
@@ -306,6 +342,7 @@ opattr_status do_cache_append(Ctx &c, Serve &s, const opattr_cache *kv, const in
     p.old = a.take<int32_t>(n);
     p.from = a.take<int32_t>(n);
     p.to = a.take<int32_t>(n);
+    p.late = a.take<int32_t>(n);
     p.first = a.take<int32_t>(n + 1);
     p.mark = a.take<int32_t>(kv->n_seqs);
     p.fresh = a.take<int32_t>(most);

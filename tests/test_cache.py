@@ -293,3 +293,35 @@ def test_shared_page_without_room_for_its_copy(opa, ctx):
         ctx.check()
     assert e.value.status == opa.E_PAGES
     assert c.refs.tolist() == [2, 2] and c.length.tolist() == [20, 0, 20]
+
+
+@pytest.mark.parametrize("page,heads,dim,n", [(16, 1, 8, 5), (128, 3, 128, 40), (64, 2, 40, 2), (16, 1, 8, 2600)])
+def test_sharers_of_unlike_lengths(ctx, page, heads, dim, n):
+    """Sequences share pages and go on from unlike places in them, all in one call.
+    The last one keeps the page and writes over what the others take along."""
+    per = 3
+    c = ctx.cache(n + 2 * n + 8, page, heads, dim, n, per)
+    m = Model(n + 2 * n + 8, page, n, per)
+    first = list(range(1, 2 * page))
+    k, v = rows(first, heads, dim, torch.bfloat16)
+    ctx.cache_append(c, i32([0]), i32([0, len(first)]), k, v)
+    m.append([0], [len(first)], first)
+    others = list(range(1, n))
+    ctx.cache_fork(c, i32([0] * (n - 1)), i32(others))
+    m.fork([0] * (n - 1), others)
+    lengths = [page + 1 + (page - 2) * (n - 1 - s) // (n - 1) for s in range(n)]      # the last is the shortest
+    ctx.cache_trim(c, i32(list(range(n))), i32(lengths))
+    m.trim(list(range(n)), lengths)
+    counts = [min(page + 3, per * page - x) for x in lengths]
+    if n > 1000:
+        counts = [1 + s % 3 if s < n - 1 else page + 3 for s in range(n)]
+    ids = [i % 251 + 1 for i in range(sum(counts))]
+    off = [0]
+    for x in counts:
+        off.append(off[-1] + x)
+    k, v = rows(ids, heads, dim, torch.bfloat16)
+    ctx.cache_append(c, i32(list(range(n))), i32(off), k, v)
+    m.append(list(range(n)), counts, ids)
+    ctx.check()
+    assert m.refs[c.table[n - 1].tolist()[1]] == 1
+    same(c, m)
