@@ -8,6 +8,13 @@
 // otherwise the call changes nothing and opattr_check reports it.  What a call
 // does is defined without reference to the order in which threads run: pages
 // are given out from the lowest free one on, sequence after sequence.
+//
+// There is nothing to compute: large calls are bound by the rows' way through memory, small
+// ones by a launch (about 2.5 us each) and a plan's chain of dependent loads.  Measured on one
+// GB300 (400 sequences of 200 .. 3,100 tokens in pages of 32, 8 heads of 128): an eighth of
+// them appended anew, 55,000 tokens: 70 us, 6.4 TB/s; their freed places closed by compaction:
+// 71 us; freeing them 6, the plan of the append 10.  Of 24 sequences, each of these calls is
+// the host's 8 us.
 #include <algorithm>
 
 #include "serve.cuh"
