@@ -31,6 +31,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "tc.cuh"
@@ -75,25 +76,20 @@ struct PromptArgs {
     int q_mul, k_mul, v_mul;             // 0 where all heads read the same rows
     int wide;                            // 1: rows of the output are 32-byte aligned and DP wide
     unsigned *next;                      // items given out past each block's first; zero between launches
-    // where keys are cut, else NULL
-    const struct Piece *plan;
-    const int *n_pieces;
-    float *parts;                        // [piece][head][sub-tile] partial results, four columns of every row side by side; then the rows' maxima and sums
-    uint32_t *tickets;                   // [place][head][sub-tile] arrivals
+    // where blocks have equal runs of keys, else NULL
+    const struct Item *plan;             // a block's items after those of the block before
+    const int *start;                    // [grid + 1] where they begin
+    float *parts;                        // [block][2][sub-tile] partial results, four columns of every row side by side; then the rows' maxima and sums
+    uint32_t *tickets;                   // [block][sub-tile] arrivals
 };
 
 // A work item: two sub-tiles of queries of one sequence, and keys of it.
 struct Item {
     int q0, lq, k0, lk;                  // the sequence's queries; the keys taken here
-    int t0, head0, hx;                   // first query within it, (first) head, and its place among heads_x
+    int t0, head0;                       // first query within it, and (first) head
     int ahead;                           // query i sees the keys up to i + ahead
-    int place, first, piece, pieces;     // its query tile; the tile's first piece, which of them this is, and how many there are
+    int first, piece, pieces;            // the first block that has some of its keys, which part this is, and how many there are
     int some;                            // 0: there are no more
-};
-
-// Pieces of keys of a query tile, as the plan lists them.
-struct Piece {
-    int q0, lq, k0, lk, t0, ahead, place, first, piece, pieces;
 };
 
 struct Ctrl {
@@ -387,12 +383,13 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                 if (lane_id() == 0) bar_arrive(smem_addr(&ctl.o_free[s]));
             };
             constexpr int PART = ROWS * (DP + 2);
-            const long long stride = (long long)p.heads_x * 2 * PART;
+            // a block's part of the item that it ends with is its second, of the one it begins with its first
+            auto part_at = [&](int k) { return parts + ((long long)k * 2 + (k == 0)) * 2 * PART; };
             if (seldom(it.pieces > 1)) {
                 // a part of the keys: the result so far goes to memory, and whoever brings the
                 // last part of the tile puts them together, in order
-                parts = p.parts + ((long long)it.first * p.heads_x + it.hx) * 2 * PART + s * PART;
-                float *part = const_cast<float *>(parts) + it.piece * stride;
+                parts = p.parts + (long long)it.first * 4 * PART + s * PART;
+                float *part = const_cast<float *>(part_at(it.piece));
 #pragma unroll 1
                 for (int d = 0; d < DP; d += 32) {
                     uint32_t o[32] = {};
@@ -411,7 +408,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                 __threadfence();
                 group_sync(s);
                 if (r == 0) {
-                    uint32_t *t = p.tickets + ((long long)it.place * p.heads_x + it.hx) * 2 + s;
+                    uint32_t *t = p.tickets + it.first * 2 + s;      // (a block ends with one item at most)
                     const bool all = atomicAdd(t, 1u) == (unsigned)it.pieces - 1;
                     if (all) atomicExch(t, 0u);
                     ctl.last[s] = all;
@@ -421,10 +418,13 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                 if (joined) {
                     __threadfence();
                     ref = -INFINITY;
-                    for (int k = 0; live && k < it.pieces; ++k) ref = fmaxf(ref, __ldcg(parts + k * stride + ROWS * DP + 2 * r));
+#pragma unroll 4
+                    for (int k = 0; k < it.pieces; ++k)
+                        if (live) ref = fmaxf(ref, __ldcg(part_at(k) + ROWS * DP + 2 * r));
                     l = 0.f;
-                    for (int k = 0; live && k < it.pieces; ++k) {
-                        const float2 y = __ldcg(reinterpret_cast<const float2 *>(parts + k * stride + ROWS * DP + 2 * r));
+#pragma unroll 4
+                    for (int k = 0; k < it.pieces; ++k) {
+                        const float2 y = live ? __ldcg(reinterpret_cast<const float2 *>(part_at(k) + ROWS * DP + 2 * r)) : make_float2(ref, 0.f);
                         l = __fmaf_rn(y.y, y.x == ref ? 1.f : exp2_fast(y.x - ref), l);
                     }
                 }
@@ -437,7 +437,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                 if (joined && live) {
 #pragma unroll 4
                     for (int k = 0; k < it.pieces; ++k) {
-                        const float *part = parts + k * stride;
+                        const float *part = part_at(k);
                         const float y = __ldcg(part + ROWS * DP + 2 * r), f = y == ref ? 1.f : exp2_fast(y - ref);
 #pragma unroll
                         for (int e = 0; e < 32; e += 4) {
@@ -702,23 +702,20 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                 mine = (int)lane_id() < a.n_seqs && good() ? (vq1 - vq0 + per - 1) / per : 0;
                 upto = warp_inclusive_scan(mine);
                 tiles = min(tiles, __shfl_sync(0xffffffffu, upto, 31));
-            } else if (p.plan) {
-                tiles = *p.n_pieces;
             }
-            const unsigned heads_x = p.heads_x, total = heads_x * (unsigned)tiles;
+            const unsigned heads_x = p.heads_x, total = p.plan ? (unsigned)p.start[blockIdx.x + 1] : heads_x * (unsigned)tiles;
             const bool none = uniform(gave_up) != 0;
             Place<1> wanted;
-            unsigned i = blockIdx.x;
+            unsigned i = p.plan ? (unsigned)p.start[blockIdx.x] : blockIdx.x;
             for (bool more = true; more;) {
                 Item it{};
                 while (i < total && !none) {
-                    const unsigned back = i / heads_x;
-                    const int hx = (int)(i - back * heads_x), head0 = hx * p.pack;
                     if (p.plan) {
-                        const Piece y = p.plan[back];
-                        it = Item{y.q0, y.lq, y.k0, y.lk, y.t0, head0, hx, y.ahead, y.place, y.first, y.piece, y.pieces, 1};
+                        it = p.plan[i];
                         break;
                     }
+                    const unsigned back = i / heads_x;
+                    const int head0 = (int)(i - back * heads_x) * p.pack;
                     const int x = tiles - 1 - (int)back;
                     int k, t0;
                     if (few) {
@@ -742,7 +739,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                     const int q0 = __shfl_sync(0xffffffffu, vq0, k), lq = __shfl_sync(0xffffffffu, vq1, k) - q0;
                     const int k0 = __shfl_sync(0xffffffffu, vk0, k), lk = __shfl_sync(0xffffffffu, vk1, k) - k0;
                     if (__shfl_sync(0xffffffffu, (int)good(), k) && t0 >= 0 && t0 < lq) {
-                        it = Item{q0, lq, k0, lk, t0, head0, hx, lk - lq, 0, 0, 0, 1, 1};
+                        it = Item{q0, lq, k0, lk, t0, head0, lk - lq, 0, 0, 1, 1};
                         break;
                     }
                     i = draw(p.next, total);
@@ -757,7 +754,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                 if (more) {
                     if (!warp_wait(smem_addr(&ctl.item_want), wanted.ph, stop)) break;
                     wanted.step();
-                    i = draw(p.next, total);
+                    i = p.plan ? i + 1 : draw(p.next, total);
                 }
             }
             if (blockIdx.x == 0) {
@@ -776,56 +773,89 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
     if (warp == MMA_WARP) tm_free(ctl.tmem, 512);
 }
 
-// ---------------------------------------------------------------- the plan where keys are cut
-// Few query tiles with many keys would leave SMs idle: then each tile's keys are cut
-// into pieces of about half of what an SM has to do (PIECE_TILES at least, and no
-// more than PIECES_PER_TILE to a tile: a piece costs a way to memory and back of 128 x
-// DP sums; a quarter was slower throughout).  One block; there are few tiles.
-constexpr int PIECE_TILES = 8, PIECES_PER_SM = 2, PIECES_PER_TILE = 32;
+// ---------------------------------------------------------------- the plan of equal runs
+// All items' key tiles are laid end to end, an item's after ITEM_COST places for what it
+// costs to begin and to end it, and cut into equal runs, one per block, of at least the
+// square root of the longest item's tiles (a part that has to be joined costs about what
+// a tile does).  One block.
+constexpr int PLACES = 2048, ITEM_COST = 2;
 
-__global__ void __launch_bounds__(1024) k_prompt_plan(PromptArgs p, int sms, Piece *plan, int *n_pieces) {
-    __shared__ int warp_buf[33];
+__global__ void __launch_bounds__(1024) k_prompt_plan(PromptArgs p, int blocks, Item *plan, int *start) {
+    __shared__ long long at[PLACES + 1];                 // where a place's items begin
     __shared__ long long wide_buf[33];
+    __shared__ int seq_of[PLACES], warp_buf[33], longest;
     pdl_wait();
     const opattr_prompt &a = p.a;
     const int per = 2 * p.span;
-    Item it{};
-    auto look = [&](int x) {                             // key tiles of place x; 0: it has no queries
-        const int b = [&] {
-            int lo = 0, hi = a.n_seqs;
-            while (hi - lo > 1) {
+    auto item_of = [&](int x, int b) {                   // of place x, which is sequence b's
+        const int q0 = a.q_offsets[b], q1 = a.q_offsets[b + 1], k0 = a.k_offsets[b], k1 = a.k_offsets[b + 1];
+        const int t0 = (x - q0 / per - b) * per;
+        if (q0 < 0 || q1 < q0 || q1 > a.q_tokens || k0 < 0 || k1 < k0 || k1 > a.k_tokens || t0 < 0 || t0 >= q1 - q0) return Item{};
+        return Item{q0, q1 - q0, k0, k1 - k0, t0, 0, (k1 - k0) - (q1 - q0), 0, 0, 1, 1};
+    };
+    if (threadIdx.x == 0) longest = 0;
+    long long total = 0;
+    for (int x0 = 0; x0 < p.tiles; x0 += 1024) {
+        const int x = x0 + (int)threadIdx.x;
+        int n = 0, lo = 0;
+        if (x < p.tiles) {
+            for (int hi = a.n_seqs; hi - lo > 1;) {
                 const int mid = (lo + hi) >> 1;
                 if (a.q_offsets[mid] / per + mid <= x) lo = mid;
                 else hi = mid;
             }
-            return lo;
-        }();
-        const int q0 = a.q_offsets[b], q1 = a.q_offsets[b + 1], k0 = a.k_offsets[b], k1 = a.k_offsets[b + 1];
-        const int t0 = (x - q0 / per - b) * per;
-        if (q0 < 0 || q1 < q0 || q1 > a.q_tokens || k0 < 0 || k1 < k0 || k1 > a.k_tokens || t0 < 0 || t0 >= q1 - q0) return 0;
-        it = Item{q0, q1 - q0, k0, k1 - k0, t0, 0, 0, (k1 - k0) - (q1 - q0), x, 0, 0, 1, 1};
-        return max(1, Work(it, p.span, a.causal).n);
-    };
-    long long all = 0;
-    for (int x = threadIdx.x; x < p.tiles; x += 1024) all += look(x);
-    all = block_sum(all, wide_buf);
-    const int most = (int)max((long long)PIECE_TILES, (all * p.heads_x + PIECES_PER_SM * sms - 1) / (PIECES_PER_SM * sms));
-    int at = 0;
-    for (int x0 = 0; x0 < p.tiles; x0 += 1024) {
-        // (as the items without a plan: from the last place to the first)
-        const int x = p.tiles - 1 - (x0 + (int)threadIdx.x);
-        const int n = x >= 0 ? look(x) : 0, pieces = min(PIECES_PER_TILE, (n + most - 1) / most);
-        int sum;
-        const int first = at + block_exclusive_scan(pieces, warp_buf, &sum);
-        for (int k = 0; k < pieces; ++k) {
-            const int j0 = (int)((long long)n * k / pieces), j1 = (int)((long long)n * (k + 1) / pieces);
-            // the last piece has what is left of the keys, and with them the masks
-            const int k1 = k + 1 == pieces ? it.lk : min(it.lk, j1 * KEYS);
-            plan[first + k] = Piece{it.q0, it.lq, it.k0 + j0 * KEYS, k1 - j0 * KEYS, it.t0, it.ahead - j0 * KEYS, x, first, k, pieces};
+            const Item it = item_of(x, lo);
+            if (it.some) n = max(1, Work(it, p.span, a.causal).n);
         }
-        at += sum;
+        long long sum;
+        const long long before = block_exclusive_scan(n ? (long long)(n + ITEM_COST) * p.heads_x : 0ll, wide_buf, &sum);
+        if (x < p.tiles) at[x] = total + before, seq_of[x] = lo;
+        total += sum;
+        n = __reduce_max_sync(0xffffffffu, n);
+        if (lane_id() == 0) atomicMax(&longest, n);
     }
-    if (threadIdx.x == 0) *n_pieces = at;
+    if (threadIdx.x == 0) at[p.tiles] = total;
+    __syncthreads();
+    const long long runs = min((long long)blocks, total / (ITEM_COST + (int)ceilf(sqrtf((float)longest))));
+    const long long S = max(1ll, runs), b = threadIdx.x;
+    // every part of run b, in order: its place, head, first step of the item, and from and to of its tiles
+    auto walk = [&](auto &&part) {
+        if (b >= S || total == 0) return;
+        const long long s0 = b * total / S, s1 = (b + 1) * total / S;
+        int x = 0;
+        for (int hi = p.tiles; hi - x > 1;) {            // (the last place that begins there has items)
+            const int mid = (x + hi) >> 1;
+            if (at[mid] <= s0) x = mid;
+            else hi = mid;
+        }
+        int cost = (int)((at[x + 1] - at[x]) / p.heads_x), hx = (int)((s0 - at[x]) / cost);
+        for (long long item = at[x] + (long long)hx * cost; item < s1; item += cost, ++hx) {
+            if (hx == p.heads_x) {
+                hx = 0;
+                while (at[++x + 1] == item);             // (s1 is no more than the total: there is one)
+                cost = (int)((at[x + 1] - at[x]) / p.heads_x);
+            }
+            const long long first = item + ITEM_COST;
+            const int n = cost - ITEM_COST, from = (int)max(0ll, s0 - first), to = (int)min((long long)n, s1 - first);
+            if (from < to) part(x, hx, first, n, from, to);
+        }
+    };
+    int mine = 0, sum;
+    walk([&](int, int, long long, int, int, int) { ++mine; });
+    int place = block_exclusive_scan(mine, warp_buf, &sum);
+    if (b < blocks) start[b] = place;
+    if (b == 0) start[blocks] = sum;
+    walk([&](int x, int hx, long long first, int n, int from, int to) {
+        Item it = item_of(x, seq_of[x]);
+        const int block1 = (int)(((first + 1) * S - 1) / total), block2 = (int)(((first + n) * S - 1) / total);
+        it.head0 = hx * p.pack;
+        it.k0 += from * KEYS;
+        // the last part has what is left of the keys, and with them the masks
+        it.lk = (to == n ? it.lk : to * KEYS) - from * KEYS;
+        it.ahead -= from * KEYS;
+        it.first = block1, it.piece = (int)b - block1, it.pieces = block2 - block1 + 1;
+        plan[place++] = it;
+    });
 }
 
 // ---------------------------------------------------------------- host
@@ -861,26 +891,34 @@ static bool row_map(CUtensorMap *m, int dtype, const opattr_rows &r, int64_t tok
 template <typename T, int DP, int DV>
 static opattr_status run_prompt(Ctx &c, Serve &s, PromptArgs &p, const CUtensorMap *m) {
     using S = Shape<DP>;
+    const opattr_prompt &a = p.a;
     const int64_t items = (int64_t)p.heads_x * p.tiles;
     const int sms = sm_count(c);
-    // Keys are cut where there are no more items than SMs and 2,048 keys to a sequence
-    // (uncut, then cut, us: 1 query over 100,000 keys, 8 heads of 128: 945, 119; 512 over
-    // 8,192, 32 heads: 102, 89; 4,096 over as many, 8 heads: 56, 55; with more items than
-    // that, 8,192 causal, 8 heads: 103, 128)
-    if (items <= sms && p.a.k_tokens / p.a.n_seqs >= 2048) {
-        const int64_t most = p.tiles + ((int64_t)PIECES_PER_SM * sms + p.heads_x - 1) / p.heads_x + 1;
-        const int64_t parts = most * p.heads_x * 2 * ROWS * (DP + 2);
-        opattr_status st = serve_ready(c, s, 2 * items);
+    // Equal runs of keys where whole items would leave SMs idle for longer than 14 tiles take,
+    // which is what a plan and joined parts cost.  What whole items take, in key tiles: the
+    // longest where each SM has one at most, else an SM's share and what the last round leaves idle
+    // (of the least item: causal prompts' items come longest first, so that the last ones are short).
+    // Whole items, then runs, us: 1 query over 100,000 keys, 8 heads of 128: 926, 100; 4 over
+    // 20,000 for each of 20, 32 heads on 8: 413, 266; 512 over 8,192: 107, 67; 4,096 causal, 8 heads:
+    // 58, 49; and on the other side 4,096 not causal: 58, 69; 8,192 causal: 108, 121; 64 x 512, 8
+    // heads of 64: 54, 79.
+    const double per = 2. * p.span, q_each = (double)a.q_tokens / a.n_seqs, keys = (double)a.k_tokens / a.n_seqs / KEYS;
+    const double queries = a.causal ? std::min(q_each / KEYS, keys) : 0., mean = keys - queries / 2, least = keys - queries;
+    const double each = std::max(1., q_each / per + .5) * a.n_seqs * p.heads_x / sms;        // items of an SM
+    const double whole = each <= 1 ? keys : std::max(keys, each * mean + (std::ceil(each) - each) * least);
+    if (p.tiles <= PLACES && whole > each * mean + 14) {
+        const int64_t parts = (int64_t)sms * 4 * ROWS * (DP + 2), most = items + sms;
+        opattr_status st = serve_ready(c, s, 2 * sms);
         if (st) return st;
-        if ((st = ensure_arena(c, Need().add<int>(1).add<Piece>(most).add<float>(parts).bytes))) return st;
+        if ((st = ensure_arena(c, Need().add<int>(sms + 1).add<Item>(most).add<float>(parts).bytes))) return st;
         Arena ar(c);
-        int *n = ar.take<int>(1);
-        Piece *plan = ar.take<Piece>(most);
-        p.n_pieces = n;
+        int *start = ar.take<int>(sms + 1);
+        Item *plan = ar.take<Item>(most);
+        p.start = start;
         p.plan = plan;
         p.parts = ar.take<float>(parts);
         p.tickets = s.tickets;
-        launch(c, "prompt_plan", k_prompt_plan, dim3(1), dim3(1024), 0, p, sms, plan, n);
+        launch(c, "prompt_plan", k_prompt_plan, dim3(1), dim3(1024), 0, p, sms, plan, start);
     }
     constexpr unsigned bit = 1u << ((std::is_same<T, __half>::value ? 3 : 0) + (DP == 64 ? 0 : DV == 96 ? 1 : 2));
     if (!(s.prompt_room & bit)) {

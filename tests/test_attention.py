@@ -118,6 +118,33 @@ def test_prompt_few_queries_many_keys(ctx, dtype, dim, heads, kv, causal, lq, lk
     assert torch.equal(check_prompt(ctx, q, k, v, lq, lk, causal)[0], first)
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype,dim,heads,kv,seqs,queries,keys", [(BF, 64, 8, 1, 40, 30, 6000), (HF, 128, 6, 3, 3, 400, 9000),
+                                                                  (BF, 80, 7, 1, 70, 3, 9000), (BF, 128, 2, 2, 1, 900, 7000)])
+def test_prompt_equal_runs(ctx, causal, dtype, dim, heads, kv, seqs, queries, keys):
+    """Runs of keys that hold several items and parts of some, beside sequences without
+    queries or keys; then with a value that one query sees alone and that is not finite."""
+    g = gen(seqs * 7 + dim)
+    rnd = torch.Generator().manual_seed(seqs)
+    lq = [int(x) for x in torch.randint(0 if seqs > 1 else queries, queries + 1, (seqs,), generator=rnd)]
+    lk = [int(x) for x in torch.randint(keys // 2 if seqs < 5 else 0, keys + 1, (seqs,), generator=rnd)]
+    if seqs > 5:
+        lk[3], lq[5] = 0, 0
+    q = randn(g, (sum(lq), heads, dim), dtype)
+    k, v = (randn(g, (sum(lk), kv, dim), dtype) for _ in range(2))
+    first, _ = check_prompt(ctx, q, k, v, lq, lk, causal)
+    assert torch.equal(check_prompt(ctx, q, k, v, lq, lk, causal)[0], first)
+    n, m = lq[-1], lk[-1]
+    if causal and n > 1 and m > 1:
+        want, _, lim, _ = attend(q[-n:], k[-m:], v[-m:], dim ** -0.5, causal_mask(n, m, DEV))
+        v[-1] = math.inf
+        out = ctx.attention(q, k, v, offsets(lq), offsets(lk))[1]
+        ctx.check()
+        assert torch.equal(out[:-n], first[:-n])
+        assert_within(out[-n:-1], want[:-1], lim[:-1], "rows that do not see it")
+        assert not torch.isfinite(out[-1]).any()
+
+
 def test_prompt_rising_scores(ctx):
     """Scores that rise along the keys: the running maximum moves at every tile,
     by more and by less than what the accumulator is rescaled for."""
