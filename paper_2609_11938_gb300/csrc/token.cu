@@ -37,10 +37,14 @@ namespace opattr {
 bool cache_ok(const opattr_cache *k);
 
 constexpr int TOKEN_WARPS = 4, TOKEN_THREADS = 32 * TOKEN_WARPS;
-// A cut costs a join, about 3 us where nothing else is to be done meanwhile; a step
-// of a block by itself 0.45 us.  So pairs of few steps are not cut, and others are
-// cut down to two steps as far as there are blocks.
+// A cut costs a join, about 3 us where nothing else is to be done meanwhile and 0.13 us a
+// part; a step of a block by itself 0.5 to 1 us.  So pairs of few steps are not cut, and others
+// as far as there are blocks, but to no less than two steps a part, nor so far that a longer
+// join takes what shorter parts give (of c steps in x parts, c / x + 0.13 x is least where
+// x is the root of 8 c; 12 measured best): 60,000 tokens, 8 heads of 128 on one: 68 us in parts
+// of two steps, 29 of nine.
 constexpr int UNCUT_STEPS = 8, MIN_STEPS = 2;
+constexpr float JOIN_STEPS = 12.f;
 
 struct TokenArgs {
     opattr_cache kv;
@@ -58,6 +62,11 @@ __device__ __forceinline__ uint4 load16(const void *p, bool on) {
     uint4 r = make_uint4(0, 0, 0, 0);
     if (on)
         asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
+    return r;
+}
+__device__ __forceinline__ float root(float x) {
+    float r;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
 template <typename T>
@@ -113,7 +122,11 @@ __global__ void __launch_bounds__(TOKEN_THREADS, NT == 1 ? 3 : 2) k_token(const 
     long long total;
     long long at = block_exclusive_scan(mine, warp_buf, &total);
     const long long pairs = (long long)p.n * units;
-    const long long W = min((long long)gridDim.x, total <= (UNCUT_STEPS + 1) * pairs ? pairs : max(1ll, total / MIN_STEPS));
+    // (in 32 bits, where no grid comes near their end: 64 took 0.3 us of every launch)
+    const int blocks = (int)gridDim.x, few = (int)min(total, 1ll << 30), few_pairs = (int)min(pairs, 1ll << 30);
+    const long long W = total <= (UNCUT_STEPS + 1) * pairs
+                            ? min(few_pairs, blocks)
+                            : min(min(few / MIN_STEPS, blocks), (int)fminf(1e6f, root(JOIN_STEPS * (float)few * (float)few_pairs)));
     if (blockIdx.x >= W) return;
     const long long s0 = blockIdx.x * total / W, s1 = (blockIdx.x + 1) * total / W;
     if (s0 >= at && s0 < at + mine) {

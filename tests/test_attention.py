@@ -406,3 +406,12 @@ def test_graph(opa):
         s.synchronize()
         assert torch.equal(got, want)
         ctx.check()
+
+
+@pytest.mark.parametrize("lens,heads,kv,dim", [([9000], 8, 1, 128), ([3000, 1, 12_000], 7, 1, 96), ([700, 700], 3, 3, 64),
+                                               ([30_000], 16, 1, 64)])
+def test_token_cuts(ctx, lens, heads, kv, dim):
+    """Few pairs cut into many parts, and parts of unlike sequences in one run."""
+    g = gen(sum(lens))
+    c, k, v = fill(g, ctx, lens, kv, dim, 16, BF)
+    check_token(ctx, c, randn(g, (len(lens), heads, dim), BF), k, v, lens)
