@@ -37,13 +37,14 @@ namespace opattr {
 bool cache_ok(const opattr_cache *k);
 
 constexpr int TOKEN_WARPS = 4, TOKEN_THREADS = 32 * TOKEN_WARPS;
-// A cut costs a join, about 3 us where nothing else is to be done meanwhile and 0.13 us a
-// part; a step of a block by itself 0.5 to 1 us.  So pairs of few steps are not cut, and others
-// as far as there are blocks, but to no less than two steps a part, nor so far that a longer
-// join takes what shorter parts give (of c steps in x parts, c / x + 0.13 x is least where
-// x is the root of 8 c; 12 measured best): 60,000 tokens, 8 heads of 128 on one: 68 us in parts
-// of two steps, 29 of nine.
-constexpr int UNCUT_STEPS = 8, MIN_STEPS = 2;
+// Pairs are cut as far as there are blocks, but not so far that a longer join takes what
+// shorter parts give: a part more costs 0.13 us to join, a step of a block by itself 0.5 to 1,
+// and c / x + 0.13 x, of c steps in x parts, is least where x is the root of 8 c (12 measured
+// best): 60,000 tokens, 8 heads of 128 on one: 68 us in parts of two steps, 29 of nine.  Pairs of
+// few steps are whole, and belong to the block that they begin in: 13 of 1 .. 596
+// tokens, 8 heads of 64 on 2: 10.7 us with every pair cut, 6.4; up to four steps 7.1, and
+// 293 of 148 .. 444, 16 heads of 128 on 4, 37.6 for 36.8.
+constexpr int WHOLE_STEPS = 3;
 constexpr float JOIN_STEPS = 12.f;
 
 struct TokenArgs {
@@ -124,9 +125,7 @@ __global__ void __launch_bounds__(TOKEN_THREADS, NT == 1 ? 3 : 2) k_token(const 
     const long long pairs = (long long)p.n * units;
     // (in 32 bits, where no grid comes near their end: 64 took 0.3 us of every launch)
     const int blocks = (int)gridDim.x, few = (int)min(total, 1ll << 30), few_pairs = (int)min(pairs, 1ll << 30);
-    const long long W = total <= (UNCUT_STEPS + 1) * pairs
-                            ? min(few_pairs, blocks)
-                            : min(min(few / MIN_STEPS, blocks), (int)fminf(1e6f, root(JOIN_STEPS * (float)few * (float)few_pairs)));
+    const long long W = min(min(few, blocks), (int)fminf(1e6f, root(JOIN_STEPS * (float)few * (float)few_pairs)));
     if (blockIdx.x >= W) return;
     const long long s0 = blockIdx.x * total / W, s1 = (blockIdx.x + 1) * total / W;
     if (s0 >= at && s0 < at + mine) {
@@ -154,8 +153,13 @@ __global__ void __launch_bounds__(TOKEN_THREADS, NT == 1 ? 3 : 2) k_token(const 
         }
         const int unit = (int)((s - base) / cost), g = unit / p.blocks_of_heads, hb = unit % p.blocks_of_heads;
         const long long unit_at = base + (long long)unit * cost + 1;   // of its first step
-        const int from = (int)max(0ll, s - unit_at), to = (int)min((long long)steps, s1 - unit_at);
-        s = unit_at + to;
+        int from = (int)max(0ll, s - unit_at), to = (int)min((long long)steps, s1 - unit_at);
+        if (steps <= WHOLE_STEPS) {
+            // a short pair is whole, and belongs to the block that it begins in
+            to = s < unit_at ? steps : from;
+            from = min(from, to);
+        }
+        s = unit_at + steps;
         if (from >= to) continue;
         const int heads = min(NQ, p.group - hb * NQ), head0 = g * p.group + hb * NQ;
         const int32_t *table = kv.table + (long long)seq * kv.pages_per_seq;
