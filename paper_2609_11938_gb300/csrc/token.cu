@@ -4,11 +4,12 @@
 // The cache is read once and there is little to compute on it, so what counts is
 // that every SM has enough loads under way until the last one is done.  All
 // (sequence, key head) pairs' tokens are laid end to end and cut into equal runs,
-// one per block, whatever the lengths (a pair counts one step more than it has,
-// for what beginning and ending it costs: without that, a block whose run is of
-// many short sequences ended 25 us after the others at 64 sequences of 1 .. 16,000
-// tokens); a pair that is cut is joined by the block that finishes its part last,
-// over the parts in order (so the bits do not depend on who that is).
+// one per block, whatever the lengths (short pairs stay whole; a pair counts one
+// step more than it has, for what beginning and ending it costs: without that, a
+// block whose run is of many short sequences ended 25 us after the others at 64
+// sequences of 1 .. 16,000 tokens); a pair that is cut is joined by the block that
+// finishes its part last, over the parts in order (so the bits do not depend on who
+// that is).
 //
 // A warp takes 16 keys at a time straight from memory into the registers that
 // the products want them in, without shared memory: the products' inner
@@ -23,7 +24,7 @@
 // over the time of a call among others): 2 sequences of 260,000 tokens, 40 heads of 128
 // on 8: 316 us, 6.8 TB/s; 64 of 1 .. 16,001, 32 heads on 8: 67.7 us, 6.0, where the
 // beginning and the end of the one launch, about 7 us, show; one of 700, 12 heads of 64:
-// the host's 13 us.  48 sequences that share the pages of 8 read them 48 times, from the
+// 7.7 us of the host's 12.  48 sequences that share the pages of 8 read them 48 times, from the
 // second level cache: 30 us.
 #include <math.h>
 
