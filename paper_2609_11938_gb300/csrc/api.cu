@@ -684,8 +684,7 @@ opattr_status opattr_check(opattr_ctx *ctx) {
     if (e == cudaSuccess) e = cudaStreamSynchronize(c.stream);
     if (e == cudaSuccess && v.err && (found = c.h_small[0]) & SERVE_TIMEOUT) {
         // a launch that gave up leaves its counts as they were
-        e = cudaMemsetAsync(v.err, 0, 256, c.stream);
-        if (e == cudaSuccess) e = cudaMemsetAsync(v.tickets, 0, sizeof(uint32_t) * v.n_tickets, c.stream);
+        e = cudaMemsetAsync(v.err, 0, 256 + sizeof(uint32_t) * TICKETS, c.stream);
         if (e == cudaSuccess) e = cudaStreamSynchronize(c.stream);
     }
     if (e != cudaSuccess || c.last_error != cudaSuccess) return finish(c, cuda_status(c, e));

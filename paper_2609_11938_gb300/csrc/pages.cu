@@ -26,7 +26,6 @@ constexpr int COPY_THREADS = 256;
 // tokens whose pieces a thread has under way (four, with half the threads, took 97 us for
 // 55,000 tokens of 8 heads of 128, two 70)
 constexpr int ROWS_AHEAD = 2;
-constexpr int FIRST_TICKETS = 4096;
 
 bool cache_ok(const opattr_cache *k) {
     if (k->dtype != OPATTR_BF16 && k->dtype != OPATTR_F16) return false;
@@ -38,48 +37,23 @@ bool cache_ok(const opattr_cache *k) {
     return ((reinterpret_cast<uintptr_t>(k->k_pages) | reinterpret_cast<uintptr_t>(k->v_pages)) & 15) == 0;
 }
 
-opattr_status serve_ready(Ctx &c, Serve &s, int64_t tickets) {
-    if (!s.err) {
-        // with the first tickets behind it
-        cudaError_t e = cudaMalloc(&s.err, 256 + sizeof(uint32_t) * FIRST_TICKETS);
-        if (e == cudaErrorMemoryAllocation) {
-            cudaGetLastError();
-            s.err = nullptr;
-            return OPATTR_E_OOM;
-        }
-        if (e == cudaSuccess) e = cudaMemsetAsync(s.err, 0, 256 + sizeof(uint32_t) * FIRST_TICKETS, c.stream);
-        if (e != cudaSuccess) return cuda_status(c, e);
-        s.tickets = s.err + 64;
-        s.n_tickets = FIRST_TICKETS;
+opattr_status serve_ready(Ctx &c, Serve &s) {
+    if (s.err) return OPATTR_OK;
+    const size_t bytes = 256 + sizeof(uint32_t) * TICKETS;
+    cudaError_t e = cudaMalloc(&s.err, bytes);
+    if (e == cudaErrorMemoryAllocation) {
+        cudaGetLastError();
+        s.err = nullptr;
+        return OPATTR_E_OOM;
     }
-    if (tickets > s.n_tickets) {
-        // launches before this one may still count in the old tickets
-        if (s.more) {
-            const cudaError_t e = cudaStreamSynchronize(c.stream);
-            if (e != cudaSuccess) return cuda_status(c, e);
-            cudaFree(s.more);
-        }
-        s.more = nullptr;
-        s.tickets = s.err + 64;
-        s.n_tickets = FIRST_TICKETS;
-        const int64_t n = 2 * tickets;
-        cudaError_t e = cudaMalloc(&s.more, sizeof(uint32_t) * n);
-        if (e == cudaErrorMemoryAllocation) {
-            cudaGetLastError();
-            s.more = nullptr;
-            return OPATTR_E_OOM;
-        }
-        if (e == cudaSuccess) e = cudaMemsetAsync(s.more, 0, sizeof(uint32_t) * n, c.stream);
-        if (e != cudaSuccess) return cuda_status(c, e);
-        s.tickets = s.more;
-        s.n_tickets = n;
-    }
-    return OPATTR_OK;
+    if (e != cudaSuccess) return cuda_status(c, e);
+    s.tickets = s.err + 64;
+    e = cudaMemsetAsync(s.err, 0, bytes, c.stream);
+    return e == cudaSuccess ? OPATTR_OK : cuda_status(c, e);
 }
 
 void serve_free(Serve &s) {
     if (s.err) cudaFree(s.err);
-    if (s.more) cudaFree(s.more);
     s = Serve{};
 }
 
@@ -337,7 +311,7 @@ opattr_status do_cache_append(Ctx &c, Serve &s, const opattr_cache *kv, const in
     if (!rows_ok(*k, tokens, kv->kv_heads, kv->head_dim) || !rows_ok(*v, tokens, kv->kv_heads, kv->head_dim))
         return OPATTR_E_INVALID_ARG;
     if (n == 0) return OPATTR_OK;
-    if ((st = serve_ready(c, s, 0))) return st;
+    if ((st = serve_ready(c, s))) return st;
     // at most: a page copied and one begun by each sequence, and the full ones
     const int64_t most = std::min<int64_t>(kv->n_pages, 2ll * n + tokens / kv->page_size);
     if ((st = ensure_arena(c, Need().add<int32_t>(1).add<int32_t>(n).add<int32_t>(n).add<int32_t>(n).add<int32_t>(n).add<int32_t>(n + 1)
@@ -410,7 +384,7 @@ opattr_status do_cache_fork(Ctx &c, Serve &s, const opattr_cache *kv, const int3
     opattr_status st = seqs_ok(kv, dst, n);
     if (st || n == 0) return st;
     if (!src) return OPATTR_E_INVALID_ARG;
-    if ((st = serve_ready(c, s, 0))) return st;
+    if ((st = serve_ready(c, s))) return st;
     if ((st = ensure_arena(c, Need().add<int32_t>(1).add<int32_t>(kv->n_seqs).bytes))) return st;
     Arena a(c);
     int32_t *go = a.take<int32_t>(1), *mark = a.take<int32_t>(kv->n_seqs);
@@ -469,7 +443,7 @@ opattr_status do_cache_trim(Ctx &c, Serve &s, const opattr_cache *kv, const int3
                             int32_t n) {
     opattr_status st = seqs_ok(kv, seqs, n);
     if (st || n == 0) return st;
-    if ((st = serve_ready(c, s, 0))) return st;
+    if ((st = serve_ready(c, s))) return st;
     if ((st = ensure_arena(c, Need().add<int32_t>(1).add<int32_t>(n).add<int32_t>(kv->n_seqs).bytes))) return st;
     Arena a(c);
     int32_t *go = a.take<int32_t>(1), *old = a.take<int32_t>(n), *mark = a.take<int32_t>(kv->n_seqs);
@@ -587,7 +561,7 @@ k_compact_move(opattr_cache kv, const int32_t *rank, const int32_t *hole, const 
 
 opattr_status do_cache_compact(Ctx &c, Serve &s, const opattr_cache *kv, int32_t *live) {
     if (!cache_ok(kv)) return OPATTR_E_INVALID_ARG;
-    opattr_status st = serve_ready(c, s, 0);
+    opattr_status st = serve_ready(c, s);
     if (st) return st;
     const int tiles = (int)((kv->n_pages + TILE_PAGES - 1) / TILE_PAGES);
     if ((st = ensure_arena(c, Need().add<int32_t>(2).add<int32_t>(tiles).add<int32_t>(kv->n_pages).add<int32_t>(kv->n_pages)

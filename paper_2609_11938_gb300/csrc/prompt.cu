@@ -908,9 +908,8 @@ static opattr_status run_prompt(Ctx &c, Serve &s, PromptArgs &p, const CUtensorM
     const double whole = each <= 1 ? keys : std::max(keys, each * mean + (std::ceil(each) - each) * least);
     if (p.tiles <= PLACES && whole > each * mean + 14) {
         const int64_t parts = (int64_t)sms * 4 * ROWS * (DP + 2), most = items + sms;
-        opattr_status st = serve_ready(c, s, 2 * sms);
+        const opattr_status st = ensure_arena(c, Need().add<int>(sms + 1).add<Item>(most).add<float>(parts).bytes);
         if (st) return st;
-        if ((st = ensure_arena(c, Need().add<int>(sms + 1).add<Item>(most).add<float>(parts).bytes))) return st;
         Arena ar(c);
         int *start = ar.take<int>(sms + 1);
         Item *plan = ar.take<Item>(most);
@@ -948,7 +947,7 @@ opattr_status do_attention(Ctx &c, Serve &s, const opattr_prompt *a) {
         return OPATTR_E_INVALID_ARG;
     if (a->q_tokens == 0) return OPATTR_OK;
     if (a->n_seqs == 0 || !a->q_offsets || !a->k_offsets) return OPATTR_E_INVALID_ARG;
-    opattr_status st = serve_ready(c, s, 0);
+    opattr_status st = serve_ready(c, s);
     if (st) return st;
     PromptArgs p{};
     p.a = *a;

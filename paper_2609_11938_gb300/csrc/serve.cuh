@@ -19,13 +19,12 @@ enum ServeErr : unsigned {
 // Device state of the context's operators, made by the first of their calls.
 struct Serve {
     unsigned *err = nullptr;         // ServeErr bits, sticky; at word 16 the prompts' count of work items drawn
-    uint32_t *tickets = nullptr;     // arrivals at each joined block of results; zero between launches
-    uint32_t *more = nullptr;        // where there are more of them than come with err
-    int64_t n_tickets = 0;
+    uint32_t *tickets = nullptr;     // arrivals at each block's cut results; zero between launches
     unsigned prompt_room = 0;        // variants of the prompt kernel that have their shared memory
 };
 
-opattr_status serve_ready(Ctx &c, Serve &s, int64_t tickets);
+constexpr int TICKETS = 4096;        // at most three blocks an SM count in them
+opattr_status serve_ready(Ctx &c, Serve &s);
 void serve_free(Serve &s);
 
 template <typename T>

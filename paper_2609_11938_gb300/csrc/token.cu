@@ -399,7 +399,7 @@ static opattr_status run_token(Ctx &c, Serve &s, TokenArgs &p) {
     const int64_t most = (int64_t)p.n * p.kv.kv_heads * p.blocks_of_heads *
                          (((int64_t)p.kv.pages_per_seq * p.kv.page_size + 16 * FR * TOKEN_WARPS - 1) / (16 * FR * TOKEN_WARPS));
     const int grid = (int)std::min<int64_t>((NT == 1 ? 3 : 2) * (int64_t)sm_count(c), most);
-    opattr_status st = serve_ready(c, s, grid);
+    opattr_status st = serve_ready(c, s);
     if (st) return st;
     const int64_t part = (int64_t)8 * NT * (DP + 2);
     if ((st = ensure_arena(c, Need().add<float>(2 * grid * part).bytes))) return st;
