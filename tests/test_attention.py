@@ -415,3 +415,58 @@ def test_token_cuts(ctx, lens, heads, kv, dim):
     g = gen(sum(lens))
     c, k, v = fill(g, ctx, lens, kv, dim, 16, BF)
     check_token(ctx, c, randn(g, (len(lens), heads, dim), BF), k, v, lens)
+
+
+def test_prompt_far_rows(ctx):
+    """Rows so far apart that their places pass 32 bits."""
+    g = gen(31)
+    n, stride = 300, 1 << 23                                   # 2.5e9 elements from the first to the last
+    x = torch.empty(n * stride, dtype=BF, device=DEV)
+    q, k, v = (x[i * 128:].as_strided((n, 2, 64), (stride, 64, 1)) for i in range(3))
+    for y in (q, k, v):
+        y.copy_(randn(g, (n, 2, 64), BF))
+    out = x[3 * 128:].as_strided((n, 2, 64), (stride, 64, 1))
+    check_prompt(ctx, q, k, v, [100, 200], None, True, out=out)
+
+
+def test_cache_past_32_bits(ctx):
+    """The last pages of a pool of more than 2^32 elements: appended to, shared, read,
+    and moved to its beginning."""
+    g = gen(32)
+    page, kv, dim = 128, 4, 128
+    n_pages = (1 << 32) // (page * kv * dim) + 40
+    c = ctx.cache(n_pages, page, kv, dim, 4, 8, BF)
+    c.refs[:n_pages - 30] = 1
+    c.low.fill_(n_pages - 30)
+    lens = [300, 900, 0, 0]
+    k, v = (randn(g, (1200, kv, dim), BF) for _ in range(2))
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    ctx.cache_append(c, i32(0, 1), i32(0, 300, 1200), k, v)
+    ctx.cache_fork(c, i32(0), i32(2))
+    more = [randn(g, (2, kv, dim), BF) for _ in range(2)]
+    ctx.cache_append(c, i32(0, 2), i32(0, 1, 2), *more)
+    assert int(c.table[c.table >= 0].min()) == n_pages - 30
+    lens = [301, 900, 301, 0]
+    rows = [torch.cat([x[:300], y[:1], x[300:], x[:300], y[1:]]) for x, y in zip((k, v), more)]
+    q = randn(g, (4, 8, dim), BF)
+    check_token(ctx, c, q, *rows, lens)
+    c.refs[:n_pages - 30] = 0
+    _, live = ctx.cache_compact(c)
+    ctx.check()
+    assert int(live) == 12 and int(c.table.max()) == 11
+    check_token(ctx, c, q, *rows, lens)
+
+
+def test_prompt_bad_offsets_of_runs(opa, ctx):
+    """As above where keys are cut into equal runs."""
+    g = gen(33)
+    q = randn(g, (20, 2, 64), BF)
+    k, v = (randn(g, (9000, 2, 64), BF) for _ in range(2))
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    for qo, ko in ((i32(0, 20), i32(0, 12_000)), (i32(0, 10, 20), i32(0, 9001, 9000)), (i32(0, 25, 20), i32(0, 10, 9000)),
+                   (i32(3, 20), i32(0, 9000)), (i32(0, -7, 20), i32(0, -2, 9000)), (i32(0, 40), i32(0, 9000))):
+        ctx.attention(q, k, v, qo, ko)
+        with pytest.raises(opa.OpattrError) as e:
+            ctx.check()
+        assert e.value.status == opa.E_INVALID_ARG
+    check_prompt(ctx, q, k, v, [20], [9000], True)
