@@ -66,16 +66,10 @@ __device__ __forceinline__ bool any_bad(bool mine, unsigned bit, unsigned *err) 
     if (bad && threadIdx.x == 0) atomicOr(err, bit);
     return bad;
 }
-// Sequences of the table, each at most once.  `mark` has a word per table row;
-// of a sequence's entries one is the last to store its index, the others see it.
-__device__ __forceinline__ bool seqs_bad(const int32_t *seqs, int n, int rows, int32_t *mark, unsigned *err) {
+// A sequence that is there twice: `mark` has a word per table row, in which a
+// sequence's entries store their index; one is the last to do so, the others see it.
+__device__ __forceinline__ bool marks_bad(const int32_t *seqs, int n, const int32_t *mark, unsigned *err) {
     bool bad = false;
-    for (int i = threadIdx.x; i < n; i += blockDim.x) {
-        const int s = seqs[i];
-        if (s < 0 || s >= rows) bad = true;
-        else mark[s] = i;
-    }
-    if (any_bad(bad, SERVE_INVALID, err)) return true;
     for (int i = threadIdx.x; i < n; i += blockDim.x) bad = bad || mark[seqs[i]] != i;
     return any_bad(bad, SERVE_INVALID, err);
 }
@@ -108,30 +102,35 @@ k_append_plan(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offset
     __shared__ uint16_t held_part[HELD];
     pdl_wait();
     if (threadIdx.x == 0) *p.go = 0;
-    if (seqs_bad(seqs, n, kv.n_seqs, p.mark, err)) return;
+    // (asked for before anything else, since the others wait on one another)
+    const int64_t low = max(0, *kv.low);
+    int early[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) early[q] = low + 4 * threadIdx.x + q < kv.n_pages ? kv.refs[low + 4 * threadIdx.x + q] : 1;
+    // each sequence's length, and the page that it is about to write into where that is filled in part
     bool bad = threadIdx.x == 0 && (offsets[0] != 0 || offsets[n] != tokens);
     for (int i = threadIdx.x; i < n; i += blockDim.x) {
-        const int more = offsets[i + 1] - offsets[i], s = seqs[i];
-        bad = bad || more < 0 || offsets[i] < 0 || length_bad(kv, s) ||
-              (int64_t)kv.length[s] + more > (int64_t)kv.pages_per_seq * kv.page_size;
-    }
-    if (any_bad(bad, SERVE_INVALID, err)) return;
-    // pages of each sequence that others hold too and that it is about to write into
-    for (int i = threadIdx.x; i < n; i += blockDim.x) {
-        const int s = seqs[i], old = kv.length[s], more = offsets[i + 1] - offsets[i];
-        int last = -1;
-        if (more > 0 && old % kv.page_size) {
-            last = kv.table[(int64_t)s * kv.pages_per_seq + old / kv.page_size];
-            if (last < 0 || last >= kv.n_pages) {
-                bad = true;
-                last = -1;
+        const int s = seqs[i], more = offsets[i + 1] - offsets[i];
+        int old = 0, last = -1, refs = 0;
+        bad = bad || more < 0 || offsets[i] < 0;
+        if (s < 0 || s >= kv.n_seqs) bad = true;
+        else {
+            p.mark[s] = i;
+            old = kv.length[s];
+            if (old < 0 || (int64_t)old + max(0, more) > (int64_t)kv.pages_per_seq * kv.page_size) bad = true;
+            else if (more > 0 && old % kv.page_size) {
+                last = kv.table[(int64_t)s * kv.pages_per_seq + old / kv.page_size];
+                if (last < 0 || last >= kv.n_pages) bad = true;
+                else refs = kv.refs[last];
             }
         }
         p.old[i] = old;
         p.to[i] = last;
+        p.from[i] = refs;
         if (i < HELD) held_page[i] = last, held_part[i] = (uint16_t)(old % kv.page_size);
     }
     if (any_bad(bad, SERVE_INVALID, err)) return;
+    if (marks_bad(seqs, n, p.mark, err)) return;
     int total = 0;
     bool any_late = false;
     for (int i0 = 0; i0 < n; i0 += blockDim.x) {
@@ -141,9 +140,10 @@ k_append_plan(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offset
             const int old = p.old[i], more = offsets[i + 1] - offsets[i], last = p.to[i];
             need = pages_for(old + more, kv.page_size) - pages_for(old, kv.page_size);
             int from = -1, late = -1;
-            if (last >= 0 && kv.refs[last] > 1) {
+            int held = p.from[i];
+            if (held > 1) {
                 // one after another: those before it have copied theirs and let go
-                int held = kv.refs[last], longest = 0;
+                int longest = 0;
                 const int near = min(i, HELD);
 #pragma unroll 8
                 for (int k = 0; k < near; ++k)
@@ -168,13 +168,12 @@ k_append_plan(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offset
     if (any_bad(total > p.room, SERVE_PAGES, err)) return;
     // the lowest `total` free pages
     int found = 0;
-    const int64_t low = max(0, *kv.low);
     for (int64_t at = low; found < total && at < kv.n_pages; at += 4 * blockDim.x) {
         const int64_t i = at + 4 * threadIdx.x;
         int r[4], mine = 0;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            r[q] = i + q < kv.n_pages ? kv.refs[i + q] : 1;
+            r[q] = at == low ? early[q] : i + q < kv.n_pages ? kv.refs[i + q] : 1;
             mine += r[q] == 0;
         }
         int sum, rank = found + block_exclusive_scan(mine, warp_buf, &sum);
@@ -298,6 +297,7 @@ k_append_rows(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offset
     }
 }
 
+// One thread to a sequence, or to four new pages; of few, a block that is quick to begin.
 static unsigned plan_threads(int64_t n) { return n <= 256 ? 256 : PLAN_THREADS; }
 static opattr_status seqs_ok(const opattr_cache *kv, const int32_t *seqs, int32_t n) {
     return cache_ok(kv) && n >= 0 && n <= kv->n_seqs && (n == 0 || seqs) ? OPATTR_OK : OPATTR_E_INVALID_ARG;
@@ -328,7 +328,7 @@ opattr_status do_cache_append(Ctx &c, Serve &s, const opattr_cache *kv, const in
     p.mark = a.take<int32_t>(kv->n_seqs);
     p.fresh = a.take<int32_t>(most);
     p.room = (int32_t)most;
-    launch(c, "append_plan", k_append_plan, dim3(1), dim3(plan_threads(n)), 0, *kv, seqs, n, offsets, (int)tokens, p, s.err);
+    launch(c, "append_plan", k_append_plan, dim3(1), dim3(plan_threads(std::max<int64_t>(n, most / 4))), 0, *kv, seqs, n, offsets, (int)tokens, p, s.err);
     const int row = kv->kv_heads * (kv->head_dim / 8);
     const unsigned rows = grid_for(tokens, std::max(1, COPY_THREADS / row), 8u * sm_count(c));
     const unsigned shared = (unsigned)std::min<int64_t>((int64_t)n * kv->kv_heads, 2 * sm_count(c));
@@ -358,15 +358,20 @@ k_fork_plan(opattr_cache kv, const int32_t *src, const int32_t *dst, int n, int3
             unsigned *err) {
     pdl_wait();
     if (threadIdx.x == 0) *go = 0;
-    if (seqs_bad(dst, n, kv.n_seqs, mark, err)) return;
     bool bad = false;
     for (int i = threadIdx.x; i < n; i += blockDim.x) {
-        const int s = src[i];
-        bad = bad || s < 0 || s >= kv.n_seqs || length_bad(kv, s) || kv.length[dst[i]] != 0;
-        if (bad) continue;
+        const int s = src[i], d = dst[i];
+        if (s < 0 || s >= kv.n_seqs || d < 0 || d >= kv.n_seqs) bad = true;
+        else {
+            mark[d] = i;
+            bad = bad || length_bad(kv, s) || kv.length[d] != 0;
+        }
+    }
+    if (any_bad(bad, SERVE_INVALID, err)) return;
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
         // a source is no destination (its mark, where it has one, names its entry in dst)
-        const int m = mark[s];
-        bad = m >= 0 && m < n && dst[m] == s;
+        const int m = mark[src[i]];
+        bad = bad || mark[dst[i]] != i || (m >= 0 && m < n && dst[m] == src[i]);
     }
     if (any_bad(bad, SERVE_INVALID, err)) return;
     if (small)
@@ -417,14 +422,19 @@ k_trim_plan(opattr_cache kv, const int32_t *seqs, const int32_t *lengths, int n,
             int32_t *go, int small, unsigned *err) {
     pdl_wait();
     if (threadIdx.x == 0) *go = 0;
-    if (seqs_bad(seqs, n, kv.n_seqs, mark, err)) return;
     bool bad = false;
     for (int i = threadIdx.x; i < n; i += blockDim.x) {
-        const int len = kv.length[seqs[i]], to = lengths ? lengths[i] : 0;
-        bad = bad || length_bad(kv, seqs[i]) || to < 0 || to > len;
-        old[i] = len;
+        const int s = seqs[i], to = lengths ? lengths[i] : 0;
+        if (s < 0 || s >= kv.n_seqs) bad = true;
+        else {
+            mark[s] = i;
+            const int len = kv.length[s];
+            bad = bad || length_bad(kv, s) || to < 0 || to > len;
+            old[i] = len;
+        }
     }
     if (any_bad(bad, SERVE_INVALID, err)) return;
+    if (marks_bad(seqs, n, mark, err)) return;
     for (int i = threadIdx.x; i < n; i += blockDim.x) kv.length[seqs[i]] = lengths ? lengths[i] : 0;
     if (small)
         for (int i = threadIdx.x >> 5; i < n; i += blockDim.x >> 5)
