@@ -493,18 +493,6 @@ k_compact_place(opattr_cache kv, const int32_t *tile_live, int tiles, int32_t *r
     __shared__ int warp_buf[33];
     pdl_wait();
     const int tile = blockIdx.x;
-    int all = 0, before = 0;
-    for (int t = threadIdx.x; tiles > 1 && t < tiles; t += blockDim.x) {
-        all += tile_live[t];
-        if (t < tile) before += tile_live[t];
-    }
-    const int L = tiles > 1 ? block_sum(all, warp_buf) : live_in(kv, 0, kv.n_pages, warp_buf);
-    before = block_sum(before, warp_buf);
-    // live pages below L
-    const int edge = tiles > 1 ? L / TILE_PAGES : 0;
-    int below = 0;
-    for (int t = threadIdx.x; t < edge; t += blockDim.x) below += tile_live[t];
-    below = block_sum(below, warp_buf) + live_in(kv, (int64_t)edge * TILE_PAGES, L, warp_buf);
     const int64_t at = (int64_t)tile * TILE_PAGES + 4 * threadIdx.x;
     int r[4], mine = 0;
 #pragma unroll
@@ -512,7 +500,24 @@ k_compact_place(opattr_cache kv, const int32_t *tile_live, int tiles, int32_t *r
         r[q] = at + q < kv.n_pages ? kv.refs[at + q] : 0;
         mine += r[q] > 0;
     }
-    int live = before + block_exclusive_scan(mine, warp_buf, (int *)nullptr);
+    int L, below = 0;                                    // live pages, and those of them below L
+    int live = block_exclusive_scan(mine, warp_buf, &L);
+    if (tiles > 1) {
+        int all = 0, before = 0;
+        for (int t = threadIdx.x; t < tiles; t += blockDim.x) {
+            all += tile_live[t];
+            if (t < tile) before += tile_live[t];
+        }
+        L = block_sum(all, warp_buf);
+        live += block_sum(before, warp_buf);
+        const int edge = L / TILE_PAGES;
+        for (int t = threadIdx.x; t < edge; t += blockDim.x) below += tile_live[t];
+        below = block_sum(below, warp_buf) + live_in(kv, (int64_t)edge * TILE_PAGES, L, warp_buf);
+    } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) below += at + q < L && r[q] > 0;
+        below = block_sum(below, warp_buf);
+    }
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         const int64_t i = at + q;
