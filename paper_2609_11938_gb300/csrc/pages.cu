@@ -339,19 +339,16 @@ opattr_status do_cache_append(Ctx &c, Serve &s, const opattr_cache *kv, const in
 
 // ---------------------------------------------------------------- fork and trim
 // The plan's block makes the change itself where the sequences' tables have few
-// entries, a warp to a sequence; a second launch costs 2.5 us.
+// entries, a thread to an entry; a second launch costs 2.5 us.  (A warp to a sequence took
+// 10 us more for 138 sequences of four pages at most.)
 constexpr int64_t SMALL_ENTRIES = 4096;
 
-// Of sequence d: the pages of s, by the threads first, first + step, ..
-__device__ __forceinline__ void fork_pages(const opattr_cache &kv, int s, int d, int first, int step) {
-    const int held = pages_for(kv.length[s], kv.page_size);
-    for (int j = first; j < held; j += step) {
-        const int page = kv.table[(int64_t)s * kv.pages_per_seq + j];
-        kv.table[(int64_t)d * kv.pages_per_seq + j] = page;
-        if (page >= 0 && page < kv.n_pages) atomicAdd(&kv.refs[page], 1);
-    }
-    // (a source is no destination here: its length stands)
-    if (first == 0 && kv.length[s] > 0) kv.length[d] = kv.length[s];
+// Page j of sequence s to sequence d; a source is no destination, its length stands.
+__device__ __forceinline__ void fork_page(const opattr_cache &kv, int s, int d, int len, int j) {
+    const int page = kv.table[(int64_t)s * kv.pages_per_seq + j];
+    kv.table[(int64_t)d * kv.pages_per_seq + j] = page;
+    if (page >= 0 && page < kv.n_pages) atomicAdd(&kv.refs[page], 1);
+    if (j == 0) kv.length[d] = len;
 }
 __global__ void __launch_bounds__(PLAN_THREADS)
 k_fork_plan(opattr_cache kv, const int32_t *src, const int32_t *dst, int n, int32_t *mark, int32_t *go, int small,
@@ -374,15 +371,21 @@ k_fork_plan(opattr_cache kv, const int32_t *src, const int32_t *dst, int n, int3
         bad = bad || mark[dst[i]] != i || (m >= 0 && m < n && dst[m] == src[i]);
     }
     if (any_bad(bad, SERVE_INVALID, err)) return;
-    if (small)
-        for (int i = threadIdx.x >> 5; i < n; i += blockDim.x >> 5) fork_pages(kv, src[i], dst[i], lane_id(), 32);
-    else if (threadIdx.x == 0) *go = 1;
+    if (small) {
+        for (int x = threadIdx.x; x < n * kv.pages_per_seq; x += blockDim.x) {
+            const int i = x / kv.pages_per_seq, j = x - i * kv.pages_per_seq, s = src[i], len = kv.length[s];
+            if (j < pages_for(len, kv.page_size)) fork_page(kv, s, dst[i], len, j);
+        }
+    } else if (threadIdx.x == 0) {
+        *go = 1;
+    }
 }
 __global__ void __launch_bounds__(COPY_THREADS)
 k_fork(opattr_cache kv, const int32_t *src, const int32_t *dst, const int32_t *go) {
     pdl_wait();
     if (*go == 0) return;
-    fork_pages(kv, src[blockIdx.x], dst[blockIdx.x], blockIdx.y * COPY_THREADS + threadIdx.x, gridDim.y * COPY_THREADS);
+    const int s = src[blockIdx.x], d = dst[blockIdx.x], len = kv.length[s], held = pages_for(len, kv.page_size);
+    for (int j = blockIdx.y * COPY_THREADS + threadIdx.x; j < held; j += gridDim.y * COPY_THREADS) fork_page(kv, s, d, len, j);
 }
 
 opattr_status do_cache_fork(Ctx &c, Serve &s, const opattr_cache *kv, const int32_t *src, const int32_t *dst, int32_t n) {
@@ -395,7 +398,7 @@ opattr_status do_cache_fork(Ctx &c, Serve &s, const opattr_cache *kv, const int3
     int32_t *go = a.take<int32_t>(1), *mark = a.take<int32_t>(kv->n_seqs);
     const int64_t entries = (int64_t)n * kv->pages_per_seq;
     const bool small = entries <= SMALL_ENTRIES;
-    launch(c, "fork_plan", k_fork_plan, dim3(1), dim3(plan_threads(small ? entries / 8 : n)), 0, *kv, src, dst, n, mark, go,
+    launch(c, "fork_plan", k_fork_plan, dim3(1), dim3(plan_threads(small ? std::max<int64_t>(n, entries / 4) : n)), 0, *kv, src, dst, n, mark, go,
            (int)small, s.err);
     if (!small)
         launch(c, "fork", k_fork, dim3(n, grid_for(kv->pages_per_seq, 4 * COPY_THREADS, 64)), dim3(COPY_THREADS), 0, *kv, src,
@@ -403,16 +406,14 @@ opattr_status do_cache_fork(Ctx &c, Serve &s, const opattr_cache *kv, const int3
     return cuda_status(c, c.last_error);
 }
 
-// The pages of sequence s from its length `to` on, of `old`.
-__device__ __forceinline__ void trim_pages(const opattr_cache &kv, int s, int old, int to, int first, int step) {
-    const int held = pages_for(old, kv.page_size), keep = pages_for(to, kv.page_size);
-    int low = INT32_MAX;
-    for (int j = keep + first; j < held; j += step) {
-        int32_t *e = &kv.table[(int64_t)s * kv.pages_per_seq + j];
-        const int page = *e;
-        *e = -1;
-        if (page >= 0 && page < kv.n_pages && atomicSub(&kv.refs[page], 1) == 1) low = min(low, page);
-    }
+// Page j of sequence s is let go; the lowest that is free now.
+__device__ __forceinline__ int trim_page(const opattr_cache &kv, int s, int j, int low) {
+    int32_t *e = &kv.table[(int64_t)s * kv.pages_per_seq + j];
+    const int page = *e;
+    *e = -1;
+    return page >= 0 && page < kv.n_pages && atomicSub(&kv.refs[page], 1) == 1 ? min(low, page) : low;
+}
+__device__ __forceinline__ void trim_low(const opattr_cache &kv, int low) {
     __syncwarp();
     low = __reduce_min_sync(0xffffffffu, low);
     if (lane_id() == 0 && low < INT32_MAX) atomicMin(kv.low, low);
@@ -436,17 +437,25 @@ k_trim_plan(opattr_cache kv, const int32_t *seqs, const int32_t *lengths, int n,
     if (any_bad(bad, SERVE_INVALID, err)) return;
     if (marks_bad(seqs, n, mark, err)) return;
     for (int i = threadIdx.x; i < n; i += blockDim.x) kv.length[seqs[i]] = lengths ? lengths[i] : 0;
-    if (small)
-        for (int i = threadIdx.x >> 5; i < n; i += blockDim.x >> 5)
-            trim_pages(kv, seqs[i], old[i], lengths ? lengths[i] : 0, lane_id(), 32);
-    else if (threadIdx.x == 0) *go = 1;
+    if (small) {
+        int low = INT32_MAX;
+        for (int x = threadIdx.x; x < n * kv.pages_per_seq; x += blockDim.x) {
+            const int i = x / kv.pages_per_seq, j = x - i * kv.pages_per_seq;
+            if (j >= pages_for(lengths ? lengths[i] : 0, kv.page_size) && j < pages_for(old[i], kv.page_size)) low = trim_page(kv, seqs[i], j, low);
+        }
+        trim_low(kv, low);
+    } else if (threadIdx.x == 0) {
+        *go = 1;
+    }
 }
 __global__ void __launch_bounds__(COPY_THREADS)
 k_trim(opattr_cache kv, const int32_t *seqs, const int32_t *lengths, const int32_t *old, const int32_t *go) {
     pdl_wait();
     if (*go == 0) return;
-    const int i = blockIdx.x;
-    trim_pages(kv, seqs[i], old[i], lengths ? lengths[i] : 0, blockIdx.y * COPY_THREADS + threadIdx.x, gridDim.y * COPY_THREADS);
+    const int i = blockIdx.x, s = seqs[i], keep = pages_for(lengths ? lengths[i] : 0, kv.page_size), held = pages_for(old[i], kv.page_size);
+    int low = INT32_MAX;
+    for (int j = keep + blockIdx.y * COPY_THREADS + threadIdx.x; j < held; j += gridDim.y * COPY_THREADS) low = trim_page(kv, s, j, low);
+    trim_low(kv, low);
 }
 
 opattr_status do_cache_trim(Ctx &c, Serve &s, const opattr_cache *kv, const int32_t *seqs, const int32_t *lengths,
@@ -459,7 +468,7 @@ opattr_status do_cache_trim(Ctx &c, Serve &s, const opattr_cache *kv, const int3
     int32_t *go = a.take<int32_t>(1), *old = a.take<int32_t>(n), *mark = a.take<int32_t>(kv->n_seqs);
     const int64_t entries = (int64_t)n * kv->pages_per_seq;
     const bool small = entries <= SMALL_ENTRIES;
-    launch(c, "trim_plan", k_trim_plan, dim3(1), dim3(plan_threads(small ? entries / 8 : n)), 0, *kv, seqs, lengths, n, mark,
+    launch(c, "trim_plan", k_trim_plan, dim3(1), dim3(plan_threads(small ? std::max<int64_t>(n, entries / 4) : n)), 0, *kv, seqs, lengths, n, mark,
            old, go, (int)small, s.err);
     if (!small)
         launch(c, "trim", k_trim, dim3(n, grid_for(kv->pages_per_seq, 4 * COPY_THREADS, 64)), dim3(COPY_THREADS), 0, *kv, seqs,
