@@ -10,11 +10,11 @@
 // are given out from the lowest free one on, sequence after sequence.
 //
 // There is nothing to compute: large calls are bound by the rows' way through memory, small
-// ones by a launch (about 2.5 us each) and a plan's chain of dependent loads.  Measured on one
-// GB300 (400 sequences of 200 .. 3,100 tokens in pages of 32, 8 heads of 128): an eighth of
-// them appended anew, 55,000 tokens: 70 us, 6.4 TB/s; their freed places closed by compaction:
-// 71 us; freeing them 6, the plan of the append 10.  Of 24 sequences, each of these calls is
-// the host's 8 us.
+// ones by launches and a plan's chain of dependent loads.  Measured on one GB300 (400
+// sequences of 200 .. 3,100 tokens in pages of 32, 8 heads of 128): an eighth of them appended
+// anew, 55,000 tokens: 70 us, 6.4 TB/s; their freed places closed by compaction: 71 us; freeing
+// them 6, the plan of the append 7.  Of 24 sequences the three calls take 16.6 us, and the
+// host 23.
 #include <algorithm>
 
 #include "serve.cuh"
@@ -339,8 +339,10 @@ opattr_status do_cache_append(Ctx &c, Serve &s, const opattr_cache *kv, const in
 
 // ---------------------------------------------------------------- fork and trim
 // The plan's block makes the change itself where the sequences' tables have few
-// entries, a thread to an entry; a second launch costs 2.5 us.  (A warp to a sequence took
-// 10 us more for 138 sequences of four pages at most.)
+// entries, a thread to an entry (a warp to a sequence took 17 us more for fork and trim
+// of 138 sequences of four pages at most).  A second launch costs the host 2 us, and the GPU what
+// the block takes for 2,500 entries: fork and trim of 40 sequences of 63 pages 8.0 us here,
+// 7.8 in two launches each; of 16 pages 7.1 and 7.3; of 100 (two launches) 10.1 and 7.9.
 constexpr int64_t SMALL_ENTRIES = 4096;
 
 // Page j of sequence s to sequence d; a source is no destination, its length stands.
