@@ -508,9 +508,13 @@ opattr_status opattr_match_noalloc(const opattr_kernels *kernels, const opattr_n
  * profile points at (Sec. 4.5 takes scaled-dot-product attention as a case
  * study), and a workload whose bytes and operations per launch are known.
  *
- * These calls order their work on the context's stream and do not wait for it
- * (they can be captured into a CUDA graph once a first call of the same or a
- * larger size has made the scratch).  Sizes and pointers are checked at the
+ * These calls order their work on the context's stream and do not wait for it.
+ * They can be captured into a CUDA graph once a first call of the same or a
+ * larger size has made the scratch.  The graph may be replayed until the
+ * context is destroyed, whatever calls come between (scratch that a graph
+ * refers to is kept when a larger call outgrows it); as the calls themselves,
+ * replays use the context's scratch, and are ordered with one another and with
+ * its calls: on its stream, or by events.  Sizes and pointers are checked at the
  * call; offsets, sequence ids, lengths and page numbers live on the device
  * and are checked there.  A call that finds one of those out of range does
  * nothing (the cache's calls), or leaves out the rows concerned (the two

@@ -58,6 +58,32 @@ opattr_status cuda_status(Ctx &c, cudaError_t e) {
     return OPATTR_E_CUDA;
 }
 
+bool capturing(Ctx &c) {
+    cudaStreamCaptureStatus s = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(c.stream, &s) != cudaSuccess) {
+        cudaGetLastError();
+        return false;
+    }
+    return s != cudaStreamCaptureStatusNone;
+}
+
+// Lets go of the arena, on a stream that has nothing under way; one that a graph
+// refers to is kept.
+static void release_arena(Ctx &c) {
+    if (c.arena && c.arena_captured) {
+        try {
+            c.retired.push_back(c.arena);
+        } catch (...) {
+            // no room to note it: it stays until the process ends
+        }
+    } else if (c.arena) {
+        cudaFree(c.arena);
+    }
+    c.arena = nullptr;
+    c.arena_cap = 0;
+    c.arena_captured = false;
+}
+
 // Grows the arena to at least `bytes` beyond its kept prefix (the first
 // arena_keep bytes, copied into a grown arena).  OPATTR_FAULT=alloc in the
 // environment makes growth fail, to exercise the out-of-memory path without
@@ -79,9 +105,7 @@ opattr_status ensure_arena(Ctx &c, size_t bytes) {
     if (c.arena && c.arena_keep == 0) {
         // nothing to keep: free first, so the old and new arenas are never held together
         if (cudaStreamSynchronize(c.stream) != cudaSuccess) return cuda_status(c, cudaGetLastError());
-        cudaFree(c.arena);
-        c.arena = nullptr;
-        c.arena_cap = 0;
+        release_arena(c);
     }
     char *fresh = nullptr;
     cudaError_t e = cudaMalloc(&fresh, cap);
@@ -99,11 +123,17 @@ opattr_status ensure_arena(Ctx &c, size_t bytes) {
             return cuda_status(c, e);
         }
         if (c.join_korder) c.join_korder = reinterpret_cast<uint32_t *>(fresh + (reinterpret_cast<char *>(c.join_korder) - c.arena));
-        cudaFree(c.arena);
+        release_arena(c);
     }
     c.arena = fresh;
     c.arena_cap = cap;
     return OPATTR_OK;
+}
+
+opattr_status ensure_lasting_arena(Ctx &c, size_t bytes) {
+    const opattr_status st = ensure_arena(c, bytes);
+    if (st == OPATTR_OK && !c.arena_captured) c.arena_captured = capturing(c);
+    return st;
 }
 
 // Why the join's enclosure has to run again, if it has.
@@ -114,9 +144,7 @@ static bool note_redo(Ctx &c) {
 
 static opattr_status drop_arena(Ctx &c) {
     if (cudaStreamSynchronize(c.stream) != cudaSuccess) return cuda_status(c, cudaGetLastError());
-    if (c.arena) cudaFree(c.arena);
-    c.arena = nullptr;
-    c.arena_cap = 0;
+    release_arena(c);
     return OPATTR_OK;
 }
 
@@ -700,6 +728,7 @@ void opattr_destroy(opattr_ctx *ctx) {
         DeviceGuard g(c.device);
         cudaStreamSynchronize(c.stream);
         if (c.arena) cudaFree(c.arena);
+        for (char *a : c.retired) cudaFree(a);
         if (c.d_status) cudaFree(c.d_status);
         if (c.h_status) cudaFreeHost(c.h_status);
         if (c.h_small) cudaFreeHost(c.h_small);

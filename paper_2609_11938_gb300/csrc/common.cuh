@@ -90,6 +90,10 @@ struct Ctx {
     char *arena = nullptr;
     size_t arena_cap = 0, arena_used = 0;
     bool arena_fixed = false;        // the arena is caller-provided memory: never grow or free it
+    // launches that a CUDA graph has captured hold addresses in the arena: once outgrown
+    // it is kept with the others of `retired` until the context goes
+    bool arena_captured = false;
+    std::vector<char *> retired;
     // status block
     DevStatus *d_status = nullptr;
     DevStatus *h_status = nullptr;   // pinned mirror
@@ -177,6 +181,11 @@ struct Need {
 };
 
 opattr_status ensure_arena(Ctx &c, size_t bytes);
+// Whether what goes onto the context's stream now is captured into a CUDA graph.
+bool capturing(Ctx &c);
+// The same for calls that may be captured: their launches may run again, from a
+// graph, at any time until the context goes, so their arena stays as long.
+opattr_status ensure_lasting_arena(Ctx &c, size_t bytes);
 int sm_count(Ctx &c);
 // The status of an enclosure that read `H` (a NOT_NESTED found beside
 // F_LEVEL_FIXUP does not count: the run on sorted ranges decides).

@@ -314,7 +314,7 @@ opattr_status do_cache_append(Ctx &c, Serve &s, const opattr_cache *kv, const in
     if ((st = serve_ready(c, s))) return st;
     // at most: a page copied and one begun by each sequence, and the full ones
     const int64_t most = std::min<int64_t>(kv->n_pages, 2ll * n + tokens / kv->page_size);
-    if ((st = ensure_arena(c, Need().add<int32_t>(1).add<int32_t>(n).add<int32_t>(n).add<int32_t>(n).add<int32_t>(n).add<int32_t>(n + 1)
+    if ((st = ensure_lasting_arena(c, Need().add<int32_t>(1).add<int32_t>(n).add<int32_t>(n).add<int32_t>(n).add<int32_t>(n).add<int32_t>(n + 1)
                                   .add<int32_t>(kv->n_seqs).add<int32_t>(most).bytes)))
         return st;
     Arena a(c);
@@ -395,7 +395,7 @@ opattr_status do_cache_fork(Ctx &c, Serve &s, const opattr_cache *kv, const int3
     if (st || n == 0) return st;
     if (!src) return OPATTR_E_INVALID_ARG;
     if ((st = serve_ready(c, s))) return st;
-    if ((st = ensure_arena(c, Need().add<int32_t>(1).add<int32_t>(kv->n_seqs).bytes))) return st;
+    if ((st = ensure_lasting_arena(c, Need().add<int32_t>(1).add<int32_t>(kv->n_seqs).bytes))) return st;
     Arena a(c);
     int32_t *go = a.take<int32_t>(1), *mark = a.take<int32_t>(kv->n_seqs);
     const int64_t entries = (int64_t)n * kv->pages_per_seq;
@@ -465,7 +465,7 @@ opattr_status do_cache_trim(Ctx &c, Serve &s, const opattr_cache *kv, const int3
     opattr_status st = seqs_ok(kv, seqs, n);
     if (st || n == 0) return st;
     if ((st = serve_ready(c, s))) return st;
-    if ((st = ensure_arena(c, Need().add<int32_t>(1).add<int32_t>(n).add<int32_t>(kv->n_seqs).bytes))) return st;
+    if ((st = ensure_lasting_arena(c, Need().add<int32_t>(1).add<int32_t>(n).add<int32_t>(kv->n_seqs).bytes))) return st;
     Arena a(c);
     int32_t *go = a.take<int32_t>(1), *old = a.take<int32_t>(n), *mark = a.take<int32_t>(kv->n_seqs);
     const int64_t entries = (int64_t)n * kv->pages_per_seq;
@@ -590,7 +590,7 @@ opattr_status do_cache_compact(Ctx &c, Serve &s, const opattr_cache *kv, int32_t
     opattr_status st = serve_ready(c, s);
     if (st) return st;
     const int tiles = (int)((kv->n_pages + TILE_PAGES - 1) / TILE_PAGES);
-    if ((st = ensure_arena(c, Need().add<int32_t>(2).add<int32_t>(tiles).add<int32_t>(kv->n_pages).add<int32_t>(kv->n_pages)
+    if ((st = ensure_lasting_arena(c, Need().add<int32_t>(2).add<int32_t>(tiles).add<int32_t>(kv->n_pages).add<int32_t>(kv->n_pages)
                                   .add<int32_t>(kv->n_pages).bytes)))
         return st;
     Arena a(c);

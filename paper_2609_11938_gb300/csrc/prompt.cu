@@ -908,7 +908,7 @@ static opattr_status run_prompt(Ctx &c, Serve &s, PromptArgs &p, const CUtensorM
     const double whole = each <= 1 ? keys : std::max(keys, each * mean + (std::ceil(each) - each) * least);
     if (p.tiles <= PLACES && whole > each * mean + 14) {
         const int64_t parts = (int64_t)sms * 4 * ROWS * (DP + 2), most = items + sms;
-        const opattr_status st = ensure_arena(c, Need().add<int>(sms + 1).add<Item>(most).add<float>(parts).bytes);
+        const opattr_status st = ensure_lasting_arena(c, Need().add<int>(sms + 1).add<Item>(most).add<float>(parts).bytes);
         if (st) return st;
         Arena ar(c);
         int *start = ar.take<int>(sms + 1);

@@ -402,7 +402,7 @@ static opattr_status run_token(Ctx &c, Serve &s, TokenArgs &p) {
     opattr_status st = serve_ready(c, s);
     if (st) return st;
     const int64_t part = (int64_t)8 * NT * (DP + 2);
-    if ((st = ensure_arena(c, Need().add<float>(2 * grid * part).bytes))) return st;
+    if ((st = ensure_lasting_arena(c, Need().add<float>(2 * grid * part).bytes))) return st;
     Arena a(c);
     p.parts = a.take<float>(2 * grid * part);
     p.tickets = s.tickets;
