@@ -510,7 +510,8 @@ opattr_status opattr_match_noalloc(const opattr_kernels *kernels, const opattr_n
  *
  * These calls order their work on the context's stream and do not wait for it.
  * They can be captured into a CUDA graph once a first call of the same or a
- * larger size has made the scratch.  The graph may be replayed until the
+ * larger size has made the scratch (OPATTR_E_OOM where it is missing, and the
+ * capture goes on).  The graph may be replayed until the
  * context is destroyed, whatever calls come between (scratch that a graph
  * refers to is kept when a larger call outgrows it); as the calls themselves,
  * replays use the context's scratch, and are ordered with one another and with

@@ -97,7 +97,8 @@ opattr_status ensure_arena(Ctx &c, size_t bytes) {
         if (bytes <= c.arena_cap) return OPATTR_OK;
     }
     bytes += c.arena_keep;
-    if (c.arena_fixed) return OPATTR_E_OOM;
+    // (nothing can be allocated under a capture, and to try would end it)
+    if (c.arena_fixed || capturing(c)) return OPATTR_E_OOM;
     const char *fault = getenv("OPATTR_FAULT");
     if (fault && strcmp(fault, "alloc") == 0) return OPATTR_E_OOM;
     size_t cap = std::max(bytes, (size_t)1 << 20);

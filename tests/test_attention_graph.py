@@ -72,3 +72,34 @@ def test_graph_outlives_its_scratch(opa):
         assert all(torch.equal(a, b) for a, b in zip(step(), want))
         ctx.check()
         del graph
+
+
+@pytest.mark.parametrize("first", [True, False])
+def test_no_scratch_under_capture(opa, first):
+    """A captured call that has no scratch yet, the context's first or one larger than those
+    before it, is refused; the capture and the context go on."""
+    g = gen(42)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s), opa.Context(0, stream=s) as ctx:
+        q = randn(g, (20, 8, 64), BF)
+        k, v = (randn(g, (9000, 2, 64), BF) for _ in range(2))
+        off, koff = i32(0, 20), i32(0, 9000)
+        if not first:
+            ctx.attention(q, q, q, off)
+        s.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            with pytest.raises(opa.OpattrError) as e:
+                ctx.attention(q, k, v, off, koff)
+            other = q + 1
+        assert e.value.status == opa.E_OOM
+        other.zero_()
+        graph.replay()
+        assert torch.equal(other, q + 1)
+        a = ctx.attention(q, k, v, off, koff)[1]
+        ctx.check()
+        with torch.cuda.graph(torch.cuda.CUDAGraph(), stream=s):
+            ctx.attention(q, k, v, off, koff)
+        assert torch.equal(ctx.attention(q, k, v, off, koff)[1], a)
+        ctx.check()
