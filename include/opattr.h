@@ -456,7 +456,8 @@ const char *opattr_status_string(opattr_status status);
 
 /* Launch accounting and per-kernel timing.  With timing on, every kernel
  * launch of the context is bracketed by CUDA events on the context's stream
- * and its duration accumulated per kernel name.  opattr_timing_report fills
+ * and its duration accumulated per kernel name (launches captured into a graph
+ * are counted, not timed).  opattr_timing_report fills
  * up to `cap` entries (names are static strings) and returns how many kernel
  * names have been seen; opattr_launch_count returns the number of kernels the
  * context has launched since creation or the last reset. */

@@ -250,7 +250,8 @@ inline void launch(Ctx &c, const char *name, void (*kern)(KArgs...), dim3 grid, 
     if (grid.x == 0 || grid.y == 0 || grid.z == 0) return;
     cudaEvent_t e0 = nullptr, e1 = nullptr;
     int slot = -1;
-    const bool timed = c.timing && (c.timing_only.empty() || c.timing_only == name);
+    // (under a capture the events would be the graph's, and have no time that can be asked for)
+    const bool timed = c.timing && (c.timing_only.empty() || c.timing_only == name) && !capturing(c);
     if (timed) {
         slot = timing_slot(c, name);
         timing_begin(c, slot, &e0, &e1);

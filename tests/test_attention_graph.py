@@ -103,3 +103,26 @@ def test_no_scratch_under_capture(opa, first):
             ctx.attention(q, k, v, off, koff)
         assert torch.equal(ctx.attention(q, k, v, off, koff)[1], a)
         ctx.check()
+
+
+def test_timing_and_capture(opa):
+    """With timing on, captured launches are not timed, those before and after it are."""
+    g = gen(43)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s), opa.Context(0, stream=s) as ctx:
+        q, k, v = (randn(g, (200, 2, 64), BF) for _ in range(3))
+        off = i32(0, 200)
+        ctx.set_timing(True)
+        want = ctx.attention(q, k, v, off)[1]
+        ctx.check()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            got = ctx.attention(q, k, v, off)[1]
+        ctx.check()
+        graph.replay()
+        again = ctx.attention(q, k, v, off)[1]
+        ctx.check()
+        assert torch.equal(got, want) and torch.equal(again, want)
+        ms, launches = ctx.timing_report()["prompt"]
+        assert launches == 2 and 0 < ms < 1e3
