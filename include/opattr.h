@@ -160,11 +160,12 @@ typedef struct {
     int32_t dedup;                 /* 1: apply opattr_dedup when given (default 1) */
     int32_t checked;               /* reserved, 0 */
     int64_t spin_limit;            /* polls a device-side wait makes before it gives up (0 =
-                                      default, 2^20; must be >= 0).  The only waits are those of
-                                      the single-pass scans (a tile waiting for an earlier tile's
-                                      prefix); one that gives up sums the earlier tiles' input
-                                      itself, so results stay exact, and the call returns
-                                      OPATTR_E_TIMEOUT */
+                                      default, 2^20; must be >= 0).  The join's only waits are
+                                      those of the single-pass scans (a tile waiting for an earlier
+                                      tile's prefix); one that gives up sums the earlier tiles'
+                                      input itself, so results stay exact, and the call returns
+                                      OPATTR_E_TIMEOUT.  Those of opattr_attention, within a block,
+                                      are bounded by time instead, see opattr_check */
 } opattr_config;
 
 /* Host-side result of opattr_match. */
@@ -635,8 +636,9 @@ opattr_status opattr_cache_compact(opattr_ctx *ctx, const opattr_cache *cache, i
 
 /* Waits for the context's stream and returns what the calls above found wrong
  * on the device since the last check: OPATTR_OK, OPATTR_E_INVALID_ARG,
- * OPATTR_E_PAGES, or OPATTR_E_TIMEOUT where a bounded wait gave up (then the
- * results do not count).  The context stays usable.  Collects the timing of
+ * OPATTR_E_PAGES, or OPATTR_E_TIMEOUT where a wait in an opattr_attention gave
+ * up after 4 s (then the results of the calls since the last check do not
+ * count, and prompts after it did nothing).  The context stays usable.  Collects the timing of
  * their launches (opattr_set_timing) too. */
 opattr_status opattr_check(opattr_ctx *ctx);
 

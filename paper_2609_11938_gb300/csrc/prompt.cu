@@ -54,6 +54,9 @@ constexpr int MMA_WARP = 8, LOAD_WARP = 9, TAIL_WARP = 10;   // and the last one
 constexpr int REGS_SOFTMAX = 208, REGS_OTHERS = 88;
 constexpr int CUTS = 4;                  // value tiles cut by a mask that can be under way: half the ring's stages
 constexpr int SHORT = 4;                 // key tiles that take as long as the lookup of an item
+// What a wait may take before its block gives up (opattr_check then returns OPATTR_E_TIMEOUT), and
+// where a test has a part of the kernel fall silent.
+constexpr unsigned WAIT_US = 4000000, SILENT_WAIT_US = 20000;
 constexpr int ITEMS = 2;                 // slots of work items: the one being computed, and the one whose tiles are fetched
 
 // Shapes by the padded head width DP (64 or 128; the copies fill what a head
@@ -81,6 +84,8 @@ struct PromptArgs {
     const int *start;                    // [grid + 1] where they begin
     float *parts;                        // [block][2][sub-tile] partial results, four columns of every row side by side; then the rows' maxima and sums
     uint32_t *tickets;                   // [block][sub-tile] arrivals
+    unsigned limit_us;                   // of every wait
+    int silent;                          // Serve::silent
 };
 
 // A work item: two sub-tiles of queries of one sequence, and keys of it.
@@ -94,9 +99,9 @@ struct Item {
 
 struct Ctrl {
     uint64_t item_full[ITEMS], item_free[ITEMS], item_want, q_full, q_free, kv_full[8], kv_free[8];
-    uint64_t s_full[2], p_half[2], p_full[2], o_full[2], o_free[2], v_full[CUTS], v_ready[CUTS], drain;
+    uint64_t s_full[2], p_half[2], p_full[2], o_full[2], o_free[2], v_full[CUTS], v_ready[CUTS], met[2], drain;
     uint32_t tmem;
-    int stop;
+    Waits waits;
     int poison[CUTS];
     int last[2];
     Item item[ITEMS];
@@ -141,9 +146,6 @@ __device__ __forceinline__ uint32_t tm_ld1(uint32_t at) {
     return r;
 }
 
-// The four warps of sub-tile s.
-__device__ __forceinline__ void group_sync(int s) { asm volatile("bar.sync %0, 128;" ::"r"(s + 1) : "memory"); }
-
 // 32 bytes of a thread in one store: whole sectors, where rows lie far apart.
 __device__ __forceinline__ void store32(void *p, const uint32_t *r) {
     asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
@@ -162,7 +164,8 @@ __device__ __forceinline__ unsigned draw(unsigned *next, unsigned total) {
     return gridDim.x + __shfl_sync(0xffffffffu, k, 0);
 }
 
-template <typename T, int DP, int DV>
+// CUT: the items come from a plan, and may be parts of the keys that are joined.
+template <typename T, int DP, int DV, bool CUT>
 __global__ void __launch_bounds__(THREADS, 1)
 k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorMap mq,
          const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, unsigned *err) {
@@ -178,7 +181,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
     unsigned char *smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const uint32_t sq = smem_addr(smem), skv = sq + 2 * S::TILE;
     const int warp = threadIdx.x >> 5;
-    volatile int *stop = &ctl.stop;
+    volatile Waits *waits = &ctl.waits;
     const opattr_prompt &a = p.a;
     const uint32_t bar_kv = smem_addr(&ctl.kv_full[0]), bar_free = smem_addr(&ctl.kv_free[0]);
     if (threadIdx.x == 0) {
@@ -192,10 +195,11 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
             bar_init(smem_addr(&ctl.p_full[i]), 4);
             bar_init(smem_addr(&ctl.o_full[i]), 1);
             bar_init(smem_addr(&ctl.o_free[i]), 4);
+            bar_init(smem_addr(&ctl.met[i]), 4);
         }
         for (int i = 0; i < CUTS; ++i) bar_init(smem_addr(&ctl.v_full[i]), 1), bar_init(smem_addr(&ctl.v_ready[i]), 1);
         bar_init(smem_addr(&ctl.drain), 1);
-        ctl.stop = 0;
+        ctl.waits.stop = 0, ctl.waits.limit_us = p.limit_us;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         map_prefetch(&mq), map_prefetch(&mk), map_prefetch(&mv);
     }
@@ -209,7 +213,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
     // the next item, for a whole warp; its slot is given back by item_done
     Place<ITEMS> slot;
     auto item_next = [&](Item &it) {
-        if (!warp_wait(smem_addr(&ctl.item_full[slot.at]), slot.ph, stop)) return false;
+        if (!warp_wait(smem_addr(&ctl.item_full[slot.at]), slot.ph, waits)) return false;
         it = ctl.item[slot.at];
         __syncwarp();
         if (lane_id() == 0) bar_arrive(smem_addr(&ctl.item_free[slot.at]));
@@ -228,7 +232,15 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
         const float c = a.scale == 0.f ? __uint_as_float(1) : fabsf(a.scale) * LOG2E;
         const uint64_t c2 = pair(c, c);
         const int row_token = r / p.pack, row_head = r % p.pack;
-        Place<1> turn_s, turn_o;
+        Place<1> turn_s, turn_o, turn_met;
+        // the four warps of the sub-tile wait for one another
+        auto meet = [&] {
+            __syncwarp();
+            if (lane_id() == 0) bar_arrive(smem_addr(&ctl.met[s]));
+            const bool all = warp_wait(smem_addr(&ctl.met[s]), turn_met.ph, waits);
+            turn_met.step();
+            return all;
+        };
         Place<CUTS> over;                                // cut value tiles, of either sub-tile
         Place<S::STAGES> ring;                           // value tiles
         ring.step();
@@ -245,7 +257,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
             float m = -INFINITY, l = 0.f;
             for (int j = 0; j < w.n; ++j) {
                 if (j < n_tiles) {
-                    if (!(ok = warp_wait(b_s, turn_s.ph, stop))) break;
+                    if (!(ok = warp_wait(b_s, turn_s.ph, waits))) break;
                     turn_s.step();
                     tm_after();
                     uint32_t x[KEYS];
@@ -321,7 +333,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                     if (a.causal && j < n_tiles) {
                         // a value that is not finite times a weight of zero would reach the rows
                         // that do not see it: such a tile's products are made here, key by key
-                        if (!(ok = warp_wait(smem_addr(&ctl.v_ready[over.at]), over.ph, stop))) break;
+                        if (!(ok = warp_wait(smem_addr(&ctl.v_ready[over.at]), over.ph, waits))) break;
                         if (seldom(*(volatile int *)&ctl.poison[over.at])) {
                             const unsigned char *v = smem + 2 * S::TILE + ring.at * S::TILE;
                             const int left = seen - j * KEYS;
@@ -369,7 +381,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
             }
             if (!ok) break;
             if (n_tiles > 0) {
-                if (!(ok = warp_wait(smem_addr(&ctl.o_full[s]), turn_o.ph, stop))) break;
+                if (!(ok = warp_wait(smem_addr(&ctl.o_full[s]), turn_o.ph, waits))) break;
                 turn_o.step();
                 tm_after();
             }
@@ -385,7 +397,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
             constexpr int PART = ROWS * (DP + 2);
             // a block's part of the item that it ends with is its second, of the one it begins with its first
             auto part_at = [&](int k) { return parts + ((long long)k * 2 + (k == 0)) * 2 * PART; };
-            if (seldom(it.pieces > 1)) {
+            if (CUT && seldom(it.pieces > 1)) {
                 // a part of the keys: the result so far goes to memory, and whoever brings the
                 // last part of the tile puts them together, in order
                 parts = p.parts + (long long)it.first * 4 * PART + s * PART;
@@ -406,14 +418,16 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                 }
                 if (live) *reinterpret_cast<float2 *>(part + ROWS * DP + 2 * r) = make_float2(ref, l);
                 __threadfence();
-                group_sync(s);
+                if (seldom(p.silent == SILENT_PARTS && (warp & 3) == 1)) break;
+                if (!meet()) break;
                 if (r == 0) {
+                    __threadfence();
                     uint32_t *t = p.tickets + it.first * 2 + s;      // (a block ends with one item at most)
                     const bool all = atomicAdd(t, 1u) == (unsigned)it.pieces - 1;
                     if (all) atomicExch(t, 0u);
                     ctl.last[s] = all;
                 }
-                group_sync(s);
+                if (!meet()) break;
                 mine = joined = *(volatile int *)&ctl.last[s];
                 if (joined) {
                     __threadfence();
@@ -497,7 +511,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                     mma_commit(smem_addr(&ctl.s_full[s]));
                 }
             };
-            auto full = [&](const Place<S::STAGES> &x) { return warp_wait(bar_kv + x.at * 8, x.ph, stop); };
+            auto full = [&](const Place<S::STAGES> &x) { return warp_wait(bar_kv + x.at * 8, x.ph, waits); };
             auto release = [&](int st) {
                 if (lead) mma_commit(bar_free + st * 8);
             };
@@ -517,13 +531,13 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                     if (!full(values) || (j + 1 < nt && !full(keys))) return false;
                     by_hand = false;
                     if (j >= from) {
-                        if (!warp_wait(smem_addr(&ctl.v_ready[over.at]), over.ph, stop)) return false;
+                        if (!warp_wait(smem_addr(&ctl.v_ready[over.at]), over.ph, waits)) return false;
                         by_hand = a.causal && uniform(*(volatile int *)&ctl.poison[over.at]);
                         over.step();
                     }
                     return true;
                 };
-                if (!(ok = warp_wait(smem_addr(&ctl.q_full), q_turn.ph, stop) && full(keys))) break;
+                if (!(ok = warp_wait(smem_addr(&ctl.q_full), q_turn.ph, waits) && full(keys))) break;
                 q_turn.step();
                 tm_after();
                 if (nt0 > 0) scores(0, keys.at);
@@ -539,10 +553,10 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                     for (int s = 0; s < 2; ++s) {
                         const int mine = s ? nt1 : nt0;
                         if (j < mine) {
-                            if (!(ok = warp_wait(smem_addr(&ctl.p_half[s]), s_turn[s].ph, stop))) break;
+                            if (!(ok = warp_wait(smem_addr(&ctl.p_half[s]), s_turn[s].ph, waits))) break;
                             if (j == 0) {
                                 // the results before these have been read (a new barrier's parity 1 is over)
-                                if (!(ok = warp_wait(smem_addr(&ctl.o_free[s]), o_turn[s].ph ^ 1, stop))) break;
+                                if (!(ok = warp_wait(smem_addr(&ctl.o_free[s]), o_turn[s].ph ^ 1, waits))) break;
                                 o_turn[s].step();
                             }
                             tm_after();
@@ -551,7 +565,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                                 for (int k = 0; k < KEYS / 32; ++k)
                                     mma_ts(tm + 256 + s * DP, tm + s * 128 + 8 * k, vd + k * 128, DO, k > 0 || j > 0);
                             }
-                            if (!(ok = warp_wait(smem_addr(&ctl.p_full[s]), s_turn[s].ph, stop))) break;
+                            if (!(ok = warp_wait(smem_addr(&ctl.p_full[s]), s_turn[s].ph, waits))) break;
                             s_turn[s].step();
                             tm_after();
                             if (!hand && lead) {
@@ -574,8 +588,8 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
             }
             // nothing of this thread's is under way when the block ends
             if (lead) mma_commit(smem_addr(&ctl.drain));
-            int never = 0;
-            bar_wait(smem_addr(&ctl.drain), 0, &never);
+            Waits last{0, p.limit_us};
+            bar_wait(smem_addr(&ctl.drain), 0, &last);
         } else if (warp == LOAD_WARP) {
             // ---- tile copies: one thread
             const bool lead = elect();
@@ -587,7 +601,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
             int pars[S::STAGES];
             for (int i = 0; i < S::STAGES; ++i) bars[i] = 0;
             bool ok = true;
-            int q_out = 0;
+            int q_out = 0, out = 0;
             Item it;
             while (ok && item_next(it)) {
                 const Work w(it, p.span, a.causal);
@@ -601,10 +615,14 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                 // and values go ahead, as far as the item before this one leaves stages free
                 bool q_due = true;
                 for (int load = 0; load < 2 * w.n; ++load) {
+                    if (seldom(++out == p.silent)) {
+                        ok = false;
+                        break;
+                    }
                     if (lead && load == ask) bar_arrive(smem_addr(&ctl.item_want));
                     if (q_due && (load == S::STAGES - 2 || load == 2 * w.n - 1 ||
                                   __all_sync(0xffffffffu, bar_is_done(smem_addr(&ctl.q_free), q_turn.ph ^ 1)))) {
-                        if (!(ok = warp_wait(smem_addr(&ctl.q_free), q_turn.ph ^ 1, stop))) break;
+                        if (!(ok = warp_wait(smem_addr(&ctl.q_free), q_turn.ph ^ 1, waits))) break;
                         q_turn.step();
                         q_due = false;
                         if (lead) {
@@ -616,7 +634,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                         }
                         q_out = 1;
                     }
-                    if (!(ok = warp_wait(bar_free + 8 * ring.at, ring.ph ^ 1, stop))) break;
+                    if (!(ok = warp_wait(bar_free + 8 * ring.at, ring.ph ^ 1, waits))) break;
                     // K0, V0, K1, V1, ..; values that are looked over have a barrier of their own: the
                     // stage's may have gone round several times before the tail's warp sees it
                     const bool keys = load % 2 == 0, cut = !keys && load / 2 >= w.cut;
@@ -634,13 +652,11 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                     ring.step();
                 }
             }
-            // copies that nobody waits for any more
-            int never = 0;
-            if (*stop) {
-                for (int i = 0; i < S::STAGES; ++i)
-                    if (bars[i]) bar_wait(bars[i], pars[i], &never);
-                if (q_out) bar_wait(bq, q_turn.ph ^ 1, &never);
-            }
+            // the block ends with no copy under way: where a wait gave up, nobody else waits for them
+            Waits last{0, p.limit_us};
+            for (int i = 0; i < S::STAGES; ++i)
+                if (bars[i]) bar_wait(bars[i], pars[i], &last);
+            if (q_out) bar_wait(bq, q_turn.ph ^ 1, &last);
         } else if (warp == TAIL_WARP) {
             // ---- value tiles that a mask cuts: rows past the sequence's keys become zeros, and,
             // causal, the others are looked over for values that are not finite
@@ -654,7 +670,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                 const Work w(it, p.span, a.causal);
                 for (int j = 0; j < w.n; ++j, ring.step(), ring.step()) {
                     if (j < w.cut) continue;
-                    if (!(ok = warp_wait(smem_addr(&ctl.v_full[over.at]), over.ph, stop))) break;
+                    if (!(ok = warp_wait(smem_addr(&ctl.v_full[over.at]), over.ph, waits))) break;
                     uint4 *v = reinterpret_cast<uint4 *>(smem + 2 * S::TILE + ring.at * S::TILE);
                     const int keys = min(KEYS, it.lk - j * KEYS);
                     unsigned most = 0;
@@ -686,7 +702,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
             // on, enough for its tiles whatever comes before it; those it does not need are passed
             // over.  A block's first item is its number, others are drawn.
             const int per = 2 * p.span;                  // tokens of an item
-            const bool few = !p.plan && a.n_seqs <= 32;
+            const bool few = !CUT && a.n_seqs <= 32;
             // after a wait that gave up nothing more is begun
             const unsigned gave_up = *(volatile unsigned *)err & SERVE_TIMEOUT;
             int vq0 = 0, vq1 = 0, vk0 = 0, vk1 = 0;
@@ -703,14 +719,14 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                 upto = warp_inclusive_scan(mine);
                 tiles = min(tiles, __shfl_sync(0xffffffffu, upto, 31));
             }
-            const unsigned heads_x = p.heads_x, total = p.plan ? (unsigned)p.start[blockIdx.x + 1] : heads_x * (unsigned)tiles;
+            const unsigned heads_x = p.heads_x, total = CUT ? (unsigned)p.start[blockIdx.x + 1] : heads_x * (unsigned)tiles;
             const bool none = uniform(gave_up) != 0;
             Place<1> wanted;
-            unsigned i = p.plan ? (unsigned)p.start[blockIdx.x] : blockIdx.x;
+            unsigned i = CUT ? (unsigned)p.start[blockIdx.x] : blockIdx.x;
             for (bool more = true; more;) {
                 Item it{};
                 while (i < total && !none) {
-                    if (p.plan) {
+                    if (CUT) {
                         it = p.plan[i];
                         break;
                     }
@@ -745,16 +761,16 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                     i = draw(p.next, total);
                 }
                 more = it.some != 0;
-                if (!warp_wait(smem_addr(&ctl.item_free[slot.at]), slot.ph ^ 1, stop)) break;
+                if (!warp_wait(smem_addr(&ctl.item_free[slot.at]), slot.ph ^ 1, waits)) break;
                 if (lane_id() == 0) {
                     ctl.item[slot.at] = it;
                     bar_arrive(smem_addr(&ctl.item_full[slot.at]));
                 }
                 slot.step();
                 if (more) {
-                    if (!warp_wait(smem_addr(&ctl.item_want), wanted.ph, stop)) break;
+                    if (!warp_wait(smem_addr(&ctl.item_want), wanted.ph, waits)) break;
                     wanted.step();
-                    i = p.plan ? i + 1 : draw(p.next, total);
+                    i = CUT ? i + 1 : draw(p.next, total);
                 }
             }
             if (blockIdx.x == 0) {
@@ -768,7 +784,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
     }
     tm_before();
     __syncthreads();
-    if (threadIdx.x == 0 && *stop) atomicOr(err, SERVE_TIMEOUT);
+    if (threadIdx.x == 0 && waits->stop) atomicOr(err, SERVE_TIMEOUT);
     __syncwarp();
     if (warp == MMA_WARP) tm_free(ctl.tmem, 512);
 }
@@ -888,9 +904,19 @@ static bool row_map(CUtensorMap *m, int dtype, const opattr_rows &r, int64_t tok
                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+template <typename T, int DP, int DV, bool CUT>
+static opattr_status launch_prompt(Ctx &c, Serve &s, const PromptArgs &p, const CUtensorMap *m, unsigned grid) {
+    constexpr unsigned bit = 1u << (2 * ((std::is_same<T, __half>::value ? 3 : 0) + (DP == 64 ? 0 : DV == 96 ? 1 : 2)) + CUT);
+    if (!(s.prompt_room & bit)) {
+        const cudaError_t e = cudaFuncSetAttribute(k_prompt<T, DP, DV, CUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<DP>::SMEM);
+        if (e != cudaSuccess) return cuda_status(c, e);
+        s.prompt_room |= bit;
+    }
+    launch(c, "prompt", k_prompt<T, DP, DV, CUT>, dim3(grid), dim3(THREADS), Shape<DP>::SMEM, p, m[0], m[1], m[2], s.err);
+    return cuda_status(c, c.last_error);
+}
 template <typename T, int DP, int DV>
 static opattr_status run_prompt(Ctx &c, Serve &s, PromptArgs &p, const CUtensorMap *m) {
-    using S = Shape<DP>;
     const opattr_prompt &a = p.a;
     const int64_t items = (int64_t)p.heads_x * p.tiles;
     const int sms = sm_count(c);
@@ -919,15 +945,8 @@ static opattr_status run_prompt(Ctx &c, Serve &s, PromptArgs &p, const CUtensorM
         p.tickets = s.tickets;
         launch(c, "prompt_plan", k_prompt_plan, dim3(1), dim3(1024), 0, p, sms, plan, start);
     }
-    constexpr unsigned bit = 1u << ((std::is_same<T, __half>::value ? 3 : 0) + (DP == 64 ? 0 : DV == 96 ? 1 : 2));
-    if (!(s.prompt_room & bit)) {
-        const cudaError_t e = cudaFuncSetAttribute(k_prompt<T, DP, DV>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
-        if (e != cudaSuccess) return cuda_status(c, e);
-        s.prompt_room |= bit;
-    }
-    launch(c, "prompt", k_prompt<T, DP, DV>, dim3((unsigned)(p.plan ? sms : std::min<int64_t>(items, sms))), dim3(THREADS), S::SMEM, p, m[0],
-           m[1], m[2], s.err);
-    return cuda_status(c, c.last_error);
+    return p.plan ? launch_prompt<T, DP, DV, true>(c, s, p, m, (unsigned)sms)
+                  : launch_prompt<T, DP, DV, false>(c, s, p, m, (unsigned)std::min<int64_t>(items, sms));
 }
 
 template <typename T>
@@ -964,6 +983,9 @@ opattr_status do_attention(Ctx &c, Serve &s, const opattr_prompt *a) {
     const int64_t tiles = a->q_tokens / (2 * p.span) + a->n_seqs;
     if (tiles * p.heads_x > INT32_MAX) return OPATTR_E_INVALID_ARG;
     p.tiles = (int)tiles;
+    p.silent = s.silent;
+    p.limit_us = s.silent ? SILENT_WAIT_US : WAIT_US;
+    s.silent = 0;
     p.next = s.err + 16;                                 // its own line
     p.wide = a->head_dim % 64 == 0 && (reinterpret_cast<uintptr_t>(a->out.data) & 31) == 0 &&
              (a->q_tokens == 1 || a->out.token_stride % 16 == 0) && (a->q_heads == 1 || a->out.head_stride % 16 == 0);

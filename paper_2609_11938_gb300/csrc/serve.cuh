@@ -21,7 +21,12 @@ struct Serve {
     unsigned *err = nullptr;         // ServeErr bits, sticky; at word 16 the prompts' count of work items drawn
     uint32_t *tickets = nullptr;     // arrivals at each block's cut results; zero between launches
     unsigned prompt_room = 0;        // variants of the prompt kernel that have their shared memory
+    // OPATTR_FAULT=prompt:N in the environment of a context's first call: in the first prompt
+    // launch, every block's copies end before the N-th tile; N is SILENT_PARTS: one warp in four does
+    // not come where parts are joined.  To exercise the waits' limit without a GPU fault.
+    int silent = 0;
 };
+constexpr int SILENT_PARTS = -1;
 
 constexpr int TICKETS = 4096;        // at most three blocks an SM count in them
 opattr_status serve_ready(Ctx &c, Serve &s);

@@ -36,30 +36,34 @@ __device__ __forceinline__ bool bar_is_done(uint32_t bar, unsigned phase) {
                  : "=r"(ok) : "r"(bar), "r"(phase) : "memory");
     return ok;
 }
-// Waits until the phase is over; gives up after WAIT_NS of waiting, or once another
-// warp of the block gave up.  The sleeps are long: warps that poll take issue slots
-// from those that compute.
-constexpr unsigned long long WAIT_NS = 4000000000ull;
+// A block's waits, in its shared memory: whether one of them gave up, and how long each may take.
+struct Waits {
+    int stop;
+    unsigned limit_us;
+};
+// Waits until the phase is over; gives up after the limit, or once another warp of the
+// block gave up.  The sleeps are long: warps that poll take issue slots from those that
+// compute.
 constexpr unsigned SLEEP_NS = 1000000;
 __device__ __forceinline__ unsigned long long clock_ns() {
     unsigned long long t;
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
     return t;
 }
-__device__ __forceinline__ bool bar_wait_on(uint32_t bar, unsigned phase, volatile int *stop) {
-    const unsigned long long t0 = clock_ns();
-    while (!*stop && clock_ns() - t0 < WAIT_NS)
+__device__ __forceinline__ bool bar_wait_on(uint32_t bar, unsigned phase, volatile Waits *w) {
+    const unsigned long long t0 = clock_ns(), limit = w->limit_us * 1000ull;
+    while (!w->stop && clock_ns() - t0 < limit)
         if (bar_done(bar, phase, SLEEP_NS)) return true;
-    *stop = 1;
+    w->stop = 1;
     return false;
 }
-__device__ __forceinline__ bool bar_wait(uint32_t bar, unsigned phase, volatile int *stop) {
-    if (seldom(!bar_done(bar, phase, SLEEP_NS))) return bar_wait_on(bar, phase, stop);
+__device__ __forceinline__ bool bar_wait(uint32_t bar, unsigned phase, volatile Waits *w) {
+    if (seldom(!bar_done(bar, phase, SLEEP_NS))) return bar_wait_on(bar, phase, w);
     return true;
 }
 // The same for a whole warp that goes on together.
-__device__ __forceinline__ bool warp_wait(uint32_t bar, unsigned phase, volatile int *stop) {
-    return __all_sync(0xffffffffu, bar_wait(bar, phase, stop));
+__device__ __forceinline__ bool warp_wait(uint32_t bar, unsigned phase, volatile Waits *w) {
+    return __all_sync(0xffffffffu, bar_wait(bar, phase, w));
 }
 
 // ---------------------------------------------------------------- tile copies
