@@ -637,9 +637,10 @@ opattr_status opattr_cache_compact(opattr_ctx *ctx, const opattr_cache *cache, i
 /* Waits for the context's stream and returns what the calls above found wrong
  * on the device since the last check: OPATTR_OK, OPATTR_E_INVALID_ARG,
  * OPATTR_E_PAGES, or OPATTR_E_TIMEOUT where a wait in an opattr_attention gave
- * up after 4 s (then the results of the calls since the last check do not
- * count, and prompts after it did nothing).  The context stays usable.  Collects the timing of
- * their launches (opattr_set_timing) too. */
+ * up, after 4 s and 10 us for each 128 of k_tokens (then the results of the
+ * calls since the last check do not count, and prompts after it did nothing).
+ * The context stays usable.  Collects the timing of their launches
+ * (opattr_set_timing) too. */
 opattr_status opattr_check(opattr_ctx *ctx);
 
 #ifdef __cplusplus

@@ -54,9 +54,10 @@ constexpr int MMA_WARP = 8, LOAD_WARP = 9, TAIL_WARP = 10;   // and the last one
 constexpr int REGS_SOFTMAX = 208, REGS_OTHERS = 88;
 constexpr int CUTS = 4;                  // value tiles cut by a mask that can be under way: half the ring's stages
 constexpr int SHORT = 4;                 // key tiles that take as long as the lookup of an item
-// What a wait may take before its block gives up (opattr_check then returns OPATTR_E_TIMEOUT), and
-// where a test has a part of the kernel fall silent.
-constexpr unsigned WAIT_US = 4000000, SILENT_WAIT_US = 20000;
+// What a wait may take before its block gives up (opattr_check then returns OPATTR_E_TIMEOUT): the
+// look-up waits for all tiles of an item, so long ones have several times what a tile takes (1 to 2 us)
+// on top.  And where a test has a part of the kernel fall silent.
+constexpr unsigned WAIT_US = 4000000, TILE_WAIT_US = 10, SILENT_WAIT_US = 20000;
 constexpr int ITEMS = 2;                 // slots of work items: the one being computed, and the one whose tiles are fetched
 
 // Shapes by the padded head width DP (64 or 128; the copies fill what a head
@@ -984,7 +985,7 @@ opattr_status do_attention(Ctx &c, Serve &s, const opattr_prompt *a) {
     if (tiles * p.heads_x > INT32_MAX) return OPATTR_E_INVALID_ARG;
     p.tiles = (int)tiles;
     p.silent = s.silent;
-    p.limit_us = s.silent ? SILENT_WAIT_US : WAIT_US;
+    p.limit_us = s.silent ? SILENT_WAIT_US : WAIT_US + TILE_WAIT_US * (unsigned)(a->k_tokens / KEYS);
     s.silent = 0;
     p.next = s.err + 16;                                 // its own line
     p.wide = a->head_dim % 64 == 0 && (reinterpret_cast<uintptr_t>(a->out.data) & 31) == 0 &&

@@ -52,3 +52,22 @@ def test_waits_run_out(opa, monkeypatch, queries, keys, heads, kv, dim, dtype, s
         for _ in range(2):
             assert torch.equal(ctx.attention(*args)[1], want)
             ctx.check()
+
+
+def test_wait_for_a_long_item(opa):
+    """One query over 800 million keys, of which the first and the last thousand matter, among two
+    thousand sequences that have none: one item of one block, whose waits last longer than
+    those of any ordinary call."""
+    n, seqs = 800_000_000, 2100
+    kv = torch.zeros((n, 1, 8), dtype=torch.bfloat16, device=DEV)
+    kv[:, 0, 0] = -200.0
+    kv[:1000, 0, 0], kv[-1000:, 0, 0] = 0.0, 0.0
+    kv[:1000, 0, 1], kv[-1000:, 0, 1] = 1.0, 3.0
+    q = torch.zeros((1, 1, 8), dtype=torch.bfloat16, device=DEV)
+    q[:, :, 0] = 1.0
+    ends = [torch.tensor([0] + [x] * seqs, dtype=torch.int32, device=DEV) for x in (1, n)]
+    with opa.Context(0) as ctx:
+        _, out, lse = ctx.attention(q, kv, kv, *ends, causal=False, scale=1.0, need_lse=True)
+        ctx.check()
+    assert out.flatten().tolist() == [0.0, 2.0] + [0.0] * 6
+    assert abs(float(lse) - 7.600902459542082) < 1e-5          # log of 2,000
