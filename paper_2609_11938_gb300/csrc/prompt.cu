@@ -117,7 +117,8 @@ struct Place {
     }
 };
 
-// What an item's sub-tiles have to do.
+// What an item's sub-tiles have to do.  (Queries and keys may come near 2^31 in number, and
+// places a tile past the last of them pass it: those are sums without a sign.)
 struct Work {
     int base[2], tiles[2], clean[2];     // first query; key tiles; the first of them that a mask cuts
     int n, cut;                          // key tiles of either; the first that is looked over
@@ -125,11 +126,11 @@ struct Work {
         const int ahead = it.ahead;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            base[s] = it.t0 + s * span;
-            const int rows = min(span, it.lq - base[s]);
+            base[s] = (int)((unsigned)it.t0 + s * span);
+            const int rows = min(span, (int)((unsigned)it.lq - base[s]));
             const int keys = rows <= 0 ? 0 : causal ? max(0, min(it.lk, base[s] + rows + ahead)) : it.lk;
-            tiles[s] = (keys + KEYS - 1) / KEYS;
-            clean[s] = (causal ? max(0, min(it.lk, base[s] + 1 + ahead)) : it.lk) / KEYS;
+            tiles[s] = ((unsigned)keys + KEYS - 1) / KEYS;
+            clean[s] = (causal ? max(0, min(it.lk, (int)((unsigned)base[s] + 1 + ahead))) : it.lk) / KEYS;
         }
         n = max(tiles[0], tiles[1]);
         cut = tiles[1] > 0 ? min(clean[0], clean[1]) : clean[0];
@@ -250,11 +251,11 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
         while (ok && item_next(it)) {
             const Work w(it, p.span, a.causal);
             const int n_tiles = s ? w.tiles[1] : w.tiles[0], clean = s ? w.clean[1] : w.clean[0];
-            const int head = it.head0 + row_head, row = (s ? w.base[1] : w.base[0]) + row_token;
-            const int seen = a.causal ? min(it.lk, row + 1 + it.ahead) : it.lk;
+            const int head = it.head0 + row_head, row = (int)((unsigned)(s ? w.base[1] : w.base[0]) + row_token);
+            const int seen = a.causal ? min(it.lk, (int)((unsigned)row + 1 + it.ahead)) : it.lk;
             // (rows past the queries, or past the sub-tile's last whole token, are nobody's: what
             // is in them has no say in when the others are rescaled)
-            const bool live = row < it.lq && row_token < p.span;
+            const bool live = (unsigned)row < (unsigned)it.lq && row_token < p.span;
             float m = -INFINITY, l = 0.f;
             for (int j = 0; j < w.n; ++j) {
                 if (j < n_tiles) {
@@ -267,7 +268,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                     tm_wait_ld();
                     if (j >= clean) {
                         // of the 32s of keys that a mask cuts, most are seen by all of the warp's rows
-                        const int left = seen - j * KEYS;
+                        const int left = (int)((unsigned)seen - j * KEYS);
 #pragma unroll
                         for (int q = 0; q < KEYS; q += 32) {
                             if (__all_sync(0xffffffffu, left >= q + 32)) continue;
@@ -337,7 +338,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                         if (!(ok = warp_wait(smem_addr(&ctl.v_ready[over.at]), over.ph, waits))) break;
                         if (seldom(*(volatile int *)&ctl.poison[over.at])) {
                             const unsigned char *v = smem + 2 * S::TILE + ring.at * S::TILE;
-                            const int left = seen - j * KEYS;
+                            const int left = (int)((unsigned)seen - j * KEYS);
 #pragma unroll 1
                             for (int d = 0; d < DP; d += 32) {
                                 uint32_t o[32] = {};
@@ -716,7 +717,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
             int mine = 0, upto = 0, tiles = p.tiles;
             if (few) {
                 fetch(min((int)lane_id(), a.n_seqs - 1));
-                mine = (int)lane_id() < a.n_seqs && good() ? (vq1 - vq0 + per - 1) / per : 0;
+                mine = (int)lane_id() < a.n_seqs && good() ? ((unsigned)(vq1 - vq0) + per - 1) / per : 0;
                 upto = warp_inclusive_scan(mine);
                 tiles = min(tiles, __shfl_sync(0xffffffffu, upto, 31));
             }
@@ -737,7 +738,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                     int k, t0;
                     if (few) {
                         k = max(0, __ffs(__ballot_sync(0xffffffffu, upto > x)) - 1);
-                        t0 = (x - __shfl_sync(0xffffffffu, upto - mine, k)) * per;
+                        t0 = (int)((unsigned)(x - __shfl_sync(0xffffffffu, upto - mine, k)) * per);
                     } else {
                         // the last sequence whose places begin at x or before it, 32 at a time
                         int lo = 0, n = a.n_seqs;
@@ -751,7 +752,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                         const int b = lo + min((int)lane_id(), n - 1);
                         fetch(b);
                         k = max(0, 31 - __clz(__ballot_sync(0xffffffffu, (int)lane_id() < n && vq0 / per + b <= x)));
-                        t0 = (x - __shfl_sync(0xffffffffu, vq0, k) / per - (lo + k)) * per;
+                        t0 = (int)((unsigned)(x - __shfl_sync(0xffffffffu, vq0, k) / per - (lo + k)) * per);
                     }
                     const int q0 = __shfl_sync(0xffffffffu, vq0, k), lq = __shfl_sync(0xffffffffu, vq1, k) - q0;
                     const int k0 = __shfl_sync(0xffffffffu, vk0, k), lk = __shfl_sync(0xffffffffu, vk1, k) - k0;
@@ -806,7 +807,7 @@ __global__ void __launch_bounds__(1024) k_prompt_plan(PromptArgs p, int blocks, 
     const int per = 2 * p.span;
     auto item_of = [&](int x, int b) {                   // of place x, which is sequence b's
         const int q0 = a.q_offsets[b], q1 = a.q_offsets[b + 1], k0 = a.k_offsets[b], k1 = a.k_offsets[b + 1];
-        const int t0 = (x - q0 / per - b) * per;
+        const int t0 = (int)((unsigned)(x - q0 / per - b) * per);
         if (q0 < 0 || q1 < q0 || q1 > a.q_tokens || k0 < 0 || k1 < k0 || k1 > a.k_tokens || t0 < 0 || t0 >= q1 - q0) return Item{};
         return Item{q0, q1 - q0, k0, k1 - k0, t0, 0, (k1 - k0) - (q1 - q0), 0, 0, 1, 1};
     };

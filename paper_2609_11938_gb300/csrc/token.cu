@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(TOKEN_THREADS, NT == 1 ? 3 : 2) k_token(const 
         const int len = kv.length[seq];
         return len > kv.pages_per_seq << p.shift ? -1 : len;
     };
-    auto steps_of = [](int len) { return len <= 0 ? 1 : (len + STEP - 1) / STEP; };
+    auto steps_of = [](int len) { return len <= 0 ? 1 : (len - 1) / STEP + 1; };
     auto cost_of = [](int steps) { return steps + 1; };        // place 0 of a pair stands for no keys
     const int per = (p.n + TOKEN_THREADS - 1) / TOKEN_THREADS, b0 = min(p.n, (int)threadIdx.x * per), b1 = min(p.n, b0 + per);
     long long mine = 0;
@@ -178,7 +178,8 @@ __global__ void __launch_bounds__(TOKEN_THREADS, NT == 1 ? 3 : 2) k_token(const 
         float o[NT][DP / 16][4] = {}, m[NT][2], l[NT][2] = {};
 #pragma unroll
         for (int t = 0; t < NT; ++t) m[t][0] = m[t][1] = -INFINITY;
-        const int last = min(len, to * STEP);                          // keys of this run: from * STEP .. last
+        // (unsigned where a step past a length near 2^31 is counted)
+        const int last = (int)min((unsigned)len, (unsigned)to * STEP);  // keys of this run: from * STEP .. last
         uint4 kr[FR][2][KC], vr[FR][4][VC];
         // pages of this warp's coming keys, one to a lane: lane i has those of step held + i
         int held = 0, pages[FR];
@@ -187,8 +188,8 @@ __global__ void __launch_bounds__(TOKEN_THREADS, NT == 1 ? 3 : 2) k_token(const 
                 held = step;
 #pragma unroll
                 for (int x = 0; x < FR; ++x) {
-                    const int key = (step + lane) * STEP + 16 * (warp * FR + x);
-                    pages[x] = key < last ? table[key >> p.shift] : 0;
+                    const unsigned key = (unsigned)(step + lane) * STEP + 16 * (warp * FR + x);
+                    pages[x] = key < (unsigned)last ? table[key >> p.shift] : 0;
                 }
             }
             return __shfl_sync(0xffffffffu, pages[f], step - held);
