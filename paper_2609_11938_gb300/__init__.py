@@ -492,7 +492,8 @@ def _distinct(t, name):
 @dataclass
 class KVCache:
     """A paged key-value cache as device tensors (opattr_cache in
-    include/opattr.h has the layouts); Context.cache makes an empty one."""
+    include/opattr.h has the layouts); Context.cache makes an empty one.  A field
+    may be replaced by another tensor that fits the others."""
     k_pages: object                 # [n_pages, kv_heads, page_size, head_dim] bfloat16 or float16
     v_pages: object
     table: object                   # int32 [n_seqs, pages_per_seq], -1 past a sequence's length
@@ -501,6 +502,21 @@ class KVCache:
     low: object                     # int32 [1]: no page below it is free
 
     def __post_init__(self):
+        self._lay_out()
+
+    def __setattr__(self, name, value):
+        old = self.__dict__.get(name)
+        object.__setattr__(self, name, value)
+        if "struct" in self.__dict__ and name in self.__dataclass_fields__ and value is not old:
+            # the calls go by the struct's addresses
+            try:
+                self._lay_out()
+            except Exception:
+                object.__setattr__(self, name, old)
+                raise
+
+    def _lay_out(self):
+        """Checks the tensors; their sizes and addresses as the calls take them."""
         dv = self.k_pages.get_device()
         if self.k_pages.dim() != 4 or self.v_pages.shape != self.k_pages.shape:
             raise ValueError("k_pages, v_pages: expected one shape [n_pages, kv_heads, page_size, head_dim]")
