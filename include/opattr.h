@@ -623,7 +623,7 @@ opattr_status opattr_cache_fork(opattr_ctx *ctx, const opattr_cache *cache, cons
                                 int32_t n);
 
 /* Sequence seqs[i] (each once) keeps its first lengths[i] tokens (i32[n]
- * device, at most its length, not the cache's own array; NULL: none), and
+ * device, at most its length; may lie in the cache's own array; NULL: none), and
  * lets go of the pages past them.  Errors: as opattr_attention. */
 opattr_status opattr_cache_trim(opattr_ctx *ctx, const opattr_cache *cache, const int32_t *seqs,
                                 const int32_t *lengths, int32_t n);

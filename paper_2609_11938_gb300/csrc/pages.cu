@@ -428,7 +428,7 @@ __device__ __forceinline__ void trim_low(const opattr_cache &kv, int low) {
 }
 __global__ void __launch_bounds__(PLAN_THREADS)
 k_trim_plan(opattr_cache kv, const int32_t *seqs, const int32_t *lengths, int n, int32_t *mark, int32_t *old,
-            int32_t *go, int small, unsigned *err) {
+            int32_t *kept, int32_t *go, int small, unsigned *err) {
     pdl_wait();
     if (threadIdx.x == 0) *go = 0;
     bool bad = false;
@@ -440,16 +440,17 @@ k_trim_plan(opattr_cache kv, const int32_t *seqs, const int32_t *lengths, int n,
             const int len = kv.length[s];
             bad = bad || length_bad(kv, s) || to < 0 || to > len;
             old[i] = len;
+            kept[i] = to;        // (`lengths` may be the cache's own, which change below)
         }
     }
     if (any_bad(bad, SERVE_INVALID, err)) return;
     if (marks_bad(seqs, n, mark, err)) return;
-    for (int i = threadIdx.x; i < n; i += blockDim.x) kv.length[seqs[i]] = lengths ? lengths[i] : 0;
+    for (int i = threadIdx.x; i < n; i += blockDim.x) kv.length[seqs[i]] = kept[i];
     if (small) {
         int low = INT32_MAX;
         for (int x = threadIdx.x; x < n * kv.pages_per_seq; x += blockDim.x) {
             const int i = x / kv.pages_per_seq, j = x - i * kv.pages_per_seq;
-            if (j >= pages_for(lengths ? lengths[i] : 0, kv.page_size) && j < pages_for(old[i], kv.page_size)) low = trim_page(kv, seqs[i], j, low);
+            if (j >= pages_for(kept[i], kv.page_size) && j < pages_for(old[i], kv.page_size)) low = trim_page(kv, seqs[i], j, low);
         }
         trim_low(kv, low);
     } else if (threadIdx.x == 0) {
@@ -457,10 +458,10 @@ k_trim_plan(opattr_cache kv, const int32_t *seqs, const int32_t *lengths, int n,
     }
 }
 __global__ void __launch_bounds__(COPY_THREADS)
-k_trim(opattr_cache kv, const int32_t *seqs, const int32_t *lengths, const int32_t *old, const int32_t *go) {
+k_trim(opattr_cache kv, const int32_t *seqs, const int32_t *kept, const int32_t *old, const int32_t *go) {
     pdl_wait();
     if (*go == 0) return;
-    const int i = blockIdx.x, s = seqs[i], keep = pages_for(lengths ? lengths[i] : 0, kv.page_size), held = pages_for(old[i], kv.page_size);
+    const int i = blockIdx.x, s = seqs[i], keep = pages_for(kept[i], kv.page_size), held = pages_for(old[i], kv.page_size);
     int low = INT32_MAX;
     for (int j = keep + blockIdx.y * COPY_THREADS + threadIdx.x; j < held; j += gridDim.y * COPY_THREADS) low = trim_page(kv, s, j, low);
     trim_low(kv, low);
@@ -471,16 +472,16 @@ opattr_status do_cache_trim(Ctx &c, Serve &s, const opattr_cache *kv, const int3
     opattr_status st = seqs_ok(kv, seqs, n);
     if (st || n == 0) return st;
     if ((st = serve_ready(c, s))) return st;
-    if ((st = ensure_lasting_arena(c, Need().add<int32_t>(1).add<int32_t>(n).add<int32_t>(kv->n_seqs).bytes))) return st;
+    if ((st = ensure_lasting_arena(c, Need().add<int32_t>(1).add<int32_t>(n).add<int32_t>(n).add<int32_t>(kv->n_seqs).bytes))) return st;
     Arena a(c);
-    int32_t *go = a.take<int32_t>(1), *old = a.take<int32_t>(n), *mark = a.take<int32_t>(kv->n_seqs);
+    int32_t *go = a.take<int32_t>(1), *old = a.take<int32_t>(n), *kept = a.take<int32_t>(n), *mark = a.take<int32_t>(kv->n_seqs);
     const int64_t entries = (int64_t)n * kv->pages_per_seq;
     const bool small = entries <= SMALL_ENTRIES;
     launch(c, "trim_plan", k_trim_plan, dim3(1), dim3(plan_threads(small ? std::max<int64_t>(n, entries / 4) : n)), 0, *kv, seqs, lengths, n, mark,
-           old, go, (int)small, s.err);
+           old, kept, go, (int)small, s.err);
     if (!small)
         launch(c, "trim", k_trim, dim3(n, grid_for(kv->pages_per_seq, 4 * COPY_THREADS, 64)), dim3(COPY_THREADS), 0, *kv, seqs,
-               lengths, (const int32_t *)old, (const int32_t *)go);
+               (const int32_t *)kept, (const int32_t *)old, (const int32_t *)go);
     return cuda_status(c, c.last_error);
 }
 
