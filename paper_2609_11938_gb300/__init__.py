@@ -483,6 +483,15 @@ def _rows(t, heads: int | None, dim: int, like, name, device):
     return p, st, sh
 
 
+def _no_grad(**tensors):
+    """These operators have no backward pass: where gradients are recorded, a
+    result that is cut off from its inputs in silence would be wrong."""
+    if _torch().is_grad_enabled():
+        for name, t in tensors.items():
+            if t.requires_grad:
+                raise ValueError(f"{name}: requires a gradient, which this call has none of: use torch.no_grad() or detach it")
+
+
 def _distinct(t, name):
     """An output's rows must not overlap."""
     if t.numel() and any(s == 0 and n > 1 for s, n in zip(t.stride(), t.shape)):
@@ -789,7 +798,8 @@ class Context:
         """Attention over packed sequences (opattr_attention): q [tokens, heads,
         dim], k and v [tokens, kv_heads, dim]; offsets int32 [n_seqs + 1] on the
         device (none: one sequence; k_offsets none: q_offsets).  scale: by
-        default 1 / sqrt(dim).  Returns (status, out, lse or None)."""
+        default 1 / sqrt(dim).  No backward pass: inputs that require a gradient
+        are refused where gradients are recorded.  Returns (status, out, lse or None)."""
         torch = _torch()
         dv = self.device
         qs, ks = q.shape, k.shape
@@ -805,6 +815,8 @@ class Context:
             raise ValueError(f"heads: {heads} of q are no multiple of {kv_heads} of k")
         if v.shape[0] != k_tokens:
             raise ValueError(f"v: expected {k_tokens} rows, got {v.shape[0]}")
+        if q.requires_grad or k.requires_grad or v.requires_grad:
+            _no_grad(q=q, k=k, v=v)
         rq, rk, rv = _rows(q, heads, dim, dt, "q", dv), _rows(k, kv_heads, dim, dt, "k", dv), _rows(v, kv_heads, dim, dt, "v", dv)
         if q_offsets is None:
             if k_offsets is not None:
@@ -869,6 +881,8 @@ class Context:
             raise ValueError(f"heads: {heads} of q are no multiple of {kv.kv_heads} of the cache")
         if seqs is None and n > kv.n_seqs:
             raise ValueError(f"q: {n} rows for {kv.n_seqs} sequences")
+        if q.requires_grad:
+            _no_grad(q=q)
         out, ro = self._out(out, q, heads, dim, dt)
         lse, p_lse = None, 0
         if need_lse:
@@ -885,6 +899,8 @@ class Context:
         kv = self._cache(cache)
         if v.shape != k.shape:
             raise ValueError(f"v: expected {list(k.shape)}, got {list(v.shape)}")
+        if k.requires_grad or v.requires_grad:
+            _no_grad(k=k, v=v)
         dt = cache.k_pages.dtype
         rk = _rows(k, kv.kv_heads, kv.head_dim, dt, "k", self.device)
         rv = _rows(v, kv.kv_heads, kv.head_dim, dt, "v", self.device)

@@ -46,3 +46,29 @@ def test_field_changed_in_place(host):
     c.length += 2
     c.refs[1] = 5
     assert c.length.tolist() == [2, 2, 2] and c.struct.length == at == c.length.data_ptr()
+
+
+def x(*shape, grad=False):
+    return torch.zeros(shape, dtype=torch.bfloat16, requires_grad=grad)
+
+
+def off(*v):
+    return torch.tensor(v, dtype=torch.int32)
+
+
+@pytest.mark.parametrize("at", [0, 1, 2])
+def test_gradients_are_not_lost_in_silence(host, at):
+    c = host.cache(4, 16, 2, 64, 3, 2)
+    qkv = [x(4, 2, 64, grad=i == at) for i in range(3)]
+    calls = [lambda: host.attention(*qkv, off(0, 4))]
+    if at:
+        calls.append(lambda: host.cache_append(c, off(0), off(0, 4), *qkv[1:]))
+    else:
+        calls.append(lambda: host.cache_attention(c, off(0, 1, 2, 0), qkv[0]))
+    for call in calls:
+        with pytest.raises(ValueError, match="requires a gradient"):
+            call()
+        with torch.no_grad(), pytest.raises(AssertionError, match="past the checks"):
+            call()
+    with pytest.raises(AssertionError, match="past the checks"):
+        host.attention(*(t.detach() for t in qkv), off(0, 4))
