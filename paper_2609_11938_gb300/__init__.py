@@ -821,9 +821,9 @@ class Context:
         if q_offsets is None:
             if k_offsets is not None:
                 raise ValueError("k_offsets: needs q_offsets")
-            q_offsets = torch.tensor([0, tokens], dtype=torch.int32, device=self._dev)
+            q_offsets = self._ends(tokens)
             if k_tokens != tokens:
-                k_offsets = torch.tensor([0, k_tokens], dtype=torch.int32, device=self._dev)
+                k_offsets = self._ends(k_tokens)
         n_seqs = q_offsets.numel() - 1
         if n_seqs < 0:
             raise ValueError("q_offsets: expected [n_seqs + 1]")
@@ -841,6 +841,13 @@ class Context:
                             0, tokens, k_tokens, *rq, *rk, *rv, *ro, p_qo, p_ko, p_lse)
         cur = self._enter()
         return self._leave(cur, opattr_attention(self.handle, args), "opattr_attention"), out, lse
+
+    def _ends(self, tokens: int):
+        """Offsets of one sequence, made on the device: a copy of host values would wait for it."""
+        torch = _torch()
+        if tokens == 0:
+            return torch.zeros(2, dtype=torch.int32, device=self._dev)
+        return torch.arange(0, tokens + 1, tokens, dtype=torch.int32, device=self._dev)
 
     def _out(self, out, q, heads, dim, dt):
         """An output of q's shape, and its rows."""

@@ -126,3 +126,30 @@ def test_timing_and_capture(opa):
         assert torch.equal(got, want) and torch.equal(again, want)
         ms, launches = ctx.timing_report()["prompt"]
         assert launches == 2 and 0 < ms < 1e3
+
+
+@pytest.mark.parametrize("queries,keys", [(200, 200), (1, 1), (20, 300), (30, 0), (2, 9000)])
+def test_one_sequence_without_offsets(opa, queries, keys):
+    """A call without offsets does not wait for the device either, and can be captured."""
+    g = gen(44)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s), opa.Context(0, stream=s) as ctx:
+        q, k, v = (randn(g, (n, 2, 64), BF) for n in (queries, keys, keys))
+        off = [i32(0, queries), i32(0, keys)]
+        want = ctx.attention(q, k, v, *off)[1]
+        ctx.check()
+        torch.cuda.set_sync_debug_mode("error")
+        try:
+            got = ctx.attention(q, k, v)[1]
+        finally:
+            torch.cuda.set_sync_debug_mode("default")
+        ctx.check()
+        assert torch.equal(got, want)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            got = ctx.attention(q, k, v)[1]
+        got.fill_(7)
+        graph.replay()
+        ctx.check()
+        assert torch.equal(got, want)
