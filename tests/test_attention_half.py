@@ -71,3 +71,18 @@ def test_token(ctx, dtype, dim, heads, kv, page, lens):
     for i, n in enumerate(lens):
         check(out[i:i + 1], q[i:i + 1], k[a:a + n], v[a:a + n], torch.ones((1, n), dtype=torch.bool, device=DEV), f"sequence {i}")
         a += n
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("dim,n,at", [(64, 40, 7), (128, 3000, 2999), (64, 9000, 0)])
+def test_token_seen_infinite_value(ctx, dtype, dim, n, at):
+    """An infinite value that is seen is the result, in its element alone."""
+    g = gen(n)
+    c = ctx.cache(-(-n // 16), 16, 1, dim, 1, -(-n // 16), dtype)
+    k, v = (randn(g, (n, 1, dim), dtype) for _ in range(2))
+    k[:] = 0.0
+    v[at, 0, 5] = float("inf")
+    ctx.cache_append(c, torch.zeros(1, dtype=torch.int32, device=DEV), offsets([n]), k, v)
+    out = ctx.cache_attention(c, None, randn(g, (1, 4, dim), dtype))[1]
+    ctx.check()
+    assert bool((out[0, :, 5] == float("inf")).all()) and int(torch.isfinite(out).sum()) == 4 * (dim - 1)
