@@ -102,7 +102,7 @@ struct Ctrl {
     uint64_t item_full[ITEMS], item_free[ITEMS], item_want, q_full, q_free, kv_full[8], kv_free[8];
     uint64_t s_full[2], p_half[2], p_full[2], o_full[2], o_free[2], v_full[CUTS], v_ready[CUTS], met[2], drain;
     uint32_t tmem;
-    Waits waits;
+    int stop;
     int poison[CUTS];
     int last[2];
     Item item[ITEMS];
@@ -183,7 +183,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
     unsigned char *smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const uint32_t sq = smem_addr(smem), skv = sq + 2 * S::TILE;
     const int warp = threadIdx.x >> 5;
-    volatile Waits *waits = &ctl.waits;
+    volatile int *stop = &ctl.stop;
     const opattr_prompt &a = p.a;
     const uint32_t bar_kv = smem_addr(&ctl.kv_full[0]), bar_free = smem_addr(&ctl.kv_free[0]);
     if (threadIdx.x == 0) {
@@ -201,7 +201,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
         }
         for (int i = 0; i < CUTS; ++i) bar_init(smem_addr(&ctl.v_full[i]), 1), bar_init(smem_addr(&ctl.v_ready[i]), 1);
         bar_init(smem_addr(&ctl.drain), 1);
-        ctl.waits.stop = 0, ctl.waits.limit_us = p.limit_us;
+        ctl.stop = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         map_prefetch(&mq), map_prefetch(&mk), map_prefetch(&mv);
     }
@@ -215,7 +215,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
     // the next item, for a whole warp; its slot is given back by item_done
     Place<ITEMS> slot;
     auto item_next = [&](Item &it) {
-        if (!warp_wait(smem_addr(&ctl.item_full[slot.at]), slot.ph, waits)) return false;
+        if (!warp_wait(smem_addr(&ctl.item_full[slot.at]), slot.ph, stop, p.limit_us)) return false;
         it = ctl.item[slot.at];
         __syncwarp();
         if (lane_id() == 0) bar_arrive(smem_addr(&ctl.item_free[slot.at]));
@@ -239,7 +239,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
         auto meet = [&] {
             __syncwarp();
             if (lane_id() == 0) bar_arrive(smem_addr(&ctl.met[s]));
-            const bool all = warp_wait(smem_addr(&ctl.met[s]), turn_met.ph, waits);
+            const bool all = warp_wait(smem_addr(&ctl.met[s]), turn_met.ph, stop, p.limit_us);
             turn_met.step();
             return all;
         };
@@ -259,7 +259,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
             float m = -INFINITY, l = 0.f;
             for (int j = 0; j < w.n; ++j) {
                 if (j < n_tiles) {
-                    if (!(ok = warp_wait(b_s, turn_s.ph, waits))) break;
+                    if (!(ok = warp_wait(b_s, turn_s.ph, stop, p.limit_us))) break;
                     turn_s.step();
                     tm_after();
                     uint32_t x[KEYS];
@@ -335,7 +335,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                     if (a.causal && j < n_tiles) {
                         // a value that is not finite times a weight of zero would reach the rows
                         // that do not see it: such a tile's products are made here, key by key
-                        if (!(ok = warp_wait(smem_addr(&ctl.v_ready[over.at]), over.ph, waits))) break;
+                        if (!(ok = warp_wait(smem_addr(&ctl.v_ready[over.at]), over.ph, stop, p.limit_us))) break;
                         if (seldom(*(volatile int *)&ctl.poison[over.at])) {
                             const unsigned char *v = smem + 2 * S::TILE + ring.at * S::TILE;
                             const int left = (int)((unsigned)seen - j * KEYS);
@@ -383,7 +383,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
             }
             if (!ok) break;
             if (n_tiles > 0) {
-                if (!(ok = warp_wait(smem_addr(&ctl.o_full[s]), turn_o.ph, waits))) break;
+                if (!(ok = warp_wait(smem_addr(&ctl.o_full[s]), turn_o.ph, stop, p.limit_us))) break;
                 turn_o.step();
                 tm_after();
             }
@@ -447,7 +447,8 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
             }
             const float share = l == 0.f ? 0.f : 1.f / l;
             T *out = (T *)a.out.data + (int64_t)(it.q0 + row) * a.out.token_stride + head * a.out.head_stride;
-#pragma unroll 1
+            // (where no parts are joined this is short: in one piece 12,301 tokens take 810 us, in a loop 826)
+#pragma unroll (CUT ? 1 : DP / 32)
             for (int d = 0; d < DP && mine; d += 32) {
                 uint32_t o[32] = {};
                 if (joined && live) {
@@ -513,7 +514,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                     mma_commit(smem_addr(&ctl.s_full[s]));
                 }
             };
-            auto full = [&](const Place<S::STAGES> &x) { return warp_wait(bar_kv + x.at * 8, x.ph, waits); };
+            auto full = [&](const Place<S::STAGES> &x) { return warp_wait(bar_kv + x.at * 8, x.ph, stop, p.limit_us); };
             auto release = [&](int st) {
                 if (lead) mma_commit(bar_free + st * 8);
             };
@@ -533,13 +534,13 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                     if (!full(values) || (j + 1 < nt && !full(keys))) return false;
                     by_hand = false;
                     if (j >= from) {
-                        if (!warp_wait(smem_addr(&ctl.v_ready[over.at]), over.ph, waits)) return false;
+                        if (!warp_wait(smem_addr(&ctl.v_ready[over.at]), over.ph, stop, p.limit_us)) return false;
                         by_hand = a.causal && uniform(*(volatile int *)&ctl.poison[over.at]);
                         over.step();
                     }
                     return true;
                 };
-                if (!(ok = warp_wait(smem_addr(&ctl.q_full), q_turn.ph, waits) && full(keys))) break;
+                if (!(ok = warp_wait(smem_addr(&ctl.q_full), q_turn.ph, stop, p.limit_us) && full(keys))) break;
                 q_turn.step();
                 tm_after();
                 if (nt0 > 0) scores(0, keys.at);
@@ -555,10 +556,10 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                     for (int s = 0; s < 2; ++s) {
                         const int mine = s ? nt1 : nt0;
                         if (j < mine) {
-                            if (!(ok = warp_wait(smem_addr(&ctl.p_half[s]), s_turn[s].ph, waits))) break;
+                            if (!(ok = warp_wait(smem_addr(&ctl.p_half[s]), s_turn[s].ph, stop, p.limit_us))) break;
                             if (j == 0) {
                                 // the results before these have been read (a new barrier's parity 1 is over)
-                                if (!(ok = warp_wait(smem_addr(&ctl.o_free[s]), o_turn[s].ph ^ 1, waits))) break;
+                                if (!(ok = warp_wait(smem_addr(&ctl.o_free[s]), o_turn[s].ph ^ 1, stop, p.limit_us))) break;
                                 o_turn[s].step();
                             }
                             tm_after();
@@ -567,7 +568,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                                 for (int k = 0; k < KEYS / 32; ++k)
                                     mma_ts(tm + 256 + s * DP, tm + s * 128 + 8 * k, vd + k * 128, DO, k > 0 || j > 0);
                             }
-                            if (!(ok = warp_wait(smem_addr(&ctl.p_full[s]), s_turn[s].ph, waits))) break;
+                            if (!(ok = warp_wait(smem_addr(&ctl.p_full[s]), s_turn[s].ph, stop, p.limit_us))) break;
                             s_turn[s].step();
                             tm_after();
                             if (!hand && lead) {
@@ -590,8 +591,8 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
             }
             // nothing of this thread's is under way when the block ends
             if (lead) mma_commit(smem_addr(&ctl.drain));
-            Waits last{0, p.limit_us};
-            bar_wait(smem_addr(&ctl.drain), 0, &last);
+            int last = 0;
+            bar_wait(smem_addr(&ctl.drain), 0, &last, p.limit_us);
         } else if (warp == LOAD_WARP) {
             // ---- tile copies: one thread
             const bool lead = elect();
@@ -624,7 +625,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                     if (lead && load == ask) bar_arrive(smem_addr(&ctl.item_want));
                     if (q_due && (load == S::STAGES - 2 || load == 2 * w.n - 1 ||
                                   __all_sync(0xffffffffu, bar_is_done(smem_addr(&ctl.q_free), q_turn.ph ^ 1)))) {
-                        if (!(ok = warp_wait(smem_addr(&ctl.q_free), q_turn.ph ^ 1, waits))) break;
+                        if (!(ok = warp_wait(smem_addr(&ctl.q_free), q_turn.ph ^ 1, stop, p.limit_us))) break;
                         q_turn.step();
                         q_due = false;
                         if (lead) {
@@ -636,7 +637,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                         }
                         q_out = 1;
                     }
-                    if (!(ok = warp_wait(bar_free + 8 * ring.at, ring.ph ^ 1, waits))) break;
+                    if (!(ok = warp_wait(bar_free + 8 * ring.at, ring.ph ^ 1, stop, p.limit_us))) break;
                     // K0, V0, K1, V1, ..; values that are looked over have a barrier of their own: the
                     // stage's may have gone round several times before the tail's warp sees it
                     const bool keys = load % 2 == 0, cut = !keys && load / 2 >= w.cut;
@@ -655,10 +656,10 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                 }
             }
             // the block ends with no copy under way: where a wait gave up, nobody else waits for them
-            Waits last{0, p.limit_us};
+            int last = 0;
             for (int i = 0; i < S::STAGES; ++i)
-                if (bars[i]) bar_wait(bars[i], pars[i], &last);
-            if (q_out) bar_wait(bq, q_turn.ph ^ 1, &last);
+                if (bars[i]) bar_wait(bars[i], pars[i], &last, p.limit_us);
+            if (q_out) bar_wait(bq, q_turn.ph ^ 1, &last, p.limit_us);
         } else if (warp == TAIL_WARP) {
             // ---- value tiles that a mask cuts: rows past the sequence's keys become zeros, and,
             // causal, the others are looked over for values that are not finite
@@ -672,7 +673,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                 const Work w(it, p.span, a.causal);
                 for (int j = 0; j < w.n; ++j, ring.step(), ring.step()) {
                     if (j < w.cut) continue;
-                    if (!(ok = warp_wait(smem_addr(&ctl.v_full[over.at]), over.ph, waits))) break;
+                    if (!(ok = warp_wait(smem_addr(&ctl.v_full[over.at]), over.ph, stop, p.limit_us))) break;
                     uint4 *v = reinterpret_cast<uint4 *>(smem + 2 * S::TILE + ring.at * S::TILE);
                     const int keys = min(KEYS, it.lk - j * KEYS);
                     unsigned most = 0;
@@ -763,14 +764,14 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                     i = draw(p.next, total);
                 }
                 more = it.some != 0;
-                if (!warp_wait(smem_addr(&ctl.item_free[slot.at]), slot.ph ^ 1, waits)) break;
+                if (!warp_wait(smem_addr(&ctl.item_free[slot.at]), slot.ph ^ 1, stop, p.limit_us)) break;
                 if (lane_id() == 0) {
                     ctl.item[slot.at] = it;
                     bar_arrive(smem_addr(&ctl.item_full[slot.at]));
                 }
                 slot.step();
                 if (more) {
-                    if (!warp_wait(smem_addr(&ctl.item_want), wanted.ph, waits)) break;
+                    if (!warp_wait(smem_addr(&ctl.item_want), wanted.ph, stop, p.limit_us)) break;
                     wanted.step();
                     i = CUT ? i + 1 : draw(p.next, total);
                 }
@@ -786,7 +787,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
     }
     tm_before();
     __syncthreads();
-    if (threadIdx.x == 0 && waits->stop) atomicOr(err, SERVE_TIMEOUT);
+    if (threadIdx.x == 0 && *stop) atomicOr(err, SERVE_TIMEOUT);
     __syncwarp();
     if (warp == MMA_WARP) tm_free(ctl.tmem, 512);
 }

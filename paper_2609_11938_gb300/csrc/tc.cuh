@@ -36,11 +36,6 @@ __device__ __forceinline__ bool bar_is_done(uint32_t bar, unsigned phase) {
                  : "=r"(ok) : "r"(bar), "r"(phase) : "memory");
     return ok;
 }
-// A block's waits, in its shared memory: whether one of them gave up, and how long each may take.
-struct Waits {
-    int stop;
-    unsigned limit_us;
-};
 // Waits until the phase is over; gives up after the limit, or once another warp of the
 // block gave up.  The sleeps are long: warps that poll take issue slots from those that
 // compute.
@@ -50,20 +45,20 @@ __device__ __forceinline__ unsigned long long clock_ns() {
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
     return t;
 }
-__device__ __forceinline__ bool bar_wait_on(uint32_t bar, unsigned phase, volatile Waits *w) {
-    const unsigned long long t0 = clock_ns(), limit = w->limit_us * 1000ull;
-    while (!w->stop && clock_ns() - t0 < limit)
+__device__ __forceinline__ bool bar_wait_on(uint32_t bar, unsigned phase, volatile int *stop, unsigned limit_us) {
+    const unsigned long long t0 = clock_ns(), limit = limit_us * 1000ull;
+    while (!*stop && clock_ns() - t0 < limit)
         if (bar_done(bar, phase, SLEEP_NS)) return true;
-    w->stop = 1;
+    *stop = 1;
     return false;
 }
-__device__ __forceinline__ bool bar_wait(uint32_t bar, unsigned phase, volatile Waits *w) {
-    if (seldom(!bar_done(bar, phase, SLEEP_NS))) return bar_wait_on(bar, phase, w);
+__device__ __forceinline__ bool bar_wait(uint32_t bar, unsigned phase, volatile int *stop, unsigned limit_us) {
+    if (seldom(!bar_done(bar, phase, SLEEP_NS))) return bar_wait_on(bar, phase, stop, limit_us);
     return true;
 }
 // The same for a whole warp that goes on together.
-__device__ __forceinline__ bool warp_wait(uint32_t bar, unsigned phase, volatile Waits *w) {
-    return __all_sync(0xffffffffu, bar_wait(bar, phase, w));
+__device__ __forceinline__ bool warp_wait(uint32_t bar, unsigned phase, volatile int *stop, unsigned limit_us) {
+    return __all_sync(0xffffffffu, bar_wait(bar, phase, stop, limit_us));
 }
 
 // ---------------------------------------------------------------- tile copies
