@@ -539,7 +539,8 @@ k_compact_place(opattr_cache kv, const int32_t *tile_live, int tiles, int32_t *r
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         const int64_t i = at + q;
-        if (i < L && r[q] == 0) hole[i - live] = (int)i;
+        // (every page is live or a hole, a count below 0 too: as many holes as pages that move)
+        if (i < L && r[q] <= 0) hole[i - live] = (int)i;
         if (i >= L && r[q] > 0) {
             rank[i] = live - below;
             mover[live - below] = (int)i;
