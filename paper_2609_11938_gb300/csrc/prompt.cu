@@ -21,13 +21,13 @@
 // size of the result's own rounding.
 //
 // Measured on one GB300 (bfloat16, causal unless said): 12,301 tokens, 32 heads of 128 on 8:
-// 770 us, 1,610 TFLOP/s; 9,728, 16 heads on 4, all keys seen: 470 us, 1,645 (there the
-// power limit holds the clock at 1.6 GHz and the tensor cores are busy for three
-// quarters of the cycles); 16 heads of 64: 405 us, 955.  At width 64 a tile's exponentials
-// and its trips through tensor memory (1,500 cycles of a group, of them 512 of the
-// special function unit) take longer than its products (512), and short prompts wait
-// for one tile's chain of steps: 8 x 512 tokens, 8 heads of 64, all seen, 17,600 cycles,
-// of which four tiles are 9,200.
+// 821 us among other calls, 1,510 TFLOP/s (790 in short bursts, 815 held for seconds); 9,728, 16
+// heads on 4, all keys seen: 504 us, 1,540.  The power limit is active there, at 1.86 GHz; of
+// the 3,040 cycles that a tile of both sub-tiles takes the products have 2,048.  16 heads of 64:
+// 383 us, 1,010: a tile's 2,320 cycles have 1,024 of products and 1,024 of the special function
+// unit, and the chain from scores through tensor memory to weights sets the pace.  Short prompts
+// wait for it: 8 x 512 tokens, 8 heads of 64, all seen, 17,000 cycles, 4,300 of them before
+// the first product, 11,700 for four tiles one after another.
 #include <math.h>
 
 #include <algorithm>
