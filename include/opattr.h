@@ -524,11 +524,12 @@ opattr_status opattr_match_noalloc(const opattr_kernels *kernels, const opattr_n
  * attention calls: a sequence id or length out of range gives rows of zeros,
  * a page out of range counts as not seen); opattr_check tells.
  *
- * Values are bfloat16 or IEEE half; products are summed, and the softmax is
- * held, in 32 bits; its weights are rounded to the values' type before they
- * are multiplied with the values, and the results once at the end.  A key
+ * Values are bfloat16 or IEEE half (a cache's pages may hold them in 8 bits,
+ * below); products are summed, and the softmax is held, in 32 bits; its weights
+ * are rounded to the values' type before they are multiplied with the values
+ * (to half where those are of 8 bits), and the results once at the end.  A key
  * outside a row's mask has no influence on it, whatever it holds. */
-typedef enum { OPATTR_BF16 = 0, OPATTR_F16 = 1 } opattr_dtype;
+typedef enum { OPATTR_BF16 = 0, OPATTR_F16 = 1, OPATTR_E4M3 = 2 /* pages of an opattr_cache8 alone */ } opattr_dtype;
 
 /* Rows of heads, DEVICE memory: element e of head h of row t is
  * data[t * token_stride + h * head_stride + e].  Strides count elements and
@@ -573,6 +574,13 @@ typedef struct {
  * OPATTR_E_CUDA. */
 opattr_status opattr_attention(opattr_ctx *ctx, const opattr_prompt *args);
 
+/* The same through a sliding window: a query sees, of the keys that it would
+ * see (`causal` is set), the last `window` ones, its own among them, and the
+ * sequence's first `sinks`.  Keys that no row of a tile sees are not read.
+ * window is at least 1, sinks at least 0.
+ * Errors: as opattr_attention; `causal` not set is OPATTR_E_INVALID_ARG. */
+opattr_status opattr_attention_window(opattr_ctx *ctx, const opattr_prompt *args, int32_t window, int32_t sinks);
+
 /* A paged key-value cache; everything in it is the caller's DEVICE memory.
  *   k_pages, v_pages  [n_pages][kv_heads][page_size][head_dim], 16-byte aligned
  *   table    i32[n_seqs][pages_per_seq]: page of each page_size tokens of a
@@ -598,6 +606,29 @@ typedef struct {
     int32_t *low;
 } opattr_cache;
 
+/* A cache whose pages hold 8 bits an element: `pages` with dtype OPATTR_E4M3,
+ * and what follows it here.  Every call that takes a cache takes &c.pages of one.
+ * The element that code x of a page stands for is x (4 bits of exponent, 3 of
+ * mantissa, at most 448, NaN) times its block's scale, a block being
+ * OPATTR_SCALE_TOKENS tokens of one head, from a multiple of that on:
+ *   k_scales, v_scales  f32[n_pages][kv_heads][page_size / OPATTR_SCALE_TOKENS]
+ *   rows   opattr_dtype of the rows that calls bring and take (q, out, k, v)
+ * head_dim is a multiple of 16.  opattr_cache_append gives a block, by the
+ * finite elements of the rows that it brings to it, the least power of two from
+ * 2^-126 to 2^119 that takes the largest to 448 at most; one that had tokens
+ * before keeps its scale where that is larger, and where it is not, their codes
+ * are rounded anew for the larger one (exact, but for those below 2^-6 after
+ * that, where scales are powers of two).  An element is rounded to nearest
+ * even, one above 448 becomes 448, and one that is not finite NaN. */
+#define OPATTR_SCALE_TOKENS 16
+typedef struct {
+    opattr_cache pages;
+    float *k_scales;
+    float *v_scales;
+    int32_t rows;
+    int32_t reserved;
+} opattr_cache8;
+
 /* One new query per sequence over the cache: row i of q and out is sequence
  * seqs[i] (i32[n] device, repeats allowed; NULL: sequence i), which sees all
  * of its length.  lse f32[n * q_heads] device, may be NULL.  A length of 0
@@ -606,6 +637,13 @@ typedef struct {
 opattr_status opattr_cache_attention(opattr_ctx *ctx, const opattr_cache *cache, const int32_t *seqs, int32_t n,
                                      int32_t q_heads, const opattr_rows *q, const opattr_rows *out, float *lse,
                                      float scale);
+
+/* The same through a sliding window: of its sequence a query sees the last
+ * `window` tokens and the first `sinks`; the others are not read.
+ * window is at least 1, sinks at least 0.  Errors: as opattr_attention. */
+opattr_status opattr_cache_attention_window(opattr_ctx *ctx, const opattr_cache *cache, const int32_t *seqs, int32_t n,
+                                            int32_t q_heads, const opattr_rows *q, const opattr_rows *out, float *lse,
+                                            float scale, int32_t window, int32_t sinks);
 
 /* Rows offsets[i] .. offsets[i + 1] of k and v (i32[n + 1] device, from 0 to
  * tokens, not decreasing) to the end of sequence seqs[i] (i32[n] device, each

@@ -27,6 +27,7 @@ __all__ = [
     "opattr_create", "opattr_enclose", "opattr_match", "opattr_aggregate", "opattr_join", "opattr_destroy",
     "opattr_status_string", "opattr_match_noalloc", "MATCH_NOALLOC_MAX", "opattr_attention", "opattr_cache_attention",
     "opattr_cache_append", "opattr_cache_fork", "opattr_cache_trim", "opattr_cache_compact", "opattr_check",
+    "opattr_attention_window", "opattr_cache_attention_window", "SCALE_TOKENS",
 ]
 
 OK, W_COUNT_MISMATCH, W_DEDUP_MISMATCH = 0, 1, 2
@@ -38,6 +39,7 @@ N_COUNTERS = 20
 OP_NONE = 0xFFFFFFFF
 TIER_NONE, TIER_HIGH, TIER_NVTX, TIER_INDUCTOR = 0, 1, 2, 3
 MATCH_NOALLOC_MAX = 65536
+SCALE_TOKENS = 16                # tokens of a head that share a scale in pages of 8 bits
 MISMATCH = {"skip_name": 0, "prefix": 1, "error": 2}
 
 _vp = ctypes.c_void_p
@@ -138,6 +140,10 @@ class Cache(ctypes.Structure):
                [(f, _vp) for f in ("k_pages", "v_pages", "table", "length", "refs", "low")]
 
 
+class Cache8(Cache):
+    _fields_ = [("k_scales", _vp), ("v_scales", _vp), ("rows", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
 _lib_lock = threading.Lock()
 _lib = None
 
@@ -196,10 +202,13 @@ def library():
             lib.opattr_cache_trim.argtypes = [_vp, _vp, _vp, _vp, i32]
             lib.opattr_cache_compact.argtypes = [_vp, _vp, _vp]
             lib.opattr_check.argtypes = [_vp]
+            lib.opattr_attention_window.argtypes = [_vp, _vp, i32, i32]
+            lib.opattr_cache_attention_window.argtypes = [_vp, _vp, _vp, i32, i32, _vp, _vp, _vp, f32, i32, i32]
             for f in ("opattr_create", "opattr_enclose", "opattr_match", "opattr_aggregate", "opattr_attribute",
                       "opattr_rollup", "opattr_set_timing", "opattr_timing_report", "opattr_attention",
                       "opattr_cache_attention", "opattr_cache_append", "opattr_cache_fork", "opattr_cache_trim",
-                      "opattr_cache_compact", "opattr_check"):
+                      "opattr_cache_compact", "opattr_check", "opattr_attention_window",
+                      "opattr_cache_attention_window"):
                 getattr(lib, f).restype = ctypes.c_int
             _lib = lib
         return _lib
@@ -334,6 +343,18 @@ def opattr_cache_attention(handle, cache, seqs_ptr: int | None, n: int, q_heads:
                            scale: float) -> int:
     """cache: a Cache by reference; q, out: Rows by reference, or their bytes."""
     return (_lib or library()).opattr_cache_attention(handle, cache, seqs_ptr, n, q_heads, q, out, lse_ptr, scale)
+
+
+def opattr_attention_window(handle, args, window: int, sinks: int) -> int:
+    """args: a Prompt (by reference) or its bytes."""
+    return (_lib or library()).opattr_attention_window(handle, args, window, sinks)
+
+
+def opattr_cache_attention_window(handle, cache, seqs_ptr: int | None, n: int, q_heads: int, q, out,
+                                  lse_ptr: int | None, scale: float, window: int, sinks: int) -> int:
+    """cache, q, out: as opattr_cache_attention."""
+    return (_lib or library()).opattr_cache_attention_window(handle, cache, seqs_ptr, n, q_heads, q, out, lse_ptr, scale,
+                                                             window, sinks)
 
 
 def opattr_cache_append(handle, cache, seqs_ptr: int, n: int, offsets_ptr: int, tokens: int, k, v) -> int:
@@ -483,6 +504,19 @@ def _rows(t, heads: int | None, dim: int, like, name, device):
     return p, st, sh
 
 
+_E4M3 = 2                        # opattr_dtype of pages of 8 bits
+_INT_MAX = 0x7fffffff
+
+
+def _window(window, sinks: int):
+    """The arguments of a sliding window."""
+    if window is None:
+        if sinks:
+            raise ValueError("sinks: without a window every key is seen")
+    elif not 1 <= window <= _INT_MAX or not 0 <= sinks <= _INT_MAX:
+        raise ValueError(f"window, sinks: expected at least 1 and 0, and less than 2^31, got {window} and {sinks}")
+
+
 def _no_grad(**tensors):
     """These operators have no backward pass: where gradients are recorded, a
     result that is cut off from its inputs in silence would be wrong."""
@@ -502,13 +536,18 @@ def _distinct(t, name):
 class KVCache:
     """A paged key-value cache as device tensors (opattr_cache in
     include/opattr.h has the layouts); Context.cache makes an empty one.  A field
-    may be replaced by another tensor that fits the others."""
-    k_pages: object                 # [n_pages, kv_heads, page_size, head_dim] bfloat16 or float16
+    may be replaced by another tensor that fits the others.  Pages of
+    float8_e4m3fn hold elements in units of a scale, one for each SCALE_TOKENS
+    tokens of a head (opattr_cache8): rows that are appended are rounded for it, and
+    queries, rows and results may be bfloat16 or float16, call by call."""
+    k_pages: object                 # [n_pages, kv_heads, page_size, head_dim] bfloat16, float16 or float8_e4m3fn
     v_pages: object
     table: object                   # int32 [n_seqs, pages_per_seq], -1 past a sequence's length
     length: object                  # int32 [n_seqs]
     refs: object                    # int32 [n_pages]: sequences that hold a page
     low: object                     # int32 [1]: no page below it is free
+    k_scales: object = None         # (8 bits) float32 [n_pages, kv_heads, page_size / SCALE_TOKENS]
+    v_scales: object = None
 
     def __post_init__(self):
         self._lay_out()
@@ -529,22 +568,43 @@ class KVCache:
         dv = self.k_pages.get_device()
         if self.k_pages.dim() != 4 or self.v_pages.shape != self.k_pages.shape:
             raise ValueError("k_pages, v_pages: expected one shape [n_pages, kv_heads, page_size, head_dim]")
-        dtype = _dtype(self.k_pages, "k_pages")
-        n, g, page, dim = self.k_pages.shape
         torch = _torch()
+        e8 = self.k_pages.dtype is torch.float8_e4m3fn
+        dtype = _E4M3 if e8 else _dtype(self.k_pages, "k_pages")
+        n, g, page, dim = self.k_pages.shape
         if page < 16 or page > 1024 or page & (page - 1):
             raise ValueError(f"page_size: expected a power of two from 16 to 1024, got {page}")
         if dim < 8 or dim > 128 or dim % 8:
             raise ValueError(f"head_dim: expected a multiple of 8 from 8 to 128, got {dim}")
+        if e8 and dim % 16:
+            raise ValueError(f"head_dim: expected a multiple of 16 for pages of 8 bits, got {dim}")
+        if (self.k_scales is None) == e8 or (self.v_scales is None) == e8:
+            raise ValueError("k_scales, v_scales: needed for pages of 8 bits, and for no others")
+        if e8 and any(x.shape != (n, g, page // SCALE_TOKENS) for x in (self.k_scales, self.v_scales)):
+            raise ValueError(f"k_scales, v_scales: expected {[n, g, page // SCALE_TOKENS]}")
         if self.table.dim() != 2 or self.length.shape != (self.table.shape[0],) or self.refs.shape != (n,) or \
                 self.low.numel() != 1 or n < 1 or g < 1 or self.table.numel() < 1:
             raise ValueError("expected table [n_seqs, pages_per_seq], length [n_seqs], refs [n_pages], low [1]")
-        self.struct = Cache(dtype, page, g, dim, self.table.shape[0], self.table.shape[1], n,
-                            _ptr(self.k_pages, self.k_pages.dtype, "k_pages", dv),
-                            _ptr(self.v_pages, self.k_pages.dtype, "v_pages", dv),
-                            _ptr(self.table, torch.int32, "table", dv), _ptr(self.length, torch.int32, "length", dv),
-                            _ptr(self.refs, torch.int32, "refs", dv), _ptr(self.low, torch.int32, "low", dv))
-        self.device, self.by_ref = dv, ctypes.byref(self.struct)
+        fields = [dtype, page, g, dim, self.table.shape[0], self.table.shape[1], n,
+                  _ptr(self.k_pages, self.k_pages.dtype, "k_pages", dv),
+                  _ptr(self.v_pages, self.k_pages.dtype, "v_pages", dv),
+                  _ptr(self.table, torch.int32, "table", dv), _ptr(self.length, torch.int32, "length", dv),
+                  _ptr(self.refs, torch.int32, "refs", dv), _ptr(self.low, torch.int32, "low", dv)]
+        if e8:
+            fields += [_ptr(self.k_scales, torch.float32, "k_scales", dv), _ptr(self.v_scales, torch.float32, "v_scales", dv)]
+        kind = Cache8 if e8 else Cache
+        # (pages of 8 bits: one for rows of either type, so that calls do not change what others read)
+        structs = [kind(*fields, r) for r in (0, 1)] if e8 else [kind(*fields)]
+        self.struct, self.device, self.by_ref = structs[0], dv, ctypes.byref(structs[0])
+        self.for_rows = {torch.bfloat16: self.by_ref, torch.float16: ctypes.byref(structs[1])} if e8 else \
+            {self.k_pages.dtype: self.by_ref}
+
+    def _rows_of(self, t, name):
+        """The struct for a call that brings rows of t's type."""
+        by_ref = self.for_rows.get(t.dtype)
+        if by_ref is None:
+            raise TypeError(f"{name}: expected {' or '.join(map(str, self.for_rows))}, got {t.dtype}")
+        return by_ref
 
 
 class Context:
@@ -794,14 +854,20 @@ class Context:
         return _ptr(t, _torch().int32, name, self.device) or 0
 
     def attention(self, q, k, v, q_offsets=None, k_offsets=None, causal: bool = True, scale: float | None = None,
-                  out=None, need_lse: bool = False):
+                  out=None, need_lse: bool = False, window: int | None = None, sinks: int = 0):
         """Attention over packed sequences (opattr_attention): q [tokens, heads,
         dim], k and v [tokens, kv_heads, dim]; offsets int32 [n_seqs + 1] on the
         device (none: one sequence; k_offsets none: q_offsets).  scale: by
-        default 1 / sqrt(dim).  No backward pass: inputs that require a gradient
+        default 1 / sqrt(dim).  window (with causal): a query sees the last `window`
+        keys up to its own, and its sequence's first `sinks` (opattr_attention_window).
+        No backward pass: inputs that require a gradient
         are refused where gradients are recorded.  Returns (status, out, lse or None)."""
         torch = _torch()
         dv = self.device
+        if window is not None or sinks:
+            _window(window, sinks)
+            if not causal:
+                raise ValueError("window: needs causal")
         qs, ks = q.shape, k.shape
         if len(qs) != 3 or len(ks) != 3:
             raise ValueError("q, k: expected [tokens, heads, dim]")
@@ -840,6 +906,8 @@ class Context:
         args = _PROMPT.pack(dtype, n_seqs, heads, kv_heads, dim, 1 if causal else 0, dim ** -0.5 if scale is None else scale,
                             0, tokens, k_tokens, *rq, *rk, *rv, *ro, p_qo, p_ko, p_lse)
         cur = self._enter()
+        if window is not None:
+            return self._leave(cur, opattr_attention_window(self.handle, args, window, sinks), "opattr_attention_window"), out, lse
         return self._leave(cur, opattr_attention(self.handle, args), "opattr_attention"), out, lse
 
     def _ends(self, tokens: int):
@@ -863,25 +931,34 @@ class Context:
     def cache(self, n_pages: int, page_size: int, kv_heads: int, head_dim: int, n_seqs: int, pages_per_seq: int,
               dtype=None) -> KVCache:
         """An empty cache of `n_pages` pages for `n_seqs` sequences of at most
-        pages_per_seq pages each (dtype: by default torch.bfloat16)."""
+        pages_per_seq pages each (dtype: by default torch.bfloat16; torch.float8_e4m3fn
+        holds them in 8 bits with a scale for each SCALE_TOKENS tokens of a head)."""
         torch = _torch()
         new = lambda shape, value: torch.full(shape, value, dtype=torch.int32, device=self._dev)  # noqa: E731
         pool = [torch.zeros((n_pages, kv_heads, page_size, head_dim), dtype=dtype or torch.bfloat16, device=self._dev)
                 for _ in range(2)]
-        return KVCache(*pool, new((n_seqs, pages_per_seq), -1), new((n_seqs,), 0), new((n_pages,), 0), new((1,), 0))
+        scales = [torch.zeros((n_pages, kv_heads, page_size // SCALE_TOKENS), dtype=torch.float32, device=self._dev)
+                  for _ in range(2)] if dtype is torch.float8_e4m3fn else []
+        return KVCache(*pool, new((n_seqs, pages_per_seq), -1), new((n_seqs,), 0), new((n_pages,), 0), new((1,), 0), *scales)
 
     def _cache(self, cache: KVCache) -> Cache:
         if cache.device != self.device:
             raise ValueError(f"cache: must live on cuda:{self.device}")
         return cache.struct
 
-    def cache_attention(self, cache: KVCache, seqs, q, scale: float | None = None, out=None, need_lse: bool = False):
+    def cache_attention(self, cache: KVCache, seqs, q, scale: float | None = None, out=None, need_lse: bool = False,
+                        window: int | None = None, sinks: int = 0):
         """Attention of one new token per sequence over the cache
         (opattr_cache_attention): q [n, heads, dim], row i of sequence seqs[i]
-        (int32 [n], or None: sequence i).  Returns (status, out, lse or None)."""
+        (int32 [n], or None: sequence i).  window: of its sequence a query sees the
+        last `window` tokens and the first `sinks` (opattr_cache_attention_window).
+        Returns (status, out, lse or None)."""
         torch = _torch()
+        if window is not None or sinks:
+            _window(window, sinks)
         kv = self._cache(cache)
-        dim, dt = kv.head_dim, cache.k_pages.dtype
+        by_ref = cache._rows_of(q, "q")
+        dim, dt = kv.head_dim, q.dtype
         rq = _rows(q, None, dim, dt, "q", self.device)
         n, heads, _ = q.shape
         if heads < 1 or heads % kv.kv_heads:
@@ -896,26 +973,31 @@ class Context:
             lse = torch.empty((n, heads), dtype=torch.float32, device=self._dev)
             p_lse = lse.data_ptr()
         p_seqs = self._i32(seqs, n, "seqs")
+        args = (self.handle, by_ref, p_seqs, n, heads, _ROWS.pack(*rq), _ROWS.pack(*ro), p_lse, dim ** -0.5 if scale is None else scale)
         cur = self._enter()
-        st = opattr_cache_attention(self.handle, cache.by_ref, p_seqs, n, heads, _ROWS.pack(*rq), _ROWS.pack(*ro), p_lse, dim ** -0.5 if scale is None else scale)
-        return self._leave(cur, st, "opattr_cache_attention"), out, lse
+        if window is not None:
+            return self._leave(cur, opattr_cache_attention_window(*args, window, sinks), "opattr_cache_attention_window"), out, lse
+        return self._leave(cur, opattr_cache_attention(*args), "opattr_cache_attention"), out, lse
 
     def cache_append(self, cache: KVCache, seqs, offsets, k, v) -> int:
         """Rows offsets[i] .. offsets[i + 1] of k and v ([tokens, kv_heads, dim])
-        to the end of sequence seqs[i], each sequence once (opattr_cache_append)."""
+        to the end of sequence seqs[i], each sequence once (opattr_cache_append).
+        Pages of 8 bits: the rows are rounded on their way in, for a scale of each
+        SCALE_TOKENS tokens of a head, which may round their last codes anew."""
         kv = self._cache(cache)
+        by_ref = cache._rows_of(k, "k")
         if v.shape != k.shape:
             raise ValueError(f"v: expected {list(k.shape)}, got {list(v.shape)}")
         if k.requires_grad or v.requires_grad:
             _no_grad(k=k, v=v)
-        dt = cache.k_pages.dtype
+        dt = k.dtype
         rk = _rows(k, kv.kv_heads, kv.head_dim, dt, "k", self.device)
         rv = _rows(v, kv.kv_heads, kv.head_dim, dt, "v", self.device)
         p_seqs = self._i32(seqs, None, "seqs")
         n = seqs.shape[0]
         p_off = self._i32(offsets, n + 1, "offsets")
         cur = self._enter()
-        st = opattr_cache_append(self.handle, cache.by_ref, p_seqs, n, p_off, k.shape[0],
+        st = opattr_cache_append(self.handle, by_ref, p_seqs, n, p_off, k.shape[0],
                                  _ROWS.pack(*rk), _ROWS.pack(*rv))
         return self._leave(cur, st, "opattr_cache_append")
 

@@ -39,10 +39,10 @@ opattr_status do_rollup(Ctx &c, const opattr_kernels *kern, const opattr_ranges 
                         const opattr_ncu *ncu, const int32_t *nidx, uint32_t n_ops, const uint32_t *class_of_op,
                         uint32_t n_classes, const opattr_op_aggregates *out);
 
-opattr_status do_attention(Ctx &c, Serve &s, const opattr_prompt *a);
+opattr_status do_attention(Ctx &c, Serve &s, const opattr_prompt *a, int32_t window, int32_t sinks);
 opattr_status do_cache_attention(Ctx &c, Serve &s, const opattr_cache *kv, const int32_t *seqs, int32_t n,
                                  int32_t q_heads, const opattr_rows *q, const opattr_rows *out, float *lse,
-                                 float scale);
+                                 float scale, int32_t window, int32_t sinks);
 opattr_status do_cache_append(Ctx &c, Serve &s, const opattr_cache *kv, const int32_t *seqs, int32_t n,
                               const int32_t *offsets, int64_t tokens, const opattr_rows *k, const opattr_rows *v);
 opattr_status do_cache_fork(Ctx &c, Serve &s, const opattr_cache *kv, const int32_t *src, const int32_t *dst, int32_t n);
@@ -638,7 +638,17 @@ opattr_status opattr_attention(opattr_ctx *ctx, const opattr_prompt *args) {
     if (c.broken) return OPATTR_E_STATE;
     DeviceGuard g(c.device);
     if (!g.ok) return OPATTR_E_CUDA;
-    return finish(c, do_attention(c, ctx->serve, args));
+    return finish(c, do_attention(c, ctx->serve, args, 0, 0));
+}
+
+opattr_status opattr_attention_window(opattr_ctx *ctx, const opattr_prompt *args, int32_t window, int32_t sinks) {
+    NvtxCall nvtx("opattr_attention_window");
+    if (!ctx || !args || window < 1 || sinks < 0 || !args->causal) return OPATTR_E_INVALID_ARG;
+    Ctx &c = ctx->c;
+    if (c.broken) return OPATTR_E_STATE;
+    DeviceGuard g(c.device);
+    if (!g.ok) return OPATTR_E_CUDA;
+    return finish(c, do_attention(c, ctx->serve, args, window, sinks));
 }
 
 opattr_status opattr_cache_attention(opattr_ctx *ctx, const opattr_cache *cache, const int32_t *seqs, int32_t n,
@@ -650,7 +660,19 @@ opattr_status opattr_cache_attention(opattr_ctx *ctx, const opattr_cache *cache,
     if (c.broken) return OPATTR_E_STATE;
     DeviceGuard g(c.device);
     if (!g.ok) return OPATTR_E_CUDA;
-    return finish(c, do_cache_attention(c, ctx->serve, cache, seqs, n, q_heads, q, out, lse, scale));
+    return finish(c, do_cache_attention(c, ctx->serve, cache, seqs, n, q_heads, q, out, lse, scale, 0, 0));
+}
+
+opattr_status opattr_cache_attention_window(opattr_ctx *ctx, const opattr_cache *cache, const int32_t *seqs, int32_t n,
+                                            int32_t q_heads, const opattr_rows *q, const opattr_rows *out, float *lse,
+                                            float scale, int32_t window, int32_t sinks) {
+    NvtxCall nvtx("opattr_cache_attention_window");
+    if (!ctx || !cache || !q || !out || window < 1 || sinks < 0) return OPATTR_E_INVALID_ARG;
+    Ctx &c = ctx->c;
+    if (c.broken) return OPATTR_E_STATE;
+    DeviceGuard g(c.device);
+    if (!g.ok) return OPATTR_E_CUDA;
+    return finish(c, do_cache_attention(c, ctx->serve, cache, seqs, n, q_heads, q, out, lse, scale, window, sinks));
 }
 
 opattr_status opattr_cache_append(opattr_ctx *ctx, const opattr_cache *cache, const int32_t *seqs, int32_t n,

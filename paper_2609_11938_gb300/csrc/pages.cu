@@ -19,6 +19,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "serve.cuh"
 
@@ -31,7 +32,10 @@ constexpr int COPY_THREADS = 256;
 constexpr int ROWS_AHEAD = 2;
 
 bool cache_ok(const opattr_cache *k) {
-    if (k->dtype != OPATTR_BF16 && k->dtype != OPATTR_F16) return false;
+    const opattr_cache8 *e8 = cache8(k);
+    const int rows = e8 ? e8->rows : k->dtype;
+    if (rows != OPATTR_BF16 && rows != OPATTR_F16) return false;
+    if (e8 && (k->head_dim % 16 || !e8->k_scales || !e8->v_scales)) return false;
     if (k->page_size < 16 || k->page_size > 1024 || (k->page_size & (k->page_size - 1))) return false;
     if (k->kv_heads < 1 || k->head_dim < 8 || k->head_dim > 128 || k->head_dim % 8) return false;
     if (k->n_seqs < 1 || k->pages_per_seq < 1 || k->n_pages < 1 || k->n_pages > INT32_MAX) return false;
@@ -97,12 +101,14 @@ struct AppendPlan {
     int32_t room;       // entries of fresh
 };
 
+// `align`: a sequence that appends writes from a multiple of it on (pages of 8 bits: the block
+// that its first row falls into may get a new scale).
 // One block: a call has few sequences, and their new pages are found where the
 // lowest free ones are (`low`: none below it is free), four reference counts to a
 // thread at a time.
 __global__ void __launch_bounds__(PLAN_THREADS)
 k_append_plan(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offsets, int tokens, AppendPlan p,
-              unsigned *err) {
+              int align, unsigned *err) {
     constexpr int HELD = 2048;
     __shared__ int warp_buf[33], held_page[HELD];
     __shared__ uint16_t held_part[HELD];
@@ -157,7 +163,7 @@ k_append_plan(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offset
                 for (int k = HELD; k < i; ++k)
                     if (p.to[k] == last) --held, longest = max(longest, p.old[k] % kv.page_size);
                 if (held > 1) from = last;
-                else if (longest > old % kv.page_size) late = last;
+                else if (longest > old % kv.page_size / align * align) late = last;
             }
             p.from[i] = from;
             p.late[i] = late;
@@ -303,16 +309,207 @@ k_append_rows(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offset
     }
 }
 
+// ---------------------------------------------------------------- rows into pages of 8 bits
+constexpr int BLOCK = OPATTR_SCALE_TOKENS;
+
+// Two values to codes, `lo` in the low byte: nearest even, at most 448, NaN stays.
+__device__ __forceinline__ uint32_t codes2(float lo, float hi) {
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ float2 values2(uint32_t two) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)two));
+    return Type2<__half>::up(r);
+}
+// The least power of two, from 2^-126 to 2^119, that takes `top` (finite) to 448 = 1.75 * 2^8 at most.
+__device__ __forceinline__ float scale_for(float top) {
+    const int bits = __float_as_int(top), e = (bits >> 23) - 127 - 8 + ((bits & 0x7fffff) > 0x600000);
+    return __int_as_float((min(119, max(-126, e)) + 127) << 23);
+}
+
+// What a warp does for a block of one head, of keys or of values: rows x (`count` of them, the
+// first at place `first`) after the block's first `first` tokens, whose codes and scale are at
+// src and src_scale (the same as dst, or in a page that is being copied).
+template <typename T, int DP>
+__device__ __forceinline__ void append_block(const T *x, int64_t stride, int first, int count, int dim, const uint8_t *src, const float *src_scale,
+                                             uint8_t *dst, float *dst_scale) {
+    constexpr int PIECES = DP / 8, SIDE = 32 / PIECES, N = BLOCK / SIDE;
+    constexpr uint32_t INF = std::is_same<T, __nv_bfloat16>::value ? 0x7f80u : 0x7c00u;
+    const int lane = lane_id(), sub = lane / PIECES, d = 8 * (lane % PIECES);
+    const bool mine = d < dim;
+    const float was = first > 0 ? *src_scale : 0.f;
+    uint4 v[N];
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+        const int r = sub + q * SIDE;
+        v[q] = mine && r < count ? __ldcs(reinterpret_cast<const uint4 *>(x + r * stride + d)) : make_uint4(0, 0, 0, 0);
+    }
+    uint32_t *w = &v[0].x;
+    auto largest = [&] {
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < 4 * N; ++i) most = __vmaxu2(most, w[i] & 0x7fff7fffu);
+        return __reduce_max_sync(0xffffffffu, max(most >> 16, most & 0xffffu));
+    };
+    uint32_t top = largest();
+    if (top >= INF) {
+        // what is not finite has no say in the scale, and becomes NaN
+        uint32_t bad[4 * N];
+#pragma unroll
+        for (int i = 0; i < 4 * N; ++i) {
+            bad[i] = __vcmpgeu2(w[i] & 0x7fff7fffu, INF << 16 | INF);
+            w[i] &= ~bad[i];
+        }
+        top = largest();
+#pragma unroll
+        for (int i = 0; i < 4 * N; ++i) w[i] |= bad[i] & 0x7fff7fffu;
+    }
+    const float2 t2 = Type2<T>::up(top);
+    const float need = scale_for(t2.x), now = was > need ? was : need;
+    const bool grown = first > 0 && !(was >= now);
+    // (a scale that this library chose is a power of two, and so is its inverse)
+    const bool power = (__float_as_int(now) & 0x7fffff) == 0 && now >= __int_as_float(1 << 23);
+    const float inverse = 1.f / now;
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+        const int r = sub + q * SIDE;
+        uint32_t y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 z = Type2<T>::up(w[4 * q + i]);
+            y[i] = power ? codes2(z.x * inverse, z.y * inverse) : codes2(__fdiv_rn(z.x, now), __fdiv_rn(z.y, now));
+        }
+        if (mine && r < count) *reinterpret_cast<uint2 *>(dst + (first + r) * dim + d) = make_uint2(y[0] | y[1] << 16, y[2] | y[3] << 16);
+    }
+    if (first > 0 && (grown || src != dst)) {
+        const float share = grown ? __fdiv_rn(was, now) : 1.f;
+        for (int r = sub; r < first; r += SIDE) {
+            if (!mine) continue;
+            uint2 y = *reinterpret_cast<const uint2 *>(src + r * dim + d);
+            if (grown) {
+                uint32_t *z = &y.x;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float2 a = values2(z[i] & 0xffffu), b = values2(z[i] >> 16);
+                    z[i] = codes2(a.x * share, a.y * share) | codes2(b.x * share, b.y * share) << 16;
+                }
+            }
+            *reinterpret_cast<uint2 *>(dst + r * dim + d) = y;
+        }
+    }
+    __syncwarp();
+    if (lane == 0) *dst_scale = now;
+}
+
+// As k_append_rows, a warp to 16 tokens of a head's keys or values.  Sequence i has the places
+// from offsets[i] / 16 + 2 i on, enough for its blocks wherever they begin; those it does not
+// need are passed over.  The block that a sequence's new rows share with rows of a copied page
+// is put together from both by whoever writes the rows; the copying blocks have the full ones.
+template <typename T, int DP>
+__global__ void __launch_bounds__(COPY_THREADS)
+k_append_rows8(opattr_cache8 c8, const int32_t *seqs, int n, const int32_t *offsets, int tokens, opattr_rows k,
+               opattr_rows v, AppendPlan p, unsigned row_blocks) {
+    pdl_wait();
+    if (*p.go == 0) return;
+    const opattr_cache &kv = c8.pages;
+    constexpr int WARPS = COPY_THREADS / 32;
+    const int dim = kv.head_dim, warp = threadIdx.x / 32, lane = lane_id(), subs = kv.page_size / BLOCK;
+    uint8_t *kp = (uint8_t *)kv.k_pages, *vp = (uint8_t *)kv.v_pages;
+    // rows of entry i from place `first` of block b of its sequence on; its tokens before them are in page `src`
+    auto block = [&](int i, int b, int g, int what, int src, int dst) {
+        const int old = p.old[i], all = old + offsets[i + 1] - offsets[i];
+        const int lo = max(old, b * BLOCK), hi = min(all, b * BLOCK + BLOCK);
+        const int64_t at = ((int64_t)dst * kv.kv_heads + g) * subs + b % subs, from = ((int64_t)src * kv.kv_heads + g) * subs + b % subs;
+        const opattr_rows &x = what ? v : k;
+        uint8_t *pool = what ? vp : kp;
+        float *scales = what ? c8.v_scales : c8.k_scales;
+        append_block<T, DP>((const T *)x.data + (int64_t)(offsets[i] + lo - old) * x.token_stride + g * x.head_stride, x.token_stride,
+                            lo - b * BLOCK, hi - lo, dim, pool + from * BLOCK * dim, scales + from, pool + at * BLOCK * dim, scales + at);
+    };
+    if (blockIdx.x >= row_blocks) {
+        const int64_t all = (int64_t)n * kv.kv_heads;
+        for (int64_t x = blockIdx.x - row_blocks; x < all; x += gridDim.x - row_blocks) {
+            const int i = (int)(x / kv.kv_heads), g = (int)(x % kv.kv_heads);
+            const int from = p.from[i];
+            auto copy = [&](int entry, int page) {
+                const int full = p.old[entry] % kv.page_size / BLOCK;
+                const int64_t src = ((int64_t)page * kv.kv_heads + g) * subs, dst = ((int64_t)p.to[entry] * kv.kv_heads + g) * subs;
+                const uint4 *ks = (const uint4 *)(kp + src * BLOCK * dim), *vs = (const uint4 *)(vp + src * BLOCK * dim);
+                uint4 *kd = (uint4 *)(kp + dst * BLOCK * dim), *vd = (uint4 *)(vp + dst * BLOCK * dim);
+                for (int e = threadIdx.x; e < full * dim; e += COPY_THREADS) {
+                    const uint4 k4 = ks[e], v4 = vs[e];
+                    kd[e] = k4;
+                    vd[e] = v4;
+                }
+                for (int e = threadIdx.x; e < full; e += COPY_THREADS) {
+                    c8.k_scales[dst + e] = c8.k_scales[src + e];
+                    c8.v_scales[dst + e] = c8.v_scales[src + e];
+                }
+            };
+            if (from >= 0) copy(i, from);
+            if (from >= -1 || p.to[i] >= 0) continue;
+            // the page stays with this sequence: first those that copy it, with what they have in its last block
+            const int page = -2 - from, old = p.old[i];
+            for (int e = 0; e < i; ++e)
+                if (p.from[e] == from && p.to[e] >= 0) {
+                    copy(e, page);
+                    if (p.old[e] % BLOCK && warp < 2) block(e, p.old[e] / BLOCK, g, warp, page, p.to[e]);
+                }
+            __syncthreads();
+            const int first = old / BLOCK, last = min(old + offsets[i + 1] - offsets[i] - 1, old - old % kv.page_size + kv.page_size - 1) / BLOCK;
+            for (int w = warp; w < 2 * (last - first + 1); w += WARPS) block(i, first + w / 2, g, w % 2, page, page);
+        }
+        return;
+    }
+    const int64_t units = ((int64_t)tokens / BLOCK + 2 * n) * kv.kv_heads * 2;
+    for (int64_t u = (int64_t)blockIdx.x * WARPS + warp; u < units; u += (int64_t)row_blocks * WARPS) {
+        const int place = (int)(u / (2 * kv.kv_heads)), rest = (int)(u - (int64_t)place * 2 * kv.kv_heads);
+        // the last sequence whose places begin there or before, 32 at a time
+        int i = 0;
+        for (int m = n; m > 1;) {
+            const int step = (m + 31) / 32, e = i + step * lane;
+            const bool le = step * lane < m && offsets[e] / BLOCK + 2 * e <= place;
+            const int at = 31 - __clz(__ballot_sync(0xffffffffu, le));
+            i += at * step;
+            m = min(step, m - at * step);
+        }
+        const int old = p.old[i], more = offsets[i + 1] - offsets[i], b = old / BLOCK + place - (offsets[i] / BLOCK + 2 * i);
+        if (more == 0 || b > (old + more - 1) / BLOCK) continue;
+        const int j = b / subs, page = kv.table[(int64_t)seqs[i] * kv.pages_per_seq + j];
+        if (page < 0 || page >= kv.n_pages) continue;             // a table that was not consistent before the call
+        const int from = p.from[i];
+        const bool shared = b * BLOCK < old;                      // (with tokens before the call)
+        if (from < -1 && (p.to[i] < 0 ? j * kv.page_size < old : shared)) continue;
+        block(i, b, rest >> 1, rest & 1, shared && from >= 0 ? from : page, page);
+    }
+}
+
 // One thread to a sequence, or to four new pages; of few, a block that is quick to begin.
 static unsigned plan_threads(int64_t n) { return n <= 256 ? 256 : PLAN_THREADS; }
 static opattr_status seqs_ok(const opattr_cache *kv, const int32_t *seqs, int32_t n) {
     return cache_ok(kv) && n >= 0 && n <= kv->n_seqs && (n == 0 || seqs) ? OPATTR_OK : OPATTR_E_INVALID_ARG;
 }
 
+template <typename T>
+static opattr_status rows8_of(Ctx &c, const opattr_cache8 &c8, const int32_t *seqs, int n, const int32_t *offsets, int tokens,
+                              const opattr_rows &k, const opattr_rows &v, const AppendPlan &p) {
+    const opattr_cache &kv = c8.pages;
+    const unsigned rows = grid_for(((int64_t)tokens / BLOCK + 2 * n) * kv.kv_heads * 2, COPY_THREADS / 32, 8u * sm_count(c));
+    const unsigned shared = (unsigned)std::min<int64_t>((int64_t)n * kv.kv_heads, 2 * sm_count(c));
+    if (kv.head_dim <= 64)
+        launch(c, "append_rows8", k_append_rows8<T, 64>, dim3(rows + shared), dim3(COPY_THREADS), 0, c8, seqs, n, offsets, tokens, k, v, p, rows);
+    else
+        launch(c, "append_rows8", k_append_rows8<T, 128>, dim3(rows + shared), dim3(COPY_THREADS), 0, c8, seqs, n, offsets, tokens, k, v, p, rows);
+    return cuda_status(c, c.last_error);
+}
+
 opattr_status do_cache_append(Ctx &c, Serve &s, const opattr_cache *kv, const int32_t *seqs, int32_t n,
                               const int32_t *offsets, int64_t tokens, const opattr_rows *k, const opattr_rows *v) {
     opattr_status st = seqs_ok(kv, seqs, n);
     if (st) return st;
+    const opattr_cache8 *e8 = cache8(kv);
     if (tokens < 0 || tokens > INT32_MAX || (n == 0 && tokens > 0) || (n > 0 && !offsets)) return OPATTR_E_INVALID_ARG;
     if (!rows_ok(*k, tokens, kv->kv_heads, kv->head_dim) || !rows_ok(*v, tokens, kv->kv_heads, kv->head_dim))
         return OPATTR_E_INVALID_ARG;
@@ -334,7 +531,10 @@ opattr_status do_cache_append(Ctx &c, Serve &s, const opattr_cache *kv, const in
     p.mark = a.take<int32_t>(kv->n_seqs);
     p.fresh = a.take<int32_t>(most);
     p.room = (int32_t)most;
-    launch(c, "append_plan", k_append_plan, dim3(1), dim3(plan_threads(std::max<int64_t>(n, most / 4))), 0, *kv, seqs, n, offsets, (int)tokens, p, s.err);
+    launch(c, "append_plan", k_append_plan, dim3(1), dim3(plan_threads(std::max<int64_t>(n, most / 4))), 0, *kv, seqs, n, offsets, (int)tokens, p,
+           e8 ? BLOCK : 1, s.err);
+    if (e8) return e8->rows == OPATTR_BF16 ? rows8_of<__nv_bfloat16>(c, *e8, seqs, n, offsets, (int)tokens, *k, *v, p)
+                                           : rows8_of<__half>(c, *e8, seqs, n, offsets, (int)tokens, *k, *v, p);
     const int row = kv->kv_heads * (kv->head_dim / 8);
     const unsigned rows = grid_for(tokens, std::max(1, COPY_THREADS / row), 8u * sm_count(c));
     const unsigned shared = (unsigned)std::min<int64_t>((int64_t)n * kv->kv_heads, 2 * sm_count(c));
@@ -556,10 +756,10 @@ k_compact_place(opattr_cache kv, const int32_t *tile_live, int tiles, int32_t *r
 constexpr int MOVE = 4 * COPY_THREADS;          // pieces of 16 bytes of a run
 // Pages over the grid; then the tables.
 __global__ void __launch_bounds__(COPY_THREADS)
-k_compact_move(opattr_cache kv, const int32_t *rank, const int32_t *hole, const int32_t *mover, const int32_t *counts) {
+k_compact_move(opattr_cache kv, float *k_scales, float *v_scales, const int32_t *rank, const int32_t *hole, const int32_t *mover, const int32_t *counts) {
     pdl_wait();
     const int moves = counts[0], L = counts[1];
-    const int page = kv.kv_heads * kv.page_size * (kv.head_dim / 8), runs = (page + MOVE - 1) / MOVE;
+    const int page = kv.kv_heads * (k_scales ? kv.page_size / BLOCK * kv.head_dim : kv.page_size * (kv.head_dim / 8)), runs = (page + MOVE - 1) / MOVE;
     const int64_t t0 = (int64_t)blockIdx.x * COPY_THREADS + threadIdx.x, step = (int64_t)gridDim.x * COPY_THREADS;
     uint4 *kp = reinterpret_cast<uint4 *>(kv.k_pages), *vp = reinterpret_cast<uint4 *>(kv.v_pages);
     // runs of a page's pieces, a block to each: every thread has all its loads under way before it stores
@@ -576,6 +776,16 @@ k_compact_move(opattr_cache kv, const int32_t *rank, const int32_t *hole, const 
         for (int q = 0; q < MOVE / COPY_THREADS; ++q) {
             const int e = first + q * COPY_THREADS;
             if (e < page) kp[dst + e] = k4[q], vp[dst + e] = v4[q];
+        }
+    }
+    if (k_scales) {
+        const int each = kv.kv_heads * (kv.page_size / BLOCK);
+        for (int64_t x = t0; x < (int64_t)moves * each; x += step) {
+            const int m = (int)(x / each), e = (int)(x - (int64_t)m * each);
+            const int64_t src = (int64_t)mover[m] * each + e, dst = (int64_t)hole[m] * each + e;
+            const float a = k_scales[src], b = v_scales[src];
+            k_scales[dst] = a;
+            v_scales[dst] = b;
         }
     }
     for (int64_t m = t0; m < moves; m += step) {
@@ -597,6 +807,7 @@ opattr_status do_cache_compact(Ctx &c, Serve &s, const opattr_cache *kv, int32_t
     if (!cache_ok(kv)) return OPATTR_E_INVALID_ARG;
     opattr_status st = serve_ready(c, s);
     if (st) return st;
+    const opattr_cache8 *e8 = cache8(kv);
     const int tiles = (int)((kv->n_pages + TILE_PAGES - 1) / TILE_PAGES);
     if ((st = ensure_lasting_arena(c, Need().add<int32_t>(2).add<int32_t>(tiles).add<int32_t>(kv->n_pages).add<int32_t>(kv->n_pages)
                                   .add<int32_t>(kv->n_pages).bytes)))
@@ -607,7 +818,8 @@ opattr_status do_cache_compact(Ctx &c, Serve &s, const opattr_cache *kv, int32_t
     if (tiles > 1) launch(c, "compact_count", k_compact_count, dim3(tiles), dim3(PLAN_THREADS), 0, *kv, tile_live);
     launch(c, "compact_place", k_compact_place, dim3(tiles), dim3(PLAN_THREADS), 0, *kv, (const int32_t *)tile_live, tiles,
            rank, hole, mover, counts, live);
-    launch(c, "compact_move", k_compact_move, dim3(8 * sm_count(c)), dim3(COPY_THREADS), 0, *kv, (const int32_t *)rank,
+    launch(c, "compact_move", k_compact_move, dim3(8 * sm_count(c)), dim3(COPY_THREADS), 0, *kv,
+           e8 ? e8->k_scales : nullptr, e8 ? e8->v_scales : nullptr, (const int32_t *)rank,
            (const int32_t *)hole, (const int32_t *)mover, (const int32_t *)counts);
     return cuda_status(c, c.last_error);
 }

@@ -79,6 +79,11 @@ __device__ __forceinline__ int seq_of_row(const int32_t *offsets, int n, int t) 
     return lo;
 }
 
+// A cache whose pages hold 8 bits, else NULL (then what follows the struct is not its own).
+inline const opattr_cache8 *cache8(const opattr_cache *kv) {
+    return kv->dtype == OPATTR_E4M3 ? reinterpret_cast<const opattr_cache8 *>(kv) : nullptr;
+}
+
 // Views with 16-byte rows: every operator moves rows by 16 bytes.
 bool rows_ok(const opattr_rows &r, int64_t tokens, int heads, int dim);
 

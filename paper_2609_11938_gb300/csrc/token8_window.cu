@@ -1,0 +1,10 @@
+// token8_window.cu -- the kernel of token.cuh for pages of 8 bits, through a window.
+#include "token.cuh"
+
+namespace opattr {
+
+opattr_status token8_window(Ctx &c, Serve &s, TokenArgs &p, int dtype) {
+    return dtype == OPATTR_BF16 ? token_of<__nv_bfloat16, true, true>(c, s, p) : token_of<__half, true, true>(c, s, p);
+}
+
+}  // namespace opattr
