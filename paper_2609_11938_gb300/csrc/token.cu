@@ -23,6 +23,8 @@ opattr_status do_cache_attention(Ctx &c, Serve &s, const opattr_cache *kv, const
     p.window = window;
     p.sinks = sinks;
     const opattr_cache8 *e8 = cache8(kv);
+    // (a block of a pool has a number of 30 bits; more would not fit the memory of a GPU)
+    if (e8 && kv->n_pages * kv->kv_heads >= (int64_t)PARTLY / (kv->page_size / OPATTR_SCALE_TOKENS)) return OPATTR_E_INVALID_ARG;
     if (e8) p.k_scales = e8->k_scales, p.v_scales = e8->v_scales;
     p.seqs = seqs;
     p.n = n;

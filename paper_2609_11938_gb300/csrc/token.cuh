@@ -48,9 +48,19 @@ constexpr int TOKEN_WARPS = 4, TOKEN_THREADS = 32 * TOKEN_WARPS;
 // few steps are whole, and belong to the block that they begin in: 13 of 1 .. 596
 // tokens, 8 heads of 64 on 2: 10.7 us with every pair cut, 6.4; up to four steps 7.1, and
 // 293 of 148 .. 444, 16 heads of 128 on 4, 37.6 for 36.8.
+constexpr unsigned PARTLY = 1u << 30;
 constexpr int WHOLE_STEPS = 3;
 constexpr float JOIN_STEPS = 12.f;
 
+#ifndef E8_BLOCKS
+#define E8_BLOCKS (DP == 64 ? 4 : 3)
+#endif
+#ifndef E8_F64
+#define E8_F64 2
+#endif
+#ifndef E8_F128
+#define E8_F128 2
+#endif
 struct TokenArgs {
     opattr_cache kv;
     const int32_t *seqs;
@@ -89,6 +99,12 @@ __device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, u
     else
         asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
             : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// The same of halves, and of sums that begin with it.
+__device__ __forceinline__ void mma16_new(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("{\n .reg .f32 z;\n mov.f32 z, 0f00000000;\n"
+        " mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {z, z, z, z};\n}"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 // An 8 x 8 matrix of 16-bit values, two of a row in a lane, transposed.
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
@@ -139,10 +155,28 @@ __device__ __forceinline__ void query_halves(uint32_t (&r)[KC][8], float &back) 
         }
 }
 
+// Loads that nothing holds back: no zeros beforehand, and the offset within the instruction.
+template <int OFF>
+__device__ __forceinline__ uint4 get16(const uint8_t *p) {
+    uint4 r;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4 + %5];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p), "n"(OFF));
+    return r;
+}
+template <int OFF>
+__device__ __forceinline__ uint2 get8(const uint8_t *p) {
+    uint2 r;
+    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2 + %3];" : "=r"(r.x), "=r"(r.y) : "l"(p), "n"(OFF));
+    return r;
+}
+__device__ __forceinline__ void fma_pair(float &a, float &b, float x, float y, float f) {
+    asm("{\n .reg .b64 s, u, v;\n mov.b64 s, {%0, %1};\n mov.b64 u, {%2, %3};\n mov.b64 v, {%4, %4};\n fma.rn.f32x2 s, u, v, s;\n mov.b64 {%0, %1}, s;\n}"
+        : "+f"(a), "+f"(b) : "f"(x), "f"(y), "f"(f));
+}
+
 // DP: the padded head width; NT: eights of queries; FR: sixteens of keys that a
 // warp takes at a time; E8: pages of 8 bits; WIN: through a window.
 template <typename T, int DP, int NT, int FR, bool E8, bool WIN>
-__global__ void __launch_bounds__(TOKEN_THREADS, NT == 1 ? 3 : 2) k_token(const __grid_constant__ TokenArgs p, unsigned *err) {
+__global__ void __launch_bounds__(TOKEN_THREADS, E8 ? (NT == 1 ? E8_BLOCKS : 2) : NT == 1 ? 3 : 2) k_token(const __grid_constant__ TokenArgs p, unsigned *err) {
     using P = std::conditional_t<E8, __half, T>;          // what the products take
     constexpr bool BF = std::is_same<P, __nv_bfloat16>::value;
     // as in prompt.cu: weights up to 2^(OFFSET + SLACK), rescaled when a maximum outgrows SLACK
@@ -165,16 +199,16 @@ __global__ void __launch_bounds__(TOKEN_THREADS, NT == 1 ? 3 : 2) k_token(const 
         const int len = kv.length[seq];
         return len > kv.pages_per_seq << p.shift ? -1 : len;
     };
-    // Steps of a length.  Through a window those that nobody sees are left out: the first `head`
-    // steps have the sinks, and later ones are `gap` further on.
+    // Steps of a length.  Through a window, sixteens of keys that nobody sees are left out: the first
+    // `head` ones have the sinks, and later ones are `gap` further on.
     auto steps_of = [&](int len, int &head, int &gap) {
-        const int all = len <= 0 ? 1 : (len - 1) / STEP + 1;
         head = gap = 0;
-        if (!WIN) return all;
-        const int low = max(0, len - p.window), first = low / STEP, few = min(p.sinks, low);
-        head = min(first, (int)(((unsigned)few + STEP - 1) / STEP));
+        if (!WIN) return len <= 0 ? 1 : (len - 1) / STEP + 1;
+        const int low = max(0, len - p.window), first = low >> 4, few = min(p.sinks, low);
+        head = min(first, (int)(((unsigned)few + 15) >> 4));
         gap = first - head;
-        return all - gap;
+        const int all = len <= 0 ? 1 : ((len - 1) >> 4) + 1 - gap;
+        return (all - 1) / (STEP / 16) + 1;
     };
     auto count_of = [&](int len) {
         int head, gap;
@@ -220,7 +254,8 @@ __global__ void __launch_bounds__(TOKEN_THREADS, NT == 1 ? 3 : 2) k_token(const 
             ++b;
             continue;
         }
-        const int unit = (int)((s - base) / cost), g = unit / p.blocks_of_heads, hb = unit % p.blocks_of_heads;
+        const long long past = s - base;
+        const int unit = past <= INT32_MAX ? (int)past / cost : (int)(past / cost), g = unit / p.blocks_of_heads, hb = unit % p.blocks_of_heads;
         const long long unit_at = base + (long long)unit * cost + 1;   // of its first step
         int from = (int)max(0ll, s - unit_at), to = (int)min((long long)steps, s1 - unit_at);
         if (steps <= WHOLE_STEPS) {
@@ -259,13 +294,31 @@ __global__ void __launch_bounds__(TOKEN_THREADS, NT == 1 ? 3 : 2) k_token(const 
         for (int t = 0; t < NT; ++t) m[t][0] = m[t][1] = -INFINITY;
         // (unsigned where a step past a length near 2^31 is counted)
         const int last = WIN ? len : (int)min((unsigned)len, (unsigned)to * STEP);  // keys of this run: from * STEP .. last
-        auto place = [&](int step) { return WIN && step >= head ? step + gap : step; };
+        // the first of the keys that this warp's f-th lot of a step has
+        auto key_at = [&](int step, int f) {
+            unsigned x = (unsigned)step * (STEP / 16) + (warp * FR + f);
+            if (WIN && x >= (unsigned)head) x += gap;
+            return 16 * x;
+        };
         // of the rows up to `lim`, the keys from the window's first on, or the sinks
         const int near = min(p.window, len), far = p.sinks - len;
         auto seen = [&](int r, int lim) { return r < lim && (!WIN || r >= lim - near || r < lim + far); };
         uint4 kr[FR][2][KC];
         std::conditional_t<E8 && DP == 64, uint2, uint4> vr[FR][4][E8 ? 1 : VC];
         float ks[FR], vs[FR], vs_next[FR];                // (pages of 8 bits) their blocks' scales
+        // (pages of 8 bits) which block of 16 tokens of the pools has a warp's keys: -1 where none is seen
+        // or the page is none, and PARTLY added where not all of them are
+        auto lot_of = [&](unsigned key, int page) -> int {
+            const int lim = (int)min(16u, (unsigned)last - key);
+            if (key >= (unsigned)last) return -1;
+            if (WIN && !((int)key + lim > len - near || (int)key < p.sinks)) return -1;
+            if (page < 0 || page >= kv.n_pages) {
+                atomicOr(err, SERVE_INVALID);
+                return -1;
+            }
+            const bool whole = lim == 16 && (!WIN || (int)key >= len - near || (int)key <= p.sinks - 16);
+            return ((page * kv.kv_heads + g) << (p.shift - 4)) + ((int)key >> 4 & (kv.page_size / 16 - 1)) + (whole ? 0 : PARTLY);
+        };
         // pages of this warp's coming keys, one to a lane: lane i has those of step held + i
         int held = 0, pages[FR];
         auto page_of = [&](int step, int f) -> int {
@@ -273,15 +326,16 @@ __global__ void __launch_bounds__(TOKEN_THREADS, NT == 1 ? 3 : 2) k_token(const 
                 held = step;
 #pragma unroll
                 for (int x = 0; x < FR; ++x) {
-                    const unsigned key = (unsigned)place(step + lane) * STEP + 16 * (warp * FR + x);
+                    const unsigned key = key_at(step + lane, x);
                     pages[x] = key < (unsigned)last ? table[key >> p.shift] : 0;
+                    if constexpr (E8) pages[x] = lot_of(key, pages[x]);
                 }
             }
             return __shfl_sync(0xffffffffu, pages[f], step - held);
         };
         // where the rows of a step's keys are; none past the run's end or of a page that is none
         auto rows_at = [&](int step, int f, int &lim) -> long long {
-            const int key = place(step) * STEP + 16 * (warp * FR + f), page = page_of(step, f);
+            const int key = key_at(step, f), page = page_of(step, f);
             lim = last - key;
             if (WIN) lim = lim > 0 && (lim - near < 16 || lim + far > 0) ? lim : 0;
             if (lim > 0 && (page < 0 || page >= kv.n_pages)) {
@@ -289,45 +343,100 @@ __global__ void __launch_bounds__(TOKEN_THREADS, NT == 1 ? 3 : 2) k_token(const 
                 lim = 0;
             }
             const long long at = ((long long)page * kv.kv_heads + g << p.shift) + (key & (kv.page_size - 1));
-            if (E8) {
-                ks[f] = lim > 0 ? p.k_scales[at >> 4] : 0.f;
-                vs_next[f] = lim > 0 ? p.v_scales[at >> 4] : 0.f;
-            }
             return at * kv.head_dim;
         };
         long long kat[FR], vat[FR];
         int klim[FR], vlim[FR];
+        // (pages of 8 bits) blocks of the keys, whether there is nothing to leave out of their rows, and whether there is nothing in them
+        int lot[FR];
+        bool kall = false, vall = false, knone = false, vnone = false;
+        const uint8_t *k_lane = (const uint8_t *)kv.k_pages + (row * DP + 16 * col), *v_lane = (const uint8_t *)kv.v_pages + (2 * col * DP + DP / 8 * row);
         auto load_keys = [&](int step) {
+            if constexpr (E8) {
+                int any = -1, all = 0;
 #pragma unroll
-            for (int f = 0; f < FR; ++f) {
-                kat[f] = rows_at(step, f, klim[f]);
+                for (int f = 0; f < FR; ++f) {
+                    lot[f] = page_of(step, f);
+                    any &= lot[f];
+                    all |= lot[f];
+                }
+                kall = kv.head_dim == DP && (unsigned)all < PARTLY;
+                knone = any == -1;
+                if (kall) {
 #pragma unroll
-                for (int r = 0; r < 2; ++r)
+                    for (int f = 0; f < FR; ++f) {
+                        const uint8_t *at = k_lane + (uint64_t)(unsigned)lot[f] * (16 * DP);
+                        kr[f][0][0] = get16<0>(at);
+                        kr[f][1][0] = get16<8 * DP>(at);
+                        if constexpr (DP == 128) {
+                            kr[f][0][KC - 1] = get16<64>(at);
+                            kr[f][1][KC - 1] = get16<8 * DP + 64>(at);
+                        }
+                        ks[f] = p.k_scales[(unsigned)lot[f]];
+                        vs_next[f] = p.v_scales[(unsigned)lot[f]];
+                    }
+                } else {
 #pragma unroll
-                    for (int i = 0; i < KC; ++i)
-                        if (E8)
-                            kr[f][r][i] = load16((const uint8_t *)kv.k_pages + kat[f] + (row + 8 * r) * kv.head_dim + 64 * i + 16 * col,
-                                                 seen(row + 8 * r, klim[f]) && 64 * i + 16 * col < kv.head_dim);
-                        else
+                    for (int f = 0; f < FR; ++f) {
+                        const bool on = lot[f] >= 0;
+                        klim[f] = on ? last - (int)key_at(step, f) : 0;
+                        lot[f] = on ? lot[f] & (PARTLY - 1) : 0;
+                        const uint8_t *at = (const uint8_t *)kv.k_pages + (uint64_t)(unsigned)lot[f] * (16 * kv.head_dim);
+#pragma unroll
+                        for (int r = 0; r < 2; ++r)
+#pragma unroll
+                            for (int i = 0; i < KC; ++i)
+                                kr[f][r][i] = load16(at + (row + 8 * r) * kv.head_dim + 64 * i + 16 * col,
+                                                     seen(row + 8 * r, klim[f]) && 64 * i + 16 * col < kv.head_dim);
+                        ks[f] = on ? p.k_scales[(unsigned)lot[f]] : 0.f;
+                        vs_next[f] = on ? p.v_scales[(unsigned)lot[f]] : 0.f;
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int f = 0; f < FR; ++f) {
+                    kat[f] = rows_at(step, f, klim[f]);
+#pragma unroll
+                    for (int r = 0; r < 2; ++r)
+#pragma unroll
+                        for (int i = 0; i < KC; ++i)
                             kr[f][r][i] = load16((const T *)kv.k_pages + kat[f] + (row + 8 * r) * kv.head_dim + 32 * i + 8 * col,
-                                                 seen(row + 8 * r, klim[f]) && 32 * i + 8 * col < kv.head_dim);
+                                                     seen(row + 8 * r, klim[f]) && 32 * i + 8 * col < kv.head_dim);
+                }
             }
         };
         auto load_values = [&]() {
+            if constexpr (E8) {
+                vall = kall, vnone = knone;
 #pragma unroll
-            for (int f = 0; f < FR; ++f) {
-                vat[f] = kat[f], vlim[f] = klim[f];
-                if (E8) vs[f] = vs_next[f];
+                for (int f = 0; f < FR; ++f) {
+                    vlim[f] = klim[f], vs[f] = vs_next[f];
+                    if (vall) {
+                        const uint8_t *at = v_lane + (uint64_t)(unsigned)lot[f] * (16 * DP);
+                        if constexpr (DP == 64) {
+                            vr[f][0][0] = get8<0>(at), vr[f][1][0] = get8<DP>(at), vr[f][2][0] = get8<8 * DP>(at), vr[f][3][0] = get8<9 * DP>(at);
+                        } else {
+                            vr[f][0][0] = get16<0>(at), vr[f][1][0] = get16<DP>(at), vr[f][2][0] = get16<8 * DP>(at), vr[f][3][0] = get16<9 * DP>(at);
+                        }
+                        continue;
+                    }
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int key = 2 * col + (r & 1) + 8 * (r >> 1);
-                    const bool on = seen(key, vlim[f]);
-                    if constexpr (E8) {
-                        const int d = DP / 8 * row;
-                        const uint8_t *at = (const uint8_t *)kv.v_pages + vat[f] + key * kv.head_dim + d;
-                        if constexpr (DP == 64) vr[f][r][0] = load8(at, on && d < kv.head_dim);
-                        else vr[f][r][0] = load16(at, on && d < kv.head_dim);
-                    } else {
+                    for (int r = 0; r < 4; ++r) {
+                        const int key = 2 * col + (r & 1) + 8 * (r >> 1), d = DP / 8 * row;
+                        const bool on = seen(key, vlim[f]) && d < kv.head_dim;
+                        const uint8_t *at = (const uint8_t *)kv.v_pages + (uint64_t)(unsigned)lot[f] * (16 * kv.head_dim) + key * kv.head_dim + d;
+                        if constexpr (DP == 64) vr[f][r][0] = load8(at, on);
+                        else vr[f][r][0] = load16(at, on);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int f = 0; f < FR; ++f) {
+                    vat[f] = kat[f], vlim[f] = klim[f];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int key = 2 * col + (r & 1) + 8 * (r >> 1);
+                        const bool on = seen(key, vlim[f]);
 #pragma unroll
                         for (int i = 0; i < VC; ++i) {
                             const int d = 64 * i + 8 * row;
@@ -340,6 +449,10 @@ __global__ void __launch_bounds__(TOKEN_THREADS, NT == 1 ? 3 : 2) k_token(const 
         load_keys(from);
         load_values();
         for (int step = from; step < to; ++step) {
+            if (E8 && vnone) {                            // (of a warp: nothing of this step is its own)
+                if (step + 1 < to) load_keys(step + 1), load_values();
+                continue;
+            }
             float x[FR][NT][4] = {};
 #pragma unroll
             for (int f = 0; f < FR; ++f)
@@ -366,9 +479,18 @@ __global__ void __launch_bounds__(TOKEN_THREADS, NT == 1 ? 3 : 2) k_token(const 
 #pragma unroll
                 for (int f = 0; f < FR; ++f)
 #pragma unroll
-                    for (int t = 0; t < NT; ++t)
+                    for (int t = 0; t < NT; ++t) {
+                        const float k0 = ks[f] * cq[t][0], k1 = ks[f] * cq[t][1];
+                        x[f][t][0] *= k0, x[f][t][1] *= k1, x[f][t][2] *= k0, x[f][t][3] *= k1;
+                    }
+                if (!vall) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) x[f][t][i] *= ks[f];
+                    for (int f = 0; f < FR; ++f)
+#pragma unroll
+                        for (int t = 0; t < NT; ++t)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) x[f][t][i] = seen(row + 8 * (i >> 1), vlim[f]) ? x[f][t][i] : -INFINITY;
+                }
             }
             if (step + 1 < to) load_keys(step + 1);
             float top[NT][2];
@@ -380,7 +502,7 @@ __global__ void __launch_bounds__(TOKEN_THREADS, NT == 1 ? 3 : 2) k_token(const 
                 for (int f = 0; f < FR; ++f)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        x[f][t][i] = seen(row + 8 * (i >> 1), vlim[f]) ? x[f][t][i] * (E8 ? cq[t][i & 1] : c) : -INFINITY;
+                        if (!E8) x[f][t][i] = seen(row + 8 * (i >> 1), vlim[f]) ? x[f][t][i] * c : -INFINITY;
                         top[t][i & 1] = fmaxf(top[t][i & 1], x[f][t][i]);
                     }
                 more = more || top[t][0] - m[t][0] > SLACK || top[t][1] - m[t][1] > SLACK;
@@ -427,10 +549,11 @@ __global__ void __launch_bounds__(TOKEN_THREADS, NT == 1 ? 3 : 2) k_token(const 
                             const uint32_t a0 = half_lo(u), a1 = half_hi(u), a2 = half_lo(w), a3 = half_hi(w);
 #pragma unroll
                             for (int t = 0; t < NT; ++t) {
-                                float z[4] = {};
-                                mma16<P>(z, a0, a1, a2, a3, pb[t][0], pb[t][1]);
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) o[t][2 * j + e][i] = __fmaf_rn(z[i], vs[f], o[t][2 * j + e][i]);
+                                float z[4];
+                                mma16_new(z, a0, a1, a2, a3, pb[t][0], pb[t][1]);
+                                float (&y)[4] = o[t][2 * j + e];
+                                fma_pair(y[0], y[1], z[0], z[1], vs[f]);
+                                fma_pair(y[2], y[3], z[2], z[3], vs[f]);
                             }
                         }
                 } else
@@ -468,8 +591,6 @@ __global__ void __launch_bounds__(TOKEN_THREADS, NT == 1 ? 3 : 2) k_token(const 
             }
         __syncthreads();
         const bool whole = from == 0 && to == steps;
-        // a pair's parts: the block it begins in keeps its own in place 1, later ones in place 0
-        const int block1 = (int)(((unit_at + 1) * W - 1) / total), block2 = (int)(((unit_at + steps) * W - 1) / total);
         constexpr int PART = NQ * (DP + 2);
         auto finish = [&](int h, int d, float top, float sum, const float *y) {
             const float share = sum == 0.f ? 0.f : 1.f / sum;
@@ -486,6 +607,7 @@ __global__ void __launch_bounds__(TOKEN_THREADS, NT == 1 ? 3 : 2) k_token(const 
         float *part = p.parts + ((long long)blockIdx.x * 2 + (from == 0)) * PART;
         for (int i = threadIdx.x; i < NQ * (DP / 8); i += TOKEN_THREADS) {
             const int h = i / (DP / 8), d = i % (DP / 8) * 8;
+            if (h >= heads || d >= kv.head_dim) continue;
             float top = -INFINITY, sum = 0.f, y[8] = {};
 #pragma unroll
             for (int w = 0; w < TOKEN_WARPS; ++w) top = fmaxf(top, sm[w][h]);
@@ -496,7 +618,6 @@ __global__ void __launch_bounds__(TOKEN_THREADS, NT == 1 ? 3 : 2) k_token(const 
 #pragma unroll
                 for (int e = 0; e < 8; ++e) y[e] = __fmaf_rn(so[w][h][d + e], keep, y[e]);
             }
-            if (h >= heads || d >= kv.head_dim) continue;
             if (whole) finish(h, d, top, sum, y);
             else {
                 __stcg(reinterpret_cast<float4 *>(part + h * DP + d), make_float4(y[0], y[1], y[2], y[3]));
@@ -505,6 +626,8 @@ __global__ void __launch_bounds__(TOKEN_THREADS, NT == 1 ? 3 : 2) k_token(const 
             }
         }
         if (!whole) {
+            // a pair's parts: the block it begins in keeps its own in place 1, later ones in place 0
+            const int block1 = (int)(((unit_at + 1) * W - 1) / total), block2 = (int)(((unit_at + steps) * W - 1) / total);
             __threadfence();
             __syncthreads();
             if (threadIdx.x == 0) last_one = atomicAdd(&p.tickets[block1], 1u) == (unsigned)(block2 - block1);
@@ -542,7 +665,7 @@ template <typename T, int DP, int NT, int FR, bool E8, bool WIN>
 static opattr_status run_token(Ctx &c, Serve &s, TokenArgs &p) {
     const int64_t most = (int64_t)p.n * p.kv.kv_heads * p.blocks_of_heads *
                          (((int64_t)p.kv.pages_per_seq * p.kv.page_size + 16 * FR * TOKEN_WARPS - 1) / (16 * FR * TOKEN_WARPS));
-    const int grid = (int)std::min<int64_t>((NT == 1 ? 3 : 2) * (int64_t)sm_count(c), most);
+    const int grid = (int)std::min<int64_t>((E8 ? (NT == 1 ? E8_BLOCKS : 2) : NT == 1 ? 3 : 2) * (int64_t)sm_count(c), most);
     opattr_status st = serve_ready(c, s);
     if (st) return st;
     const int64_t part = (int64_t)8 * NT * (DP + 2);
@@ -555,9 +678,9 @@ static opattr_status run_token(Ctx &c, Serve &s, TokenArgs &p) {
 }
 template <typename T, bool E8, bool WIN>
 static opattr_status token_of(Ctx &c, Serve &s, TokenArgs &p) {
-    constexpr int FR = E8 ? 2 : 1;
-    if (p.kv.head_dim <= 64) return p.group <= 8 ? run_token<T, 64, 1, 2 * FR, E8, WIN>(c, s, p) : run_token<T, 64, 2, 2 * FR, E8, WIN>(c, s, p);
-    return p.group <= 8 ? run_token<T, 128, 1, FR, E8, WIN>(c, s, p) : run_token<T, 128, 2, FR, E8, WIN>(c, s, p);
+    constexpr int F64 = E8 ? E8_F64 : 2, F128 = E8 ? E8_F128 : 1;
+    if (p.kv.head_dim <= 64) return p.group <= 8 ? run_token<T, 64, 1, F64, E8, WIN>(c, s, p) : run_token<T, 64, 2, F64, E8, WIN>(c, s, p);
+    return p.group <= 8 ? run_token<T, 128, 1, F128, E8, WIN>(c, s, p) : run_token<T, 128, 2, F128, E8, WIN>(c, s, p);
 }
 
 // By the type of the queries; each in a file of its own, which compiles beside the others.
