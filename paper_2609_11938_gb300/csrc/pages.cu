@@ -346,25 +346,20 @@ __device__ __forceinline__ void append_block(const T *x, int64_t stride, int fir
         const int r = sub + q * SIDE;
         v[q] = mine && r < count ? __ldcs(reinterpret_cast<const uint4 *>(x + r * stride + d)) : make_uint4(0, 0, 0, 0);
     }
-    uint32_t *w = &v[0].x;
-    auto largest = [&] {
-        uint32_t most = 0;
+    uint32_t *w = &v[0].x, most = 0;
 #pragma unroll
-        for (int i = 0; i < 4 * N; ++i) most = __vmaxu2(most, w[i] & 0x7fff7fffu);
-        return __reduce_max_sync(0xffffffffu, max(most >> 16, most & 0xffffu));
-    };
-    uint32_t top = largest();
+    for (int i = 0; i < 4 * N; ++i) most = __vmaxu2(most, w[i] & 0x7fff7fffu);
+    uint32_t top = __reduce_max_sync(0xffffffffu, max(most >> 16, most & 0xffffu));
     if (top >= INF) {
         // what is not finite has no say in the scale, and becomes NaN
-        uint32_t bad[4 * N];
+        most = 0;
 #pragma unroll
         for (int i = 0; i < 4 * N; ++i) {
-            bad[i] = __vcmpgeu2(w[i] & 0x7fff7fffu, INF << 16 | INF);
-            w[i] &= ~bad[i];
+            const uint32_t size = w[i] & 0x7fff7fffu, bad = __vcmpgeu2(size, INF << 16 | INF);
+            most = __vmaxu2(most, size & ~bad);
+            w[i] |= bad & 0x7fff7fffu;
         }
-        top = largest();
-#pragma unroll
-        for (int i = 0; i < 4 * N; ++i) w[i] |= bad[i] & 0x7fff7fffu;
+        top = __reduce_max_sync(0xffffffffu, max(most >> 16, most & 0xffffu));
     }
     const float2 t2 = Type2<T>::up(top);
     const float need = scale_for(t2.x), now = was > need ? was : need;
@@ -372,17 +367,21 @@ __device__ __forceinline__ void append_block(const T *x, int64_t stride, int fir
     // (a scale that this library chose is a power of two, and so is its inverse)
     const bool power = (__float_as_int(now) & 0x7fffff) == 0 && now >= __int_as_float(1 << 23);
     const float inverse = 1.f / now;
+    auto store = [&](auto &&by) {
 #pragma unroll
-    for (int q = 0; q < N; ++q) {
-        const int r = sub + q * SIDE;
-        uint32_t y[4];
+        for (int q = 0; q < N; ++q) {
+            const int r = sub + q * SIDE;
+            uint32_t y[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 z = Type2<T>::up(w[4 * q + i]);
-            y[i] = power ? codes2(z.x * inverse, z.y * inverse) : codes2(__fdiv_rn(z.x, now), __fdiv_rn(z.y, now));
+            for (int i = 0; i < 4; ++i) {
+                const float2 z = Type2<T>::up(w[4 * q + i]);
+                y[i] = codes2(by(z.x), by(z.y));
+            }
+            if (mine && r < count) *reinterpret_cast<uint2 *>(dst + (first + r) * dim + d) = make_uint2(y[0] | y[1] << 16, y[2] | y[3] << 16);
         }
-        if (mine && r < count) *reinterpret_cast<uint2 *>(dst + (first + r) * dim + d) = make_uint2(y[0] | y[1] << 16, y[2] | y[3] << 16);
-    }
+    };
+    if (power) store([&](float z) { return z * inverse; });
+    else store([&](float z) { return __fdiv_rn(z, now); });
     if (first > 0 && (grown || src != dst)) {
         const float share = grown ? __fdiv_rn(was, now) : 1.f;
         for (int r = sub; r < first; r += SIDE) {
@@ -403,27 +402,26 @@ __device__ __forceinline__ void append_block(const T *x, int64_t stride, int fir
     if (lane == 0) *dst_scale = now;
 }
 
-// As k_append_rows, a warp to 16 tokens of a head's keys or values.  Sequence i has the places
-// from offsets[i] / 16 + 2 i on, enough for its blocks wherever they begin; those it does not
-// need are passed over.  The block that a sequence's new rows share with rows of a copied page
-// is put together from both by whoever writes the rows; the copying blocks have the full ones.
+// As k_append_rows, a warp to 16 tokens of a head's keys or values at a time.  Sequence i has the
+// places from offsets[i] / 16 + 2 i on, enough for its blocks wherever they begin; those it does not
+// need are passed over.  A block of threads looks a place up once for `1 / parts` of its heads.  The
+// tokens that a sequence's new rows share a scale with, where their page is copied, are put together from both
+// by whoever writes the rows; the copying blocks have the full sixteens.
 template <typename T, int DP>
-__global__ void __launch_bounds__(COPY_THREADS)
+__global__ void __launch_bounds__(COPY_THREADS, DP == 64 ? 4 : 3)
 k_append_rows8(opattr_cache8 c8, const int32_t *seqs, int n, const int32_t *offsets, int tokens, opattr_rows k,
-               opattr_rows v, AppendPlan p, unsigned row_blocks) {
+               opattr_rows v, AppendPlan p, unsigned row_blocks, int parts) {
     pdl_wait();
     if (*p.go == 0) return;
     const opattr_cache &kv = c8.pages;
     constexpr int WARPS = COPY_THREADS / 32;
     const int dim = kv.head_dim, warp = threadIdx.x / 32, lane = lane_id(), subs = kv.page_size / BLOCK;
-    uint8_t *kp = (uint8_t *)kv.k_pages, *vp = (uint8_t *)kv.v_pages;
-    // rows of entry i from place `first` of block b of its sequence on; its tokens before them are in page `src`
-    auto block = [&](int i, int b, int g, int what, int src, int dst) {
-        const int old = p.old[i], all = old + offsets[i + 1] - offsets[i];
+    // rows of entry i from its old length `old` or from block b of its sequence on, up to `all`; its tokens before them are in page `src`
+    auto block = [&](int i, int old, int all, int b, int g, int what, int src, int dst) {
         const int lo = max(old, b * BLOCK), hi = min(all, b * BLOCK + BLOCK);
         const int64_t at = ((int64_t)dst * kv.kv_heads + g) * subs + b % subs, from = ((int64_t)src * kv.kv_heads + g) * subs + b % subs;
         const opattr_rows &x = what ? v : k;
-        uint8_t *pool = what ? vp : kp;
+        uint8_t *pool = (uint8_t *)(what ? kv.v_pages : kv.k_pages);
         float *scales = what ? c8.v_scales : c8.k_scales;
         append_block<T, DP>((const T *)x.data + (int64_t)(offsets[i] + lo - old) * x.token_stride + g * x.head_stride, x.token_stride,
                             lo - b * BLOCK, hi - lo, dim, pool + from * BLOCK * dim, scales + from, pool + at * BLOCK * dim, scales + at);
@@ -433,39 +431,44 @@ k_append_rows8(opattr_cache8 c8, const int32_t *seqs, int n, const int32_t *offs
         for (int64_t x = blockIdx.x - row_blocks; x < all; x += gridDim.x - row_blocks) {
             const int i = (int)(x / kv.kv_heads), g = (int)(x % kv.kv_heads);
             const int from = p.from[i];
-            auto copy = [&](int entry, int page) {
+            // the full sixteens of an entry's keys or values, by threads t, t + step, ..
+            auto copy = [&](int entry, int page, int what, int t, int step) {
                 const int full = p.old[entry] % kv.page_size / BLOCK;
                 const int64_t src = ((int64_t)page * kv.kv_heads + g) * subs, dst = ((int64_t)p.to[entry] * kv.kv_heads + g) * subs;
-                const uint4 *ks = (const uint4 *)(kp + src * BLOCK * dim), *vs = (const uint4 *)(vp + src * BLOCK * dim);
-                uint4 *kd = (uint4 *)(kp + dst * BLOCK * dim), *vd = (uint4 *)(vp + dst * BLOCK * dim);
-                for (int e = threadIdx.x; e < full * dim; e += COPY_THREADS) {
-                    const uint4 k4 = ks[e], v4 = vs[e];
-                    kd[e] = k4;
-                    vd[e] = v4;
-                }
-                for (int e = threadIdx.x; e < full; e += COPY_THREADS) {
-                    c8.k_scales[dst + e] = c8.k_scales[src + e];
-                    c8.v_scales[dst + e] = c8.v_scales[src + e];
-                }
+                uint8_t *pool = (uint8_t *)(what ? kv.v_pages : kv.k_pages);
+                float *scales = what ? c8.v_scales : c8.k_scales;
+                const uint4 *xs = (const uint4 *)(pool + src * BLOCK * dim);
+                uint4 *xd = (uint4 *)(pool + dst * BLOCK * dim);
+#pragma unroll 4
+                for (int e = t; e < full * dim; e += step) xd[e] = xs[e];
+                for (int e = t; e < full; e += step) scales[dst + e] = scales[src + e];
             };
-            if (from >= 0) copy(i, from);
+            if (from >= 0) copy(i, from, threadIdx.x & 1, threadIdx.x >> 1, COPY_THREADS / 2);
             if (from >= -1 || p.to[i] >= 0) continue;
-            // the page stays with this sequence: first those that copy it, with what they have in its last block
-            const int page = -2 - from, old = p.old[i];
-            for (int e = 0; e < i; ++e)
-                if (p.from[e] == from && p.to[e] >= 0) {
-                    copy(e, page);
-                    if (p.old[e] % BLOCK && warp < 2) block(e, p.old[e] / BLOCK, g, warp, page, p.to[e]);
-                }
+            // the page stays with this sequence: first those that copy it, with what they have in its last block, a
+            // warp to keys or values of each
+            const int page = -2 - from;
+            for (int e0 = 0, task = 0; e0 < i; e0 += 32) {
+                const int e = e0 + lane;
+                unsigned theirs = __ballot_sync(0xffffffffu, e < i && p.from[e] == from && p.to[e] >= 0);
+                for (; theirs; theirs &= theirs - 1)
+                    for (int what = 0; what < 2; ++what, ++task) {
+                        if (task % WARPS != warp) continue;
+                        const int y = e0 + __ffs(theirs) - 1, old = p.old[y];
+                        copy(y, page, what, lane, 32);
+                        if (old % BLOCK) block(y, old, old + offsets[y + 1] - offsets[y], old / BLOCK, g, what, page, p.to[y]);
+                    }
+            }
             __syncthreads();
-            const int first = old / BLOCK, last = min(old + offsets[i + 1] - offsets[i] - 1, old - old % kv.page_size + kv.page_size - 1) / BLOCK;
-            for (int w = warp; w < 2 * (last - first + 1); w += WARPS) block(i, first + w / 2, g, w % 2, page, page);
+            const int old = p.old[i], end = old + offsets[i + 1] - offsets[i];
+            const int first = old / BLOCK, last = min(end - 1, old - old % kv.page_size + kv.page_size - 1) / BLOCK;
+            for (int w = warp; w < 2 * (last - first + 1); w += WARPS) block(i, old, end, first + w / 2, g, w % 2, page, page);
         }
         return;
     }
-    const int64_t units = ((int64_t)tokens / BLOCK + 2 * n) * kv.kv_heads * 2;
-    for (int64_t u = (int64_t)blockIdx.x * WARPS + warp; u < units; u += (int64_t)row_blocks * WARPS) {
-        const int place = (int)(u / (2 * kv.kv_heads)), rest = (int)(u - (int64_t)place * 2 * kv.kv_heads);
+    const int64_t all = ((int64_t)tokens / BLOCK + 2 * n) * parts;
+    for (int64_t x = blockIdx.x; x < all; x += row_blocks) {
+        const int place = (int)(x / parts), part = (int)(x - (int64_t)place * parts);
         // the last sequence whose places begin there or before, 32 at a time
         int i = 0;
         for (int m = n; m > 1;) {
@@ -482,7 +485,8 @@ k_append_rows8(opattr_cache8 c8, const int32_t *seqs, int n, const int32_t *offs
         const int from = p.from[i];
         const bool shared = b * BLOCK < old;                      // (with tokens before the call)
         if (from < -1 && (p.to[i] < 0 ? j * kv.page_size < old : shared)) continue;
-        block(i, b, rest >> 1, rest & 1, shared && from >= 0 ? from : page, page);
+        for (int u = part * WARPS + warp; u < 2 * kv.kv_heads; u += parts * WARPS)
+            block(i, old, old + more, b, u >> 1, u & 1, shared && from >= 0 ? from : page, page);
     }
 }
 
@@ -496,12 +500,15 @@ template <typename T>
 static opattr_status rows8_of(Ctx &c, const opattr_cache8 &c8, const int32_t *seqs, int n, const int32_t *offsets, int tokens,
                               const opattr_rows &k, const opattr_rows &v, const AppendPlan &p) {
     const opattr_cache &kv = c8.pages;
-    const unsigned rows = grid_for(((int64_t)tokens / BLOCK + 2 * n) * kv.kv_heads * 2, COPY_THREADS / 32, 8u * sm_count(c));
+    // few places: their heads are shared out, so that every SM has some
+    const int64_t places = (int64_t)tokens / BLOCK + 2 * n, wave = 8 * sm_count(c);
+    const int parts = (int)std::max<int64_t>(1, std::min<int64_t>(wave / places, (2 * kv.kv_heads + COPY_THREADS / 32 - 1) / (COPY_THREADS / 32)));
+    const unsigned rows = (unsigned)std::min<int64_t>(places * parts, 2 * wave);
     const unsigned shared = (unsigned)std::min<int64_t>((int64_t)n * kv.kv_heads, 2 * sm_count(c));
     if (kv.head_dim <= 64)
-        launch(c, "append_rows8", k_append_rows8<T, 64>, dim3(rows + shared), dim3(COPY_THREADS), 0, c8, seqs, n, offsets, tokens, k, v, p, rows);
+        launch(c, "append_rows8", k_append_rows8<T, 64>, dim3(rows + shared), dim3(COPY_THREADS), 0, c8, seqs, n, offsets, tokens, k, v, p, rows, parts);
     else
-        launch(c, "append_rows8", k_append_rows8<T, 128>, dim3(rows + shared), dim3(COPY_THREADS), 0, c8, seqs, n, offsets, tokens, k, v, p, rows);
+        launch(c, "append_rows8", k_append_rows8<T, 128>, dim3(rows + shared), dim3(COPY_THREADS), 0, c8, seqs, n, offsets, tokens, k, v, p, rows, parts);
     return cuda_status(c, c.last_error);
 }
 

@@ -28,7 +28,7 @@ struct Serve {
 };
 constexpr int SILENT_PARTS = -1;
 
-constexpr int TICKETS = 4096;        // at most three blocks an SM count in them
+constexpr int TICKETS = 4096;        // at most four blocks an SM, or their sixteen warps, count in them
 opattr_status serve_ready(Ctx &c, Serve &s);
 void serve_free(Serve &s);
 

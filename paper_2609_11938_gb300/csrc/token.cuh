@@ -55,6 +55,9 @@ constexpr float JOIN_STEPS = 12.f;
 #ifndef E8_BLOCKS
 #define E8_BLOCKS (DP == 64 ? 4 : 3)
 #endif
+#ifndef E8_TEAMS
+#define E8_TEAMS 1
+#endif
 #ifndef E8_F64
 #define E8_F64 2
 #endif
@@ -174,22 +177,30 @@ __device__ __forceinline__ void fma_pair(float &a, float &b, float x, float y, f
 }
 
 // DP: the padded head width; NT: eights of queries; FR: sixteens of keys that a
-// warp takes at a time; E8: pages of 8 bits; WIN: through a window.
-template <typename T, int DP, int NT, int FR, bool E8, bool WIN>
+// warp takes at a time; E8: pages of 8 bits; WIN: through a window.  TW: warps that share a pair's
+// keys: all of a block, or each by itself.
+template <typename T, int DP, int NT, int FR, bool E8, bool WIN, int TW>
 __global__ void __launch_bounds__(TOKEN_THREADS, E8 ? (NT == 1 ? E8_BLOCKS : 2) : NT == 1 ? 3 : 2) k_token(const __grid_constant__ TokenArgs p, unsigned *err) {
     using P = std::conditional_t<E8, __half, T>;          // what the products take
     constexpr bool BF = std::is_same<P, __nv_bfloat16>::value;
     // as in prompt.cu: weights up to 2^(OFFSET + SLACK), rescaled when a maximum outgrows SLACK
     constexpr float OFFSET = BF ? 0.f : 8.f, SLACK = BF ? 8.f : 7.f;
-    constexpr int KC = DP / (E8 ? 64 : 32), VC = DP / 64, STEP = 16 * FR * TOKEN_WARPS, NQ = 8 * NT, ROW = DP + 4;
+    constexpr int KC = DP / (E8 ? 64 : 32), VC = DP / 64, STEP = 16 * FR * TW, NQ = 8 * NT, ROW = DP + 4;
     __shared__ float so[TOKEN_WARPS][NQ][ROW];
     __shared__ float sm[TOKEN_WARPS][NQ], sl[TOKEN_WARPS][NQ];
     __shared__ long long warp_buf[33];
-    __shared__ long long first_at;
-    __shared__ int first_seq, last_one;
+    constexpr int TEAMS = TOKEN_WARPS / TW;                    // of a block
+    __shared__ long long first_at[TEAMS];
+    __shared__ int first_seq[TEAMS], last_one;
     pdl_wait();
     const opattr_cache &kv = p.kv;
     const int lane = lane_id(), warp = threadIdx.x >> 5, row = lane >> 2, col = lane & 3;
+    const int mate = TW == 1 ? 0 : warp, own = TW == 1 ? warp : 0, me = TW == 1 ? lane : (int)threadIdx.x;
+    const int team = TW == 1 ? (int)blockIdx.x * TOKEN_WARPS + warp : (int)blockIdx.x;
+    auto together = [] {
+        if (TW == 1) __syncwarp();
+        else __syncthreads();
+    };
     const int units = kv.kv_heads * p.blocks_of_heads;
 
     // ---- this block's run
@@ -226,25 +237,31 @@ __global__ void __launch_bounds__(TOKEN_THREADS, E8 ? (NT == 1 ? E8_BLOCKS : 2) 
     long long at = block_exclusive_scan(mine, warp_buf, &total);
     const long long pairs = (long long)p.n * units;
     // (in 32 bits, where no grid comes near their end: 64 took 0.3 us of every launch)
-    const int blocks = (int)gridDim.x, few = (int)min(total, 1ll << 30), few_pairs = (int)min(pairs, 1ll << 30);
+    const int blocks = (int)gridDim.x * TEAMS, few = (int)min(total, 1ll << 30), few_pairs = (int)min(pairs, 1ll << 30);
     const long long W = min(min(few, blocks), (int)fminf(1e6f, root(JOIN_STEPS * (float)few * (float)few_pairs)));
-    if (blockIdx.x >= W) return;
-    const long long s0 = blockIdx.x * total / W, s1 = (blockIdx.x + 1) * total / W;
-    if (s0 >= at && s0 < at + mine) {
-        int b = b0;
-        for (;; ++b) {
-            const long long of = (long long)cost_of(count_of(len_of(seq_of(b)))) * units;
-            if (s0 < at + of) break;
-            at += of;
+    if ((long long)blockIdx.x * TEAMS >= W) return;
+#pragma unroll
+    for (int x = 0; x < TEAMS; ++x) {
+        const long long begin = ((long long)blockIdx.x * TEAMS + x) * total / W;
+        if (begin >= at && begin < at + mine) {
+            int b = b0;
+            long long here = at;
+            for (;; ++b) {
+                const long long of = (long long)cost_of(count_of(len_of(seq_of(b)))) * units;
+                if (begin < here + of) break;
+                here += of;
+            }
+            first_seq[x] = b;
+            first_at[x] = here;
         }
-        first_seq = b;
-        first_at = at;
     }
+    const long long s0 = team * total / W, s1 = (team + 1ll) * total / W;
     __syncthreads();
+    if (TW == 1 && team >= W) return;
 
     // ---- its pairs, one after another
-    int b = first_seq;
-    long long base = first_at;                    // where sequence b's steps begin
+    int b = first_seq[own];
+    long long base = first_at[own];                    // where sequence b's steps begin
     const float c = p.scale * LOG2E;
     for (long long s = s0; s < s1;) {
         int head, gap;
@@ -296,7 +313,7 @@ __global__ void __launch_bounds__(TOKEN_THREADS, E8 ? (NT == 1 ? E8_BLOCKS : 2) 
         const int last = WIN ? len : (int)min((unsigned)len, (unsigned)to * STEP);  // keys of this run: from * STEP .. last
         // the first of the keys that this warp's f-th lot of a step has
         auto key_at = [&](int step, int f) {
-            unsigned x = (unsigned)step * (STEP / 16) + (warp * FR + f);
+            unsigned x = (unsigned)step * (STEP / 16) + (mate * FR + f);
             if (WIN && x >= (unsigned)head) x += gap;
             return 16 * x;
         };
@@ -589,7 +606,7 @@ __global__ void __launch_bounds__(TOKEN_THREADS, E8 ? (NT == 1 ? E8_BLOCKS : 2) 
                     *reinterpret_cast<float4 *>(at + 4) = make_float4(o[t][4 * i + 2][q], o[t][4 * i + 2][q + 2], o[t][4 * i + 3][q], o[t][4 * i + 3][q + 2]);
                 }
             }
-        __syncthreads();
+        together();
         const bool whole = from == 0 && to == steps;
         constexpr int PART = NQ * (DP + 2);
         auto finish = [&](int h, int d, float top, float sum, const float *y) {
@@ -604,15 +621,15 @@ __global__ void __launch_bounds__(TOKEN_THREADS, E8 ? (NT == 1 ? E8_BLOCKS : 2) 
                 p.lse[(long long)b * p.q_heads + head0 + h] =
                     sum == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) - OFFSET + log2f(sum)) * LN2;
         };
-        float *part = p.parts + ((long long)blockIdx.x * 2 + (from == 0)) * PART;
-        for (int i = threadIdx.x; i < NQ * (DP / 8); i += TOKEN_THREADS) {
+        float *part = p.parts + ((long long)team * 2 + (from == 0)) * PART;
+        for (int i = me; i < NQ * (DP / 8); i += 32 * TW) {
             const int h = i / (DP / 8), d = i % (DP / 8) * 8;
             if (h >= heads || d >= kv.head_dim) continue;
             float top = -INFINITY, sum = 0.f, y[8] = {};
 #pragma unroll
-            for (int w = 0; w < TOKEN_WARPS; ++w) top = fmaxf(top, sm[w][h]);
+            for (int w = own; w < own + TW; ++w) top = fmaxf(top, sm[w][h]);
 #pragma unroll
-            for (int w = 0; w < TOKEN_WARPS; ++w) {
+            for (int w = own; w < own + TW; ++w) {
                 const float keep = sm[w][h] == top ? 1.f : exp2_fast(sm[w][h] - top);
                 sum = __fmaf_rn(sl[w][h], keep, sum);
 #pragma unroll
@@ -629,12 +646,19 @@ __global__ void __launch_bounds__(TOKEN_THREADS, E8 ? (NT == 1 ? E8_BLOCKS : 2) 
             // a pair's parts: the block it begins in keeps its own in place 1, later ones in place 0
             const int block1 = (int)(((unit_at + 1) * W - 1) / total), block2 = (int)(((unit_at + steps) * W - 1) / total);
             __threadfence();
-            __syncthreads();
-            if (threadIdx.x == 0) last_one = atomicAdd(&p.tickets[block1], 1u) == (unsigned)(block2 - block1);
-            __syncthreads();
-            if (last_one) {
+            together();
+            int last = 0;
+            if (me == 0) last = atomicAdd(&p.tickets[block1], 1u) == (unsigned)(block2 - block1);
+            if (TW == 1) {
+                last = __shfl_sync(0xffffffffu, last, 0);
+            } else {
+                if (me == 0) last_one = last;
+                together();
+                last = last_one;
+            }
+            if (last) {
                 __threadfence();
-                for (int i = threadIdx.x; i < NQ * (DP / 8); i += TOKEN_THREADS) {
+                for (int i = me; i < NQ * (DP / 8); i += 32 * TW) {
                     const int h = i / (DP / 8), d = i % (DP / 8) * 8;
                     if (h >= heads || d >= kv.head_dim) continue;
                     float top = -INFINITY, sum = 0.f, y[8] = {};
@@ -654,27 +678,35 @@ __global__ void __launch_bounds__(TOKEN_THREADS, E8 ? (NT == 1 ? E8_BLOCKS : 2) 
                     }
                     finish(h, d, top, sum, y);
                 }
-                if (threadIdx.x == 0) p.tickets[block1] = 0;
+                if (me == 0) p.tickets[block1] = 0;
             }
         }
-        __syncthreads();
+        together();
     }
 }
 
-template <typename T, int DP, int NT, int FR, bool E8, bool WIN>
-static opattr_status run_token(Ctx &c, Serve &s, TokenArgs &p) {
+template <typename T, int DP, int NT, int FR, bool E8, bool WIN, int TW>
+static opattr_status run_teams(Ctx &c, Serve &s, TokenArgs &p) {
     const int64_t most = (int64_t)p.n * p.kv.kv_heads * p.blocks_of_heads *
-                         (((int64_t)p.kv.pages_per_seq * p.kv.page_size + 16 * FR * TOKEN_WARPS - 1) / (16 * FR * TOKEN_WARPS));
-    const int grid = (int)std::min<int64_t>((E8 ? (NT == 1 ? E8_BLOCKS : 2) : NT == 1 ? 3 : 2) * (int64_t)sm_count(c), most);
+                         (((int64_t)p.kv.pages_per_seq * p.kv.page_size + 16 * FR * TW - 1) / (16 * FR * TW));
+    constexpr int TEAMS = TOKEN_WARPS / TW;
+    const int grid = (int)std::min<int64_t>((E8 ? (NT == 1 ? E8_BLOCKS : 2) : NT == 1 ? 3 : 2) * (int64_t)sm_count(c), std::min<int64_t>((most + TEAMS - 1) / TEAMS, TICKETS / TEAMS));
     opattr_status st = serve_ready(c, s);
     if (st) return st;
     const int64_t part = (int64_t)8 * NT * (DP + 2);
-    if ((st = ensure_lasting_arena(c, Need().add<float>(2 * grid * part).bytes))) return st;
+    if ((st = ensure_lasting_arena(c, Need().add<float>(2 * (int64_t)grid * TEAMS * part).bytes))) return st;
     Arena a(c);
-    p.parts = a.take<float>(2 * grid * part);
+    p.parts = a.take<float>(2 * (int64_t)grid * TEAMS * part);
     p.tickets = s.tickets;
-    launch(c, E8 ? "token8" : "token", k_token<T, DP, NT, FR, E8, WIN>, dim3(grid), dim3(TOKEN_THREADS), 0, p, s.err);
+    launch(c, E8 ? "token8" : "token", k_token<T, DP, NT, FR, E8, WIN, TW>, dim3(grid), dim3(TOKEN_THREADS), 0, p, s.err);
     return cuda_status(c, c.last_error);
+}
+template <typename T, int DP, int NT, int FR, bool E8, bool WIN>
+static opattr_status run_token(Ctx &c, Serve &s, TokenArgs &p) {
+    if constexpr (E8) {
+        if ((int64_t)p.n * p.kv.kv_heads * p.blocks_of_heads >= E8_TEAMS * (int64_t)sm_count(c) * TOKEN_WARPS * (NT == 1 ? E8_BLOCKS : 2)) return run_teams<T, DP, NT, FR, E8, WIN, 1>(c, s, p);
+    }
+    return run_teams<T, DP, NT, FR, E8, WIN, TOKEN_WARPS>(c, s, p);
 }
 template <typename T, bool E8, bool WIN>
 static opattr_status token_of(Ctx &c, Serve &s, TokenArgs &p) {
