@@ -12,7 +12,7 @@ bool rows_ok(const opattr_rows &r, int64_t tokens, int heads, int dim) {
     return dim % 8 == 0;
 }
 
-opattr_status prompt_plain(Ctx &c, Serve &s, PromptArgs &p, const CUtensorMap *m) {
+opattr_status prompt_plain(Ctx &c, Serve &s, PromptArgs &p, const Maps<true> &m) {
     return p.a.dtype == OPATTR_BF16 ? prompt_of<__nv_bfloat16, false>(c, s, p, m) : prompt_of<__half, false>(c, s, p, m);
 }
 
@@ -85,13 +85,17 @@ opattr_status do_attention(Ctx &c, Serve &s, const opattr_prompt *a, int32_t win
     p.v_mul = a->kv_heads > 1 && a->v.head_stride != 0;
     if (!encode_tiled()) return OPATTR_E_CUDA;
     // without keys there is nothing to copy, and any rows stand in for them
-    CUtensorMap m[3];
+    Maps<true> m;
     const opattr_rows &k = a->k_tokens ? a->k : a->q, &v = a->k_tokens ? a->v : a->q;
     const int64_t keys = a->k_tokens ? a->k_tokens : 1;
-    if (!row_map(&m[0], a->dtype, a->q, a->q_tokens, a->q_heads, a->head_dim, p.pack, p.span) ||
-        !row_map(&m[1], a->dtype, k, keys, a->kv_heads, a->head_dim, 1, KEYS) ||
-        !row_map(&m[2], a->dtype, v, keys, a->kv_heads, a->head_dim, 1, KEYS))
+    if (!row_map(&m.q, a->dtype, a->q, a->q_tokens, a->q_heads, a->head_dim, p.pack, p.span) ||
+        !row_map(&m.k, a->dtype, k, keys, a->kv_heads, a->head_dim, 1, KEYS) ||
+        !row_map(&m.v, a->dtype, v, keys, a->kv_heads, a->head_dim, 1, KEYS))
         return OPATTR_E_INVALID_ARG;
+    if (sinks > 0 && (!row_map(&m.k16, a->dtype, k, keys, a->kv_heads, a->head_dim, 1, SIXTEEN) ||
+                      !row_map(&m.v16, a->dtype, v, keys, a->kv_heads, a->head_dim, 1, SIXTEEN)))
+        return OPATTR_E_INVALID_ARG;
+    if (window && sinks == 0) m.k16 = m.k, m.v16 = m.v;  // (no copy goes by them)
     return window ? prompt_window(c, s, p, m) : prompt_plain(c, s, p, m);
 }
 

@@ -40,6 +40,7 @@
 namespace opattr {
 
 constexpr int KEYS = 128;                // keys of a tile
+constexpr int SIXTEEN = 16;              // rows of a copy that is put together with others to a tile
 constexpr int ROWS = 128;                // rows of a sub-tile: one thread and one lane of tensor memory each
 constexpr int THREADS = 384;             // two warpgroups for the softmax of two sub-tiles, one for the rest
 constexpr int MMA_WARP = 8, LOAD_WARP = 9, TAIL_WARP = 10;   // and the last one looks up items
@@ -81,6 +82,16 @@ struct PromptArgs {
     unsigned limit_us;                   // of every wait
     int silent;                          // Serve::silent
     int window, sinks;                   // (through a window) last keys that a query sees, and first ones
+};
+
+// Of the queries, keys and values; and of the keys and values sixteen rows at a time.
+template <bool WIN>
+struct Maps {
+    CUtensorMap q, k, v;
+};
+template <>
+struct Maps<true> : Maps<false> {
+    CUtensorMap k16, v16;
 };
 
 // A work item: two sub-tiles of queries of one sequence, and keys of it.
@@ -133,57 +144,58 @@ struct Work {
     }
     // For all lanes of a warp, which take the same branches with it.
     __device__ __forceinline__ void all_lanes() { cut = uniform(cut); }
-    __device__ __forceinline__ int place(int j) const { return j; }
+    __device__ __forceinline__ int key(int j) const { return j * KEYS; }
     __device__ __forceinline__ bool looked_over(int j) const { return j >= cut; }
     __device__ __forceinline__ bool masked(int s, int j) const { return j >= (s ? clean[1] : clean[0]); }
 };
 
-// Through a window the key tiles that no row of the item sees are left out: tiles count on from
-// the `head` ones that have the sinks to those from the first row's window on, `gap` further.
-// (A later row's window begins further on; what an item has of that is masked.)
+// Through a window the keys that no row of the item sees are left out: the item's tiles are of the
+// sinks, filled up to whole sixteens (`sunk` rows, of which no more than the sinks are seen), and from
+// there on of the keys from the first row's window on.  (A later row's window begins further on; what
+// an item has of that is masked.)
 template <bool CUT>
 struct Work<true, CUT> {
-    int base[2], tiles[2], clean[2];     // (clean: a key tile's own number, as the places below)
+    int base[2], tiles[2], clean[2];     // first query; key tiles; the first of them that a row's end cuts
     int low[2];                          // tiles below it are cut by the window of the sub-tile's last row
-    int n, cut, below, head, gap, from;  // below: as low, of either; from: tiles before this part
-    int sunk;                            // tiles of nothing but sinks
+    int n, cut, below, from;             // key tiles of either; clean and low of either; tiles before this part
+    int sunk, gap, whole;                // rows of sinks; keys left out after them; tiles of nothing but sinks
     // the first key of the window of the query that stands at p
     static __device__ __forceinline__ int edge(int p, int window) { return p >= window ? p - window + 1 : 0; }
     __device__ __forceinline__ Work(const Item &it, const PromptArgs &p) {
         const int ahead = it.ahead;
         const int first = edge(it.t0 + ahead, p.window), few = min(p.sinks, first);
-        head = min(first / KEYS, (int)(((unsigned)few + KEYS - 1) / KEYS));
-        gap = first / KEYS - head;
+        sunk = (int)(((unsigned)few + SIXTEEN - 1) / SIXTEEN * SIXTEEN);
+        if (sunk >= first) sunk = 0, gap = 0;            // (nothing is left out)
+        else gap = first - sunk;
+        whole = (gap ? few : p.sinks) / KEYS;
         from = CUT ? it.from : 0;
-        sunk = p.sinks / KEYS;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             base[s] = (int)((unsigned)it.t0 + s * p.span);
             const int rows = min(p.span, (int)((unsigned)it.lq - base[s]));
-            const int keys = rows <= 0 ? 0 : max(0, min(it.lk, base[s] + rows + ahead));
-            const int all = ((unsigned)keys + KEYS - 1) / KEYS;
-            tiles[s] = all > head ? all - gap : all;
-            clean[s] = max(0, min(it.lk, (int)((unsigned)base[s] + 1 + ahead))) / KEYS;
-            low[s] = rows <= 0 ? 0 : ((unsigned)edge(base[s] + rows - 1 + ahead, p.window) + KEYS - 1) / KEYS;
+            const int keys = rows <= 0 ? 0 : max(0, min(it.lk, base[s] + rows + ahead) - gap);
+            tiles[s] = ((unsigned)keys + KEYS - 1) / KEYS;
+            clean[s] = max(0, min(it.lk, (int)((unsigned)base[s] + 1 + ahead)) - gap) / KEYS;
+            low[s] = rows <= 0 ? 0 : ((unsigned)max(0, edge(base[s] + rows - 1 + ahead, p.window) - gap) + KEYS - 1) / KEYS;
         }
         n = max(tiles[0], tiles[1]);
         if (CUT) n = min(n, it.to) - from;
+        cut = base[1] < it.lq && base[1] >= 0 ? min(clean[0], clean[1]) : clean[0];
 #pragma unroll
         for (int s = 0; s < 2; ++s) tiles[s] = CUT ? max(0, min(tiles[s] - from, n)) : tiles[s];
-        cut = base[1] < it.lq && base[1] >= 0 ? min(clean[0], clean[1]) : clean[0];
         below = max(low[0], low[1]);
     }
-    __device__ __forceinline__ void all_lanes() {
-        cut = uniform(cut), below = uniform(below), head = uniform(head), gap = uniform(gap), from = uniform(from), sunk = uniform(sunk);
-    }
-    __device__ __forceinline__ int place(int j) const { return from + j + (from + j >= head ? gap : 0); }
+    __device__ __forceinline__ void all_lanes() { cut = uniform(cut), below = uniform(below), from = uniform(from), whole = uniform(whole); }
+    // the key of a tile's first row, were it not a sink's; and that of a sink's
+    __device__ __forceinline__ int key(int j) const { return (from + j) * KEYS + gap; }
+    __device__ __forceinline__ int sink(int j) const { return (from + j) * KEYS; }
     __device__ __forceinline__ bool looked_over(int j) const {
-        const int x = place(j);
-        return x >= cut || (x < below && x >= sunk);
+        const int x = from + j;
+        return x >= cut || (x < below && x >= whole);
     }
     __device__ __forceinline__ bool masked(int s, int j) const {
-        const int x = place(j);
-        return x >= (s ? clean[1] : clean[0]) || (x < (s ? low[1] : low[0]) && x >= sunk);
+        const int x = from + j;
+        return x >= (s ? clean[1] : clean[0]) || (x < (s ? low[1] : low[0]) && x >= whole);
     }
 };
 
@@ -196,6 +208,13 @@ __device__ __forceinline__ uint32_t tm_ld1(uint32_t at) {
     uint32_t r;
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(at));
     return r;
+}
+
+// The lowest n bits; none below 1, and all from 32 on.
+__device__ __forceinline__ uint32_t bits_below(int n) {
+    uint32_t r;
+    asm("shl.b32 %0, 1, %1;" : "=r"(r) : "r"(max(n, 0)));
+    return r - 1;
 }
 
 // 32 bytes of a thread in one store: whole sectors, where rows lie far apart.
@@ -220,8 +239,7 @@ __device__ __forceinline__ unsigned draw(unsigned *next, unsigned total) {
 // window.
 template <typename T, int DP, int DV, bool CUT, bool WIN>
 __global__ void __launch_bounds__(THREADS, 1)
-k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorMap mq,
-         const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, unsigned *err) {
+k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ Maps<WIN> maps, unsigned *err) {
     using S = Shape<DP>;
     constexpr bool BF = std::is_same<T, __nv_bfloat16>::value;
     // Weights stand at up to 2^(OFFSET + SLACK): the accumulator is rescaled only
@@ -254,7 +272,8 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
         bar_init(smem_addr(&ctl.drain), 1);
         ctl.stop = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        map_prefetch(&mq), map_prefetch(&mk), map_prefetch(&mv);
+        map_prefetch(&maps.q), map_prefetch(&maps.k), map_prefetch(&maps.v);
+        if constexpr (WIN) map_prefetch(&maps.k16), map_prefetch(&maps.v16);
     }
     if (warp == MMA_WARP) tm_alloc(smem_addr(&ctl.tmem), 512);
     tm_before();
@@ -320,14 +339,15 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                     tm_wait_ld();
                     if (w.masked(s, j)) {
                         // of the 32s of keys that a mask cuts, most are seen by all of the warp's rows
-                        const int at = w.place(j) * KEYS, left = (int)((unsigned)seen - at);
+                        const int at = w.key(j), left = (int)((unsigned)seen - at);
 #pragma unroll
                         for (int q = 0; q < KEYS; q += 32) {
                             if constexpr (WIN) {
-                                const int low = edge - at - q, few = p.sinks - at - q;
-                                if (__all_sync(0xffffffffu, left >= q + 32 && (low <= 0 || few >= 32))) continue;
+                                // a bit for each that is seen
+                                const uint32_t some = bits_below(left - q) & (~bits_below(edge - at - q) | bits_below(p.sinks - w.sink(j) - q));
+                                if (__all_sync(0xffffffffu, some == 0xffffffffu)) continue;
 #pragma unroll
-                                for (int i = 0; i < 32; ++i) x[q + i] = i < left - q && (i >= low || i < few) ? x[q + i] : 0xff800000u;
+                                for (int i = 0; i < 32; ++i) x[q + i] = some >> i & 1 ? x[q + i] : 0xff800000u;
                             } else {
                                 if (__all_sync(0xffffffffu, left >= q + 32)) continue;
 #pragma unroll
@@ -397,7 +417,9 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                         if (!(ok = warp_wait(smem_addr(&ctl.v_ready[over.at]), over.ph, stop, p.limit_us))) break;
                         if (seldom(*(volatile int *)&ctl.poison[over.at])) {
                             const unsigned char *v = smem + 2 * S::TILE + ring.at * S::TILE;
-                            const int at = w.place(j) * KEYS, left = (int)((unsigned)seen - at);
+                            const int at = w.key(j), left = (int)((unsigned)seen - at);
+                            int few = 0;
+                            if constexpr (WIN) few = p.sinks - w.sink(j);
 #pragma unroll 1
                             for (int d = 0; d < DP; d += 32) {
                                 uint32_t o[32] = {};
@@ -419,7 +441,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                                         for (int q = 0; q < 4; ++q) {
                                             const float2 y = Type2<T>::up(uu[q]);
                                             uint32_t *z = o + e + 2 * q;
-                                            if (i < left && (!WIN || i >= edge - at || i < p.sinks - at)) {
+                                            if (i < left && (!WIN || i >= edge - at || i < few)) {
                                                 z[0] = __float_as_uint(__fmaf_rn(weight, y.x, __uint_as_float(z[0])));
                                                 z[1] = __float_as_uint(__fmaf_rn(weight, y.y, __uint_as_float(z[1])));
                                             }
@@ -692,7 +714,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                             bar_expect(bq, subs * p.pack * p.span * DP * 2);
                             for (int s = 0; s < subs; ++s)
                                 for (int d = 0; d < DP / 64; ++d)
-                                    tile_load(sq + s * S::TILE + d * S::HALF, &mq, 64 * d, it.head0 * p.q_mul,
+                                    tile_load(sq + s * S::TILE + d * S::HALF, &maps.q, 64 * d, it.head0 * p.q_mul,
                                               it.q0 + (s ? w.base[1] : w.base[0]), bq);
                         }
                         q_out = 1;
@@ -704,9 +726,20 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                     const uint32_t bar = cut ? smem_addr(&ctl.v_full[over.at]) : bar_kv + 8 * ring.at;
                     if (lead) {
                         bar_expect(bar, S::TILE);
-                        for (int d = 0; d < DP / 64; ++d)
-                            tile_load(skv + ring.at * S::TILE + d * S::HALF, keys ? &mk : &mv, 64 * d, g * (keys ? p.k_mul : p.v_mul),
-                                      it.k0 + w.place(load / 2) * KEYS, bar);
+                        const int head = g * (keys ? p.k_mul : p.v_mul);
+                        const uint32_t to = skv + ring.at * S::TILE;
+                        bool sinks = false;
+                        if constexpr (WIN) {
+                            const int few = w.sunk - w.sink(load / 2);
+                            sinks = few > 0;
+                            if (sinks)
+                                for (int r = 0; r < KEYS; r += SIXTEEN)
+                                    for (int d = 0; d < DP / 64; ++d)
+                                        tile_load(to + d * S::HALF + r * 128, keys ? &maps.k16 : &maps.v16, 64 * d, head,
+                                                  it.k0 + (r < few ? w.sink(load / 2) : w.key(load / 2)) + r, bar);
+                        }
+                        if (!sinks)
+                            for (int d = 0; d < DP / 64; ++d) tile_load(to + d * S::HALF, keys ? &maps.k : &maps.v, 64 * d, head, it.k0 + w.key(load / 2), bar);
                         if (cut) bar_arrive(bar_kv + 8 * ring.at);
                     }
                     bars[ring.at] = bar;
@@ -735,7 +768,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ CUtensorM
                     if (!w.looked_over(j)) continue;
                     if (!(ok = warp_wait(smem_addr(&ctl.v_full[over.at]), over.ph, stop, p.limit_us))) break;
                     uint4 *v = reinterpret_cast<uint4 *>(smem + 2 * S::TILE + ring.at * S::TILE);
-                    const int keys = min(KEYS, it.lk - w.place(j) * KEYS);
+                    const int keys = min(KEYS, it.lk - w.key(j));
                     unsigned most = 0;
                     for (int d = 0; d < DP / 64; ++d) {
                         if (a.causal) {
@@ -944,18 +977,18 @@ __global__ void __launch_bounds__(1024) k_prompt_plan(PromptArgs p, int blocks, 
 
 // ---------------------------------------------------------------- host
 template <typename T, int DP, int DV, bool CUT, bool WIN>
-static opattr_status launch_prompt(Ctx &c, Serve &s, const PromptArgs &p, const CUtensorMap *m, unsigned grid) {
+static opattr_status launch_prompt(Ctx &c, Serve &s, const PromptArgs &p, const Maps<true> &m, unsigned grid) {
     constexpr unsigned bit = 1u << (2 * ((std::is_same<T, __half>::value ? 3 : 0) + (DP == 64 ? 0 : DV == 96 ? 1 : 2)) + CUT + (WIN ? 12 : 0));
     if (!(s.prompt_room & bit)) {
         const cudaError_t e = cudaFuncSetAttribute(k_prompt<T, DP, DV, CUT, WIN>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<DP>::SMEM);
         if (e != cudaSuccess) return cuda_status(c, e);
         s.prompt_room |= bit;
     }
-    launch(c, "prompt", k_prompt<T, DP, DV, CUT, WIN>, dim3(grid), dim3(THREADS), Shape<DP>::SMEM, p, m[0], m[1], m[2], s.err);
+    launch(c, "prompt", k_prompt<T, DP, DV, CUT, WIN>, dim3(grid), dim3(THREADS), Shape<DP>::SMEM, p, static_cast<const Maps<WIN> &>(m), s.err);
     return cuda_status(c, c.last_error);
 }
 template <typename T, int DP, int DV, bool WIN>
-static opattr_status run_prompt(Ctx &c, Serve &s, PromptArgs &p, const CUtensorMap *m) {
+static opattr_status run_prompt(Ctx &c, Serve &s, PromptArgs &p, const Maps<true> &m) {
     const opattr_prompt &a = p.a;
     const int64_t items = (int64_t)p.heads_x * p.tiles;
     const int sms = sm_count(c);
@@ -992,13 +1025,13 @@ static opattr_status run_prompt(Ctx &c, Serve &s, PromptArgs &p, const CUtensorM
 }
 
 template <typename T, bool WIN>
-static opattr_status prompt_of(Ctx &c, Serve &s, PromptArgs &p, const CUtensorMap *m) {
+static opattr_status prompt_of(Ctx &c, Serve &s, PromptArgs &p, const Maps<true> &m) {
     if (p.a.head_dim <= 64) return run_prompt<T, 64, 64, WIN>(c, s, p, m);
     return p.a.head_dim <= 96 ? run_prompt<T, 128, 96, WIN>(c, s, p, m) : run_prompt<T, 128, 128, WIN>(c, s, p, m);
 }
 
 // Each in a file of its own, which compiles beside the other.
-opattr_status prompt_plain(Ctx &c, Serve &s, PromptArgs &p, const CUtensorMap *m);
-opattr_status prompt_window(Ctx &c, Serve &s, PromptArgs &p, const CUtensorMap *m);
+opattr_status prompt_plain(Ctx &c, Serve &s, PromptArgs &p, const Maps<true> &m);
+opattr_status prompt_window(Ctx &c, Serve &s, PromptArgs &p, const Maps<true> &m);
 
 }  // namespace opattr

@@ -3,7 +3,7 @@
 
 namespace opattr {
 
-opattr_status prompt_window(Ctx &c, Serve &s, PromptArgs &p, const CUtensorMap *m) {
+opattr_status prompt_window(Ctx &c, Serve &s, PromptArgs &p, const Maps<true> &m) {
     return p.a.dtype == OPATTR_BF16 ? prompt_of<__nv_bfloat16, true>(c, s, p, m) : prompt_of<__half, true>(c, s, p, m);
 }
 
