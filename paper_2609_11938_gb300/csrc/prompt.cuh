@@ -756,7 +756,6 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ Maps<WIN>
         } else if (warp == TAIL_WARP) {
             // ---- value tiles that a mask cuts: rows past the sequence's keys become zeros, and,
             // causal, the others are looked over for values that are not finite
-            constexpr unsigned INF = BF ? 0x7f80u : 0x7c00u;
             Place<CUTS> over;
             Place<S::STAGES> ring;
             ring.step();
@@ -769,19 +768,20 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ Maps<WIN>
                     if (!(ok = warp_wait(smem_addr(&ctl.v_full[over.at]), over.ph, stop, p.limit_us))) break;
                     uint4 *v = reinterpret_cast<uint4 *>(smem + 2 * S::TILE + ring.at * S::TILE);
                     const int keys = min(KEYS, it.lk - w.key(j));
-                    unsigned most = 0;
+                    // (zero times what is not finite is NaN, and stays it in a sum)
+                    uint32_t sum[4] = {};
                     for (int d = 0; d < DP / 64; ++d) {
                         if (a.causal) {
 #pragma unroll 8
                             for (int i = lane_id(); i < keys * 8; i += 32) {
                                 const uint4 y = v[d * (S::HALF / 16) + i];
-                                most = __vmaxu2(most, __vmaxu2(__vmaxu2(y.x & 0x7fff7fffu, y.y & 0x7fff7fffu),
-                                                               __vmaxu2(y.z & 0x7fff7fffu, y.w & 0x7fff7fffu)));
+                                sum[0] = Type2<T>::add_zeros(y.x, sum[0]), sum[1] = Type2<T>::add_zeros(y.y, sum[1]);
+                                sum[2] = Type2<T>::add_zeros(y.z, sum[2]), sum[3] = Type2<T>::add_zeros(y.w, sum[3]);
                             }
                         }
                         for (int i = keys * 8 + lane_id(); i < S::HALF / 16; i += 32) v[d * (S::HALF / 16) + i] = make_uint4(0, 0, 0, 0);
                     }
-                    const bool found = __any_sync(0xffffffffu, (most >> 16) >= INF || (most & 0xffffu) >= INF);
+                    const bool found = __any_sync(0xffffffffu, (sum[0] | sum[1] | sum[2] | sum[3]) & 0x7fff7fffu);
                     fence_smem_async();
                     __syncwarp();
                     if (lane_id() == 0) {

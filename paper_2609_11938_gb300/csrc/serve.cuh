@@ -45,6 +45,12 @@ struct Type2<__nv_bfloat16> {
         asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
         return r;
     }
+    // 0 x + sum, for both values
+    static __device__ __forceinline__ uint32_t add_zeros(uint32_t x, uint32_t sum) {
+        uint32_t r;
+        asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(x), "r"(0u), "r"(sum));
+        return r;
+    }
 };
 template <>
 struct Type2<__half> {
@@ -54,6 +60,11 @@ struct Type2<__half> {
     static __device__ __forceinline__ uint32_t down(float lo, float hi) {
         uint32_t r;
         asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+        return r;
+    }
+    static __device__ __forceinline__ uint32_t add_zeros(uint32_t x, uint32_t sum) {
+        uint32_t r;
+        asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(x), "r"(0u), "r"(sum));
         return r;
     }
 };
