@@ -410,9 +410,30 @@ __global__ void __launch_bounds__(TOKEN_THREADS, E8 ? (NT == 1 ? E8_BLOCKS : 2) 
                     }
                 }
             } else {
+                if constexpr (WIN) {
+                    kall = kv.head_dim == DP;
+#pragma unroll
+                    for (int f = 0; f < FR; ++f) {
+                        kat[f] = rows_at(step, f, klim[f]);
+                        kall = kall && klim[f] >= 16 && (klim[f] <= near || klim[f] + far >= 16);
+                    }
+                }
+                if (WIN && kall) {
+#pragma unroll
+                    for (int f = 0; f < FR; ++f) {
+                        const uint8_t *at = (const uint8_t *)((const T *)kv.k_pages + kat[f] + (row * DP + 8 * col));
+                        kr[f][0][0] = get16<0>(at), kr[f][1][0] = get16<16 * DP>(at);
+                        kr[f][0][1] = get16<64>(at), kr[f][1][1] = get16<16 * DP + 64>(at);
+                        if constexpr (DP == 128) {
+                            kr[f][0][KC - 2] = get16<128>(at), kr[f][1][KC - 2] = get16<16 * DP + 128>(at);
+                            kr[f][0][KC - 1] = get16<192>(at), kr[f][1][KC - 1] = get16<16 * DP + 192>(at);
+                        }
+                    }
+                    return;
+                }
 #pragma unroll
                 for (int f = 0; f < FR; ++f) {
-                    kat[f] = rows_at(step, f, klim[f]);
+                    if (!WIN) kat[f] = rows_at(step, f, klim[f]);
 #pragma unroll
                     for (int r = 0; r < 2; ++r)
 #pragma unroll
@@ -447,9 +468,19 @@ __global__ void __launch_bounds__(TOKEN_THREADS, E8 ? (NT == 1 ? E8_BLOCKS : 2) 
                     }
                 }
             } else {
+                if (WIN) vall = kall;
 #pragma unroll
                 for (int f = 0; f < FR; ++f) {
                     vat[f] = kat[f], vlim[f] = klim[f];
+                    if (WIN && vall) {
+                        const uint8_t *at = (const uint8_t *)((const T *)kv.v_pages + kat[f] + (2 * col * DP + 8 * row));
+                        vr[f][0][0] = get16<0>(at), vr[f][1][0] = get16<2 * DP>(at), vr[f][2][0] = get16<16 * DP>(at), vr[f][3][0] = get16<18 * DP>(at);
+                        if constexpr (DP == 128) {
+                            vr[f][0][E8 ? 0 : VC - 1] = get16<128>(at), vr[f][1][E8 ? 0 : VC - 1] = get16<2 * DP + 128>(at);
+                            vr[f][2][E8 ? 0 : VC - 1] = get16<16 * DP + 128>(at), vr[f][3][E8 ? 0 : VC - 1] = get16<18 * DP + 128>(at);
+                        }
+                        continue;
+                    }
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const int key = 2 * col + (r & 1) + 8 * (r >> 1);
@@ -519,7 +550,7 @@ __global__ void __launch_bounds__(TOKEN_THREADS, E8 ? (NT == 1 ? E8_BLOCKS : 2) 
                 for (int f = 0; f < FR; ++f)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        if (!E8) x[f][t][i] = seen(row + 8 * (i >> 1), vlim[f]) ? x[f][t][i] * c : -INFINITY;
+                        if (!E8) x[f][t][i] = (WIN && vall) || seen(row + 8 * (i >> 1), vlim[f]) ? x[f][t][i] * c : -INFINITY;
                         top[t][i & 1] = fmaxf(top[t][i & 1], x[f][t][i]);
                     }
                 more = more || top[t][0] - m[t][0] > SLACK || top[t][1] - m[t][1] > SLACK;
