@@ -35,7 +35,9 @@ bool cache_ok(const opattr_cache *k) {
     const opattr_cache8 *e8 = cache8(k);
     const int rows = e8 ? e8->rows : k->dtype;
     if (rows != OPATTR_BF16 && rows != OPATTR_F16) return false;
-    if (e8 && (k->head_dim % 16 || !e8->k_scales || !e8->v_scales)) return false;
+    if (e8 && (k->head_dim % 16 || !e8->k_scales || !e8->v_scales ||
+               ((reinterpret_cast<uintptr_t>(e8->k_scales) | reinterpret_cast<uintptr_t>(e8->v_scales)) & 3)))
+        return false;
     if (k->page_size < 16 || k->page_size > 1024 || (k->page_size & (k->page_size - 1))) return false;
     if (k->kv_heads < 1 || k->head_dim < 8 || k->head_dim > 128 || k->head_dim % 8) return false;
     if (k->n_seqs < 1 || k->pages_per_seq < 1 || k->n_pages < 1 || k->n_pages > INT32_MAX) return false;

@@ -165,7 +165,7 @@ struct Work<true, CUT> {
         const int ahead = it.ahead;
         const int first = edge(it.t0 + ahead, p.window), few = min(p.sinks, first);
         sunk = (int)(((unsigned)few + SIXTEEN - 1) / SIXTEEN * SIXTEEN);
-        if (sunk >= first) sunk = 0, gap = 0;            // (nothing is left out)
+        if ((unsigned)sunk >= (unsigned)first) sunk = 0, gap = 0;   // (nothing is left out)
         else gap = first - sunk;
         whole = (gap ? few : p.sinks) / KEYS;
         from = CUT ? it.from : 0;
@@ -348,6 +348,7 @@ k_prompt(const __grid_constant__ PromptArgs p, const __grid_constant__ Maps<WIN>
                                 if (__all_sync(0xffffffffu, some == 0xffffffffu)) continue;
 #pragma unroll
                                 for (int i = 0; i < 32; ++i) x[q + i] = some >> i & 1 ? x[q + i] : 0xff800000u;
+
                             } else {
                                 if (__all_sync(0xffffffffu, left >= q + 32)) continue;
 #pragma unroll

@@ -353,7 +353,7 @@ __global__ void __launch_bounds__(TOKEN_THREADS, E8 ? (NT == 1 ? E8_BLOCKS : 2) 
         // where the rows of a step's keys are; none past the run's end or of a page that is none
         auto rows_at = [&](int step, int f, int &lim) -> long long {
             const int key = key_at(step, f), page = page_of(step, f);
-            lim = last - key;
+            lim = (int)((unsigned)last - (unsigned)key);
             if (WIN) lim = lim > 0 && (lim - near < 16 || lim + far > 0) ? lim : 0;
             if (lim > 0 && (page < 0 || page >= kv.n_pages)) {
                 atomicOr(err, SERVE_INVALID);
