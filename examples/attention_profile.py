@@ -5,12 +5,15 @@ Context.attention and into a paged cache, then every chat grows token by token
 (cache_append, cache_attention), one is forked into two continuations, some end
 (cache_trim) and the cache is compacted.  Every launch is timed, and what is known of
 its traffic stands in for the Nsight Compute rows; the join attributes both to the
-calls, rolls them up by operator and writes profile.json.
+calls, rolls them up by operator and writes profile.json.  With --window every token
+sees the last W ones and a few first ones (sinks), with --8bit the cache holds keys and
+values in 8 bits.
 
-    python examples/attention_profile.py [profile.json]
+    python examples/attention_profile.py [profile.json] [--window W] [--sinks S] [--8bit]
 """
 from __future__ import annotations
 
+import argparse
 import os
 import sys
 import time
@@ -67,23 +70,28 @@ class Recorder:
                                up(np.stack(self.rows), np.float32))
 
 
-def serve(rec: Recorder, prompts=(128, 70, 200, 33), steps=8, seed=0):
+def serve(rec: Recorder, prompts=(128, 70, 200, 33), steps=8, seed=0, window=None, sinks=0, eight_bits=False):
     """The serving loop.  Returns the cache and the last step's queries and results."""
     ctx = rec.ctx
+    # bytes of a token's keys, or values, in the cache, and names of the kernels that move them
+    held = HEADS * DIM + HEADS * 4 / opa.SCALE_TOKENS if eight_bits else ROW
+    appends, reads = ("append_rows8", "token8") if eight_bits else ("append_rows", "token")
+    view = dict(window=window, sinks=sinks)
+    near = lambda n: min(n, window + sinks) if window else n  # noqa: E731  (of n tokens, those that the last one sees)
     dev = f"cuda:{ctx.device}"
     gen = torch.Generator(device=dev)
     gen.manual_seed(seed)
     new = lambda n: [torch.randn((n, HEADS, DIM), generator=gen, device=dev).bfloat16() for _ in range(3)]  # noqa: E731
     i32 = lambda x: torch.tensor(list(x), dtype=torch.int32, device=dev)  # noqa: E731
     n_seqs, per_seq = len(prompts) + 2, -(-(max(prompts) + steps + 8) // PAGE)
-    cache = ctx.cache(n_seqs * per_seq, PAGE, HEADS, DIM, n_seqs, per_seq)
+    cache = ctx.cache(n_seqs * per_seq, PAGE, HEADS, DIM, n_seqs, per_seq, torch.float8_e4m3fn if eight_bits else None)
     lengths = list(prompts) + [0, 0]
     # prompts
     tokens = sum(prompts)
     offsets = i32(np.concatenate([[0], np.cumsum(prompts)]))
     q, k, v = new(tokens)
-    rec.call(0, "prompt", 3 * ROW * tokens, ROW * tokens, lambda: ctx.attention(q, k, v, offsets))
-    rec.call(1, "append_rows", 2 * ROW * tokens, 2 * ROW * tokens,
+    rec.call(0, "prompt", 3 * ROW * tokens, ROW * tokens, lambda: ctx.attention(q, k, v, offsets, **view))
+    rec.call(1, appends, 2 * ROW * tokens, 2 * held * tokens,
              lambda: ctx.cache_append(cache, i32(range(len(prompts))), offsets, k, v))
     live = list(range(len(prompts)))
     q = out = None
@@ -93,11 +101,11 @@ def serve(rec: Recorder, prompts=(128, 70, 200, 33), steps=8, seed=0):
         n = len(live)
         seqs = i32(live)
         q, k, v = new(n)
-        rec.call(1, "append_rows", 2 * ROW * n, 2 * ROW * n, lambda: ctx.cache_append(cache, seqs, i32(range(n + 1)), k, v))
+        rec.call(1, appends, 2 * ROW * n, 2 * held * n, lambda: ctx.cache_append(cache, seqs, i32(range(n + 1)), k, v))
         for s in live:
             lengths[s] += 1
-        seen = sum(lengths[s] for s in live)
-        out = rec.call(2, "token", 2 * ROW * seen + ROW * n, ROW * n, lambda: ctx.cache_attention(cache, seqs, q)[1])
+        seen = sum(near(lengths[s]) for s in live)
+        out = rec.call(2, reads, 2 * held * seen + ROW * n, ROW * n, lambda: ctx.cache_attention(cache, seqs, q, **view)[1])
 
     for _ in range(steps):
         step()
@@ -113,7 +121,7 @@ def serve(rec: Recorder, prompts=(128, 70, 200, 33), steps=8, seed=0):
     rec.call(4, "trim_plan", 0, 0, lambda: ctx.cache_trim(cache, i32([1, n_seqs - 2])))
     used = cache.refs > 0
     moved = int(used[int(used.sum()):].sum())
-    rec.call(5, "compact_move", 2 * ROW * PAGE * moved, 2 * ROW * PAGE * moved, lambda: ctx.cache_compact(cache))
+    rec.call(5, "compact_move", 2 * held * PAGE * moved, 2 * held * PAGE * moved, lambda: ctx.cache_compact(cache))
     step()
     return cache, live, q, out
 
@@ -137,11 +145,11 @@ def profile(rec: Recorder, path):
     return host(rolled), matched, totals
 
 
-def main(path="profile.json"):
+def main(path="profile.json", **how):
     with opa.Context(0) as ctx:
         rec = Recorder(ctx)
-        serve(Recorder(ctx))                             # code is loaded and scratch made once, untimed
-        serve(rec)
+        serve(Recorder(ctx), **how)                      # code is loaded and scratch made once, untimed
+        serve(rec, **how)
         rolled, matched, totals = profile(rec, path)
     print(f"{'operator':24s} {'launches':>8s} {'us':>9s} {'MB read':>9s} {'MB written':>10s} {'GB/s':>7s}")
     for i, name in enumerate(OPERATORS):
@@ -154,4 +162,10 @@ def main(path="profile.json"):
 
 
 if __name__ == "__main__":
-    main(*sys.argv[1:2])
+    parser = argparse.ArgumentParser(description="a small serving loop, profiled")
+    parser.add_argument("path", nargs="?", default="profile.json")
+    parser.add_argument("--window", type=int)
+    parser.add_argument("--sinks", type=int, default=0)
+    parser.add_argument("--8bit", dest="eight_bits", action="store_true")
+    args = vars(parser.parse_args())
+    main(args.pop("path"), **args)

@@ -158,8 +158,10 @@ def stands_for(cache, s):
     at = cache.table[s, :-(-n // page)].long()
     rows = []
     for pages, scales in ((cache.k_pages, cache.k_scales), (cache.v_pages, cache.v_scales)):
-        x = pages.view(torch.uint8)[at].view(torch.float8_e4m3fn).to(torch.float32).double()
-        if scales is not None:
+        if scales is None:
+            x = pages[at].double()
+        else:
+            x = pages.view(torch.uint8)[at].view(torch.float8_e4m3fn).to(torch.float32).double()
             x = x * scales[at].double().repeat_interleave(BLOCK, 2)[..., None]
         rows.append(x.transpose(1, 2).reshape(-1, x.shape[1], x.shape[3])[:n])
     return rows
