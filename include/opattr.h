@@ -512,8 +512,8 @@ opattr_status opattr_match_noalloc(const opattr_kernels *kernels, const opattr_n
  *
  * These calls order their work on the context's stream and do not wait for it.
  * They can be captured into a CUDA graph once a first call of the same or a
- * larger size has made the scratch (OPATTR_E_OOM where it is missing, and the
- * capture goes on).  The graph may be replayed until the
+ * larger size (and of the same window and kind of cache) has made the scratch
+ * (OPATTR_E_OOM where it is missing, and the capture goes on).  The graph may be replayed until the
  * context is destroyed, whatever calls come between (scratch that a graph
  * refers to is kept when a larger call outgrows it); as the calls themselves,
  * replays use the context's scratch, and are ordered with one another and with
@@ -651,6 +651,8 @@ opattr_status opattr_cache_attention_window(opattr_ctx *ctx, const opattr_cache 
  * others as well is copied first (its filled part), and pages are taken from
  * the lowest free one on.  Too few free pages: OPATTR_E_PAGES from
  * opattr_check, and nothing is changed.
+ * Pages of 8 bits: the rows are rounded as opattr_cache8 says; what a copied page had is rounded
+ * anew in the copy alone.
  * Errors: as opattr_attention. */
 opattr_status opattr_cache_append(opattr_ctx *ctx, const opattr_cache *cache, const int32_t *seqs, int32_t n,
                                   const int32_t *offsets, int64_t tokens, const opattr_rows *k, const opattr_rows *v);

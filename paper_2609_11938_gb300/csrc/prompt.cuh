@@ -28,6 +28,18 @@
 // unit, and the chain from scores through tensor memory to weights sets the pace.  Short prompts
 // wait for it: 8 x 512 tokens, 8 heads of 64, all seen, 17,000 cycles, 4,300 of them before
 // the first product, 11,700 for four tiles one after another.
+//
+// Through a window (WIN): query i sees j <= i + Lk - Lq that is among the last `window` of these, or below
+// `sinks`.  An item's tiles begin where the window of its first row does, whatever key that is, and the sinks
+// (in whole sixteens of rows) share the first one: with tiles at multiples of 128 and the sinks in one of their own,
+// 31 sequences of 1 .. 3,300, 16 heads of 128 on 4, window 512, took 123 us, so 108; with what a mask hides in
+// a tile as a word of bits for each 32 keys in the place of three comparisons a key, 96.  14,001 tokens, 32 heads on 8,
+// window 4,096, 4 sinks: 534 us in short bursts, 1,500 TFLOP/s.  Short items keep less of it: those 31 sequences 94 us, 600; of
+// the 26,000 cycles that an item's four tiles take a mean block has 10,000 in the steady pace of long ones, 2,300 more for
+// masks (2,900 cycles a masked tile, 1,500 another), 3,500 to write results, 2,300 until its first scores, 2,500 for its
+// queries, which cannot be fetched before the scores of the item before it are done.
+// Tried: the queries asked for while the ring is full (94 us: 97); masks that pass over 32s that nobody in the warp sees
+// (registers run out: 96, 177).
 #pragma once
 #include <math.h>
 

@@ -1,5 +1,5 @@
-// token.cu -- attention of one new token of each sequence over the paged cache
-// (opattr_cache_attention).
+// token.cuh -- attention of one new token of each sequence over the paged cache
+// (opattr_cache_attention, opattr_cache_attention_window).
 //
 // The cache is read once and there is little to compute on it, so what counts is
 // that every SM has enough loads under way until the last one is done.  All
@@ -30,6 +30,21 @@
 // beginning and the end of the one launch, about 7 us, show; one of 700, 12 heads of 64:
 // 7.7 us of the host's 12.  48 sequences that share the pages of 8 read them 48 times, from the
 // second level cache: 30 us.
+//
+// Pages of 8 bits (E8): half the bytes, so that what is done for each of them counts.  Codes become halves, exactly,
+// on the way into the products (a query of bfloat16 is brought into half's range by a power of
+// two); the scale of 16 keys multiplies their scores, and the sums of their values' products: no weight carries a
+// scale, so blocks may be as far apart as they like.  Where a warp's keys are whole sixteens of a full width, which
+// is checked once for a lane's 32 coming steps, its loads have no conditions and their offsets are in the
+// instruction (2 sequences of 500,000 tokens, 40 heads of 128 on 8: 374 us with the conditions, 304 without).  Where
+// pairs are many each warp has some of its own, and nobody waits for a block.
+// Through a window (WIN) the sixteens of keys that are not seen are left out of a sequence's steps; the first
+// ones have the sinks, the others begin where the window does.
+//   8 bits, bytes as above: 2 of 500,000, 40 heads of 128 on 8: 304 us, 6.8 TB/s; 64 of 1 .. 16,001, 32 heads on 8: 44 us,
+//   4.7, of which about 13 are the launch, first loads and joins; 200 of 4,096, 16 heads of 64: 279 us, 6.0.
+//   A window of 4,096 and 4 sinks, 16 bits: 96 of 1 .. 20,001, 32 heads of 128 on 8: 83 us, 6.0.
+// Tried for 8 bits: a ring of copies in shared memory, three to six steps ahead, in the place of loads into registers: 350 us
+// for the 304 at every depth, and 77 for 79 at 200 sequences of 64 wide heads.
 #pragma once
 #include <math.h>
 
@@ -52,18 +67,17 @@ constexpr unsigned PARTLY = 1u << 30;
 constexpr int WHOLE_STEPS = 3;
 constexpr float JOIN_STEPS = 12.f;
 
-#ifndef E8_BLOCKS
-#define E8_BLOCKS (DP == 64 ? 4 : 3)
-#endif
-#ifndef E8_TEAMS
-#define E8_TEAMS 1
-#endif
-#ifndef E8_F64
-#define E8_F64 2
-#endif
-#ifndef E8_F128
-#define E8_F128 2
-#endif
+// Pages of 8 bits: sixteens of keys that a warp takes at a time, and blocks that an SM holds (by registers).
+// Of 64 wide heads, 200 sequences of 1,028 tokens, 16 heads: two sixteens in four blocks 79 us, one in five 84, four in
+// three 94; of 128 wide, 2 sequences of 500,000, 40 heads on 8: two in three blocks 307 us, one in four 318, two in four (which do
+// not fit) 454.  Each warp has pairs of its own once there are so many for an SM (TW below), us with
+// all of a block's warps at one and by themselves: 16 heads of 64, 608 pairs of 1,028 tokens 22 and 25, 1,216 39 and 40, 1,824
+// 54 and 53, 3,648 102 and 91; 32 heads of 128 on 8, 1,216 pairs 66 and 68, 1,824 89 and 85, 3,648 173 and 163.
+template <int DP, int NT>
+struct Eight {
+    static constexpr int BLOCKS = NT > 1 ? 2 : DP == 64 ? 4 : 3, PAIRS = DP == 64 ? 8 : 12;
+};
+
 struct TokenArgs {
     opattr_cache kv;
     const int32_t *seqs;
@@ -180,7 +194,7 @@ __device__ __forceinline__ void fma_pair(float &a, float &b, float x, float y, f
 // warp takes at a time; E8: pages of 8 bits; WIN: through a window.  TW: warps that share a pair's
 // keys: all of a block, or each by itself.
 template <typename T, int DP, int NT, int FR, bool E8, bool WIN, int TW>
-__global__ void __launch_bounds__(TOKEN_THREADS, E8 ? (NT == 1 ? E8_BLOCKS : 2) : NT == 1 ? 3 : 2) k_token(const __grid_constant__ TokenArgs p, unsigned *err) {
+__global__ void __launch_bounds__(TOKEN_THREADS, E8 ? Eight<DP, NT>::BLOCKS : NT == 1 ? 3 : 2) k_token(const __grid_constant__ TokenArgs p, unsigned *err) {
     using P = std::conditional_t<E8, __half, T>;          // what the products take
     constexpr bool BF = std::is_same<P, __nv_bfloat16>::value;
     // as in prompt.cu: weights up to 2^(OFFSET + SLACK), rescaled when a maximum outgrows SLACK
@@ -721,7 +735,7 @@ static opattr_status run_teams(Ctx &c, Serve &s, TokenArgs &p) {
     const int64_t most = (int64_t)p.n * p.kv.kv_heads * p.blocks_of_heads *
                          (((int64_t)p.kv.pages_per_seq * p.kv.page_size + 16 * FR * TW - 1) / (16 * FR * TW));
     constexpr int TEAMS = TOKEN_WARPS / TW;
-    const int grid = (int)std::min<int64_t>((E8 ? (NT == 1 ? E8_BLOCKS : 2) : NT == 1 ? 3 : 2) * (int64_t)sm_count(c), std::min<int64_t>((most + TEAMS - 1) / TEAMS, TICKETS / TEAMS));
+    const int grid = (int)std::min<int64_t>((E8 ? Eight<DP, NT>::BLOCKS : NT == 1 ? 3 : 2) * (int64_t)sm_count(c), std::min<int64_t>((most + TEAMS - 1) / TEAMS, TICKETS / TEAMS));
     opattr_status st = serve_ready(c, s);
     if (st) return st;
     const int64_t part = (int64_t)8 * NT * (DP + 2);
@@ -735,13 +749,13 @@ static opattr_status run_teams(Ctx &c, Serve &s, TokenArgs &p) {
 template <typename T, int DP, int NT, int FR, bool E8, bool WIN>
 static opattr_status run_token(Ctx &c, Serve &s, TokenArgs &p) {
     if constexpr (E8) {
-        if ((int64_t)p.n * p.kv.kv_heads * p.blocks_of_heads >= E8_TEAMS * (int64_t)sm_count(c) * TOKEN_WARPS * (NT == 1 ? E8_BLOCKS : 2)) return run_teams<T, DP, NT, FR, E8, WIN, 1>(c, s, p);
+        if ((int64_t)p.n * p.kv.kv_heads * p.blocks_of_heads >= Eight<DP, NT>::PAIRS * (int64_t)sm_count(c)) return run_teams<T, DP, NT, FR, E8, WIN, 1>(c, s, p);
     }
     return run_teams<T, DP, NT, FR, E8, WIN, TOKEN_WARPS>(c, s, p);
 }
 template <typename T, bool E8, bool WIN>
 static opattr_status token_of(Ctx &c, Serve &s, TokenArgs &p) {
-    constexpr int F64 = E8 ? E8_F64 : 2, F128 = E8 ? E8_F128 : 1;
+    constexpr int F64 = 2, F128 = E8 ? 2 : 1;
     if (p.kv.head_dim <= 64) return p.group <= 8 ? run_token<T, 64, 1, F64, E8, WIN>(c, s, p) : run_token<T, 64, 2, F64, E8, WIN>(c, s, p);
     return p.group <= 8 ? run_token<T, 128, 1, F128, E8, WIN>(c, s, p) : run_token<T, 128, 2, F128, E8, WIN>(c, s, p);
 }
