@@ -7,7 +7,7 @@ namespace opattr {
 bool cache_ok(const opattr_cache *k);
 
 opattr_status token_plain(Ctx &c, Serve &s, TokenArgs &p, int dtype) {
-    return dtype == OPATTR_BF16 ? token_of<__nv_bfloat16, false, false>(c, s, p) : token_of<__half, false, false>(c, s, p);
+    return token_of<false, false, false>(c, s, p, dtype);
 }
 
 opattr_status do_cache_attention(Ctx &c, Serve &s, const opattr_cache *kv, const int32_t *seqs, int32_t n,
@@ -37,6 +37,7 @@ opattr_status do_cache_attention(Ctx &c, Serve &s, const opattr_cache *kv, const
     p.scale = scale;
     while ((1 << p.shift) < kv->page_size) ++p.shift;
     const int dtype = e8 ? e8->rows : kv->dtype;
+    if (e8 && kv->head_dim != 64 && kv->head_dim != 128) return window ? token8_window_odd(c, s, p, dtype) : token8_plain_odd(c, s, p, dtype);
     if (e8) return window ? token8_window(c, s, p, dtype) : token8_plain(c, s, p, dtype);
     return window ? token_window(c, s, p, dtype) : token_plain(c, s, p, dtype);
 }

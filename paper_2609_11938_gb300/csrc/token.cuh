@@ -34,9 +34,10 @@
 // Pages of 8 bits (E8): half the bytes, so that what is done for each of them counts.  Codes become halves, exactly,
 // on the way into the products (a query of bfloat16 is brought into half's range by a power of
 // two); the scale of 16 keys multiplies their scores, and the sums of their values' products: no weight carries a
-// scale, so blocks may be as far apart as they like.  Where a warp's keys are whole sixteens of a full width, which
-// is checked once for a lane's 32 coming steps, its loads have no conditions and their offsets are in the
-// instruction (2 sequences of 500,000 tokens, 40 heads of 128 on 8: 374 us with the conditions, 304 without).  Where
+// scale, so blocks may be as far apart as they like.  Where a warp's keys are whole sixteens, which
+// is checked once for a lane's 32 coming steps, its loads have no conditions; those of heads 64 or 128 wide have their
+// offsets in the instruction (2 sequences of 500,000 tokens, 40 heads of 128 on 8: 374 us with the conditions, 304
+// without), those of other widths add them, in kernels of their own (16 of 30,000, 32 heads of 96 on 8: 160, 145).  Where
 // pairs are many each warp has some of its own, and nobody waits for a block.
 // Through a window (WIN) the sixteens of keys that are not seen are left out of a sequence's steps; the first
 // ones have the sinks, the others begin where the window does.
@@ -192,8 +193,8 @@ __device__ __forceinline__ void fma_pair(float &a, float &b, float x, float y, f
 
 // DP: the padded head width; NT: eights of queries; FR: sixteens of keys that a
 // warp takes at a time; E8: pages of 8 bits; WIN: through a window.  TW: warps that share a pair's
-// keys: all of a block, or each by itself.
-template <typename T, int DP, int NT, int FR, bool E8, bool WIN, int TW>
+// keys: all of a block, or each by itself.  FULL: heads are as wide as they are padded to.
+template <typename T, int DP, int NT, int FR, bool E8, bool WIN, int TW, bool FULL>
 __global__ void __launch_bounds__(TOKEN_THREADS, E8 ? Eight<DP, NT>::BLOCKS : NT == 1 ? 3 : 2) k_token(const __grid_constant__ TokenArgs p, unsigned *err) {
     using P = std::conditional_t<E8, __half, T>;          // what the products take
     constexpr bool BF = std::is_same<P, __nv_bfloat16>::value;
@@ -391,17 +392,29 @@ __global__ void __launch_bounds__(TOKEN_THREADS, E8 ? Eight<DP, NT>::BLOCKS : NT
                     any &= lot[f];
                     all |= lot[f];
                 }
-                kall = kv.head_dim == DP && (unsigned)all < PARTLY;
+                kall = (!FULL || kv.head_dim == DP) && (unsigned)all < PARTLY;   // (left out, registers run out)
                 knone = any == -1;
                 if (kall) {
 #pragma unroll
                     for (int f = 0; f < FR; ++f) {
-                        const uint8_t *at = k_lane + (uint64_t)(unsigned)lot[f] * (16 * DP);
-                        kr[f][0][0] = get16<0>(at);
-                        kr[f][1][0] = get16<8 * DP>(at);
-                        if constexpr (DP == 128) {
-                            kr[f][0][KC - 1] = get16<64>(at);
-                            kr[f][1][KC - 1] = get16<8 * DP + 64>(at);
+                        if (FULL) {
+                            const uint8_t *at = k_lane + (uint64_t)(unsigned)lot[f] * (16 * DP);
+                            kr[f][0][0] = get16<0>(at);
+                            kr[f][1][0] = get16<8 * DP>(at);
+                            if constexpr (DP == 128) {
+                                kr[f][0][KC - 1] = get16<64>(at);
+                                kr[f][1][KC - 1] = get16<8 * DP + 64>(at);
+                            }
+                        } else {
+                            // (in the place of elements that a row does not have its first ones: the queries have
+                            // zeros there, and a code that is NaN makes the row's score NaN in its own place as well)
+                            const uint8_t *at = (const uint8_t *)kv.k_pages + (uint64_t)(unsigned)lot[f] * (16 * kv.head_dim) + row * kv.head_dim;
+#pragma unroll
+                            for (int i = 0; i < KC; ++i) {
+                                const int d = 64 * i + 16 * col < kv.head_dim ? 64 * i + 16 * col : 0;
+                                kr[f][0][i] = get16<0>(at + d);
+                                kr[f][1][i] = get16<0>(at + d + 8 * kv.head_dim);
+                            }
                         }
                         ks[f] = p.k_scales[(unsigned)lot[f]];
                         vs_next[f] = p.v_scales[(unsigned)lot[f]];
@@ -425,12 +438,22 @@ __global__ void __launch_bounds__(TOKEN_THREADS, E8 ? Eight<DP, NT>::BLOCKS : NT
                 }
             } else {
                 if constexpr (WIN) {
-                    kall = kv.head_dim == DP;
+                    kall = true;
 #pragma unroll
                     for (int f = 0; f < FR; ++f) {
                         kat[f] = rows_at(step, f, klim[f]);
                         kall = kall && klim[f] >= 16 && (klim[f] <= near || klim[f] + far >= 16);
                     }
+                }
+                if (WIN && kall && !FULL) {
+#pragma unroll
+                    for (int f = 0; f < FR; ++f)
+#pragma unroll
+                        for (int r = 0; r < 2; ++r)
+#pragma unroll
+                            for (int i = 0; i < KC; ++i)
+                                kr[f][r][i] = load16((const T *)kv.k_pages + kat[f] + (row + 8 * r) * kv.head_dim + 32 * i + 8 * col, 32 * i + 8 * col < kv.head_dim);
+                    return;
                 }
                 if (WIN && kall) {
 #pragma unroll
@@ -463,12 +486,24 @@ __global__ void __launch_bounds__(TOKEN_THREADS, E8 ? Eight<DP, NT>::BLOCKS : NT
 #pragma unroll
                 for (int f = 0; f < FR; ++f) {
                     vlim[f] = klim[f], vs[f] = vs_next[f];
-                    if (vall) {
+                    if (vall && FULL) {
                         const uint8_t *at = v_lane + (uint64_t)(unsigned)lot[f] * (16 * DP);
                         if constexpr (DP == 64) {
                             vr[f][0][0] = get8<0>(at), vr[f][1][0] = get8<DP>(at), vr[f][2][0] = get8<8 * DP>(at), vr[f][3][0] = get8<9 * DP>(at);
                         } else {
                             vr[f][0][0] = get16<0>(at), vr[f][1][0] = get16<DP>(at), vr[f][2][0] = get16<8 * DP>(at), vr[f][3][0] = get16<9 * DP>(at);
+                        }
+                        continue;
+                    }
+                    if (vall) {
+                        // (results past the width are nobody's)
+                        const int d = DP / 8 * row < kv.head_dim ? DP / 8 * row : 0;
+                        const uint8_t *at = (const uint8_t *)kv.v_pages + (uint64_t)(unsigned)lot[f] * (16 * kv.head_dim) + 2 * col * kv.head_dim + d;
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const uint8_t *x = at + ((r & 1) + 8 * (r >> 1)) * kv.head_dim;
+                            if constexpr (DP == 64) vr[f][r][0] = get8<0>(x);
+                            else vr[f][r][0] = get16<0>(x);
                         }
                         continue;
                     }
@@ -486,7 +521,7 @@ __global__ void __launch_bounds__(TOKEN_THREADS, E8 ? Eight<DP, NT>::BLOCKS : NT
 #pragma unroll
                 for (int f = 0; f < FR; ++f) {
                     vat[f] = kat[f], vlim[f] = klim[f];
-                    if (WIN && vall) {
+                    if (WIN && vall && FULL) {
                         const uint8_t *at = (const uint8_t *)((const T *)kv.v_pages + kat[f] + (2 * col * DP + 8 * row));
                         vr[f][0][0] = get16<0>(at), vr[f][1][0] = get16<2 * DP>(at), vr[f][2][0] = get16<16 * DP>(at), vr[f][3][0] = get16<18 * DP>(at);
                         if constexpr (DP == 128) {
@@ -498,7 +533,7 @@ __global__ void __launch_bounds__(TOKEN_THREADS, E8 ? Eight<DP, NT>::BLOCKS : NT
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const int key = 2 * col + (r & 1) + 8 * (r >> 1);
-                        const bool on = seen(key, vlim[f]);
+                        const bool on = (WIN && vall) || seen(key, vlim[f]);
 #pragma unroll
                         for (int i = 0; i < VC; ++i) {
                             const int d = 64 * i + 8 * row;
@@ -730,7 +765,7 @@ __global__ void __launch_bounds__(TOKEN_THREADS, E8 ? Eight<DP, NT>::BLOCKS : NT
     }
 }
 
-template <typename T, int DP, int NT, int FR, bool E8, bool WIN, int TW>
+template <typename T, int DP, int NT, int FR, bool E8, bool WIN, int TW, bool FULL>
 static opattr_status run_teams(Ctx &c, Serve &s, TokenArgs &p) {
     const int64_t most = (int64_t)p.n * p.kv.kv_heads * p.blocks_of_heads *
                          (((int64_t)p.kv.pages_per_seq * p.kv.page_size + 16 * FR * TW - 1) / (16 * FR * TW));
@@ -743,21 +778,25 @@ static opattr_status run_teams(Ctx &c, Serve &s, TokenArgs &p) {
     Arena a(c);
     p.parts = a.take<float>(2 * (int64_t)grid * TEAMS * part);
     p.tickets = s.tickets;
-    launch(c, E8 ? "token8" : "token", k_token<T, DP, NT, FR, E8, WIN, TW>, dim3(grid), dim3(TOKEN_THREADS), 0, p, s.err);
+    launch(c, E8 ? "token8" : "token", k_token<T, DP, NT, FR, E8, WIN, TW, FULL>, dim3(grid), dim3(TOKEN_THREADS), 0, p, s.err);
     return cuda_status(c, c.last_error);
 }
-template <typename T, int DP, int NT, int FR, bool E8, bool WIN>
+template <typename T, int DP, int NT, int FR, bool E8, bool WIN, bool FULL>
 static opattr_status run_token(Ctx &c, Serve &s, TokenArgs &p) {
     if constexpr (E8) {
-        if ((int64_t)p.n * p.kv.kv_heads * p.blocks_of_heads >= Eight<DP, NT>::PAIRS * (int64_t)sm_count(c)) return run_teams<T, DP, NT, FR, E8, WIN, 1>(c, s, p);
+        if ((int64_t)p.n * p.kv.kv_heads * p.blocks_of_heads >= Eight<DP, NT>::PAIRS * (int64_t)sm_count(c)) return run_teams<T, DP, NT, FR, E8, WIN, 1, FULL>(c, s, p);
     }
-    return run_teams<T, DP, NT, FR, E8, WIN, TOKEN_WARPS>(c, s, p);
+    return run_teams<T, DP, NT, FR, E8, WIN, TOKEN_WARPS, FULL>(c, s, p);
 }
-template <typename T, bool E8, bool WIN>
+template <typename T, bool E8, bool WIN, bool FULL>
 static opattr_status token_of(Ctx &c, Serve &s, TokenArgs &p) {
     constexpr int F64 = 2, F128 = E8 ? 2 : 1;
-    if (p.kv.head_dim <= 64) return p.group <= 8 ? run_token<T, 64, 1, F64, E8, WIN>(c, s, p) : run_token<T, 64, 2, F64, E8, WIN>(c, s, p);
-    return p.group <= 8 ? run_token<T, 128, 1, F128, E8, WIN>(c, s, p) : run_token<T, 128, 2, F128, E8, WIN>(c, s, p);
+    if (p.kv.head_dim <= 64) return p.group <= 8 ? run_token<T, 64, 1, F64, E8, WIN, FULL>(c, s, p) : run_token<T, 64, 2, F64, E8, WIN, FULL>(c, s, p);
+    return p.group <= 8 ? run_token<T, 128, 1, F128, E8, WIN, FULL>(c, s, p) : run_token<T, 128, 2, F128, E8, WIN, FULL>(c, s, p);
+}
+template <bool E8, bool WIN, bool FULL>
+static opattr_status token_of(Ctx &c, Serve &s, TokenArgs &p, int dtype) {
+    return dtype == OPATTR_BF16 ? token_of<__nv_bfloat16, E8, WIN, FULL>(c, s, p) : token_of<__half, E8, WIN, FULL>(c, s, p);
 }
 
 // By the type of the queries; each in a file of its own, which compiles beside the others.
@@ -765,5 +804,8 @@ opattr_status token_plain(Ctx &c, Serve &s, TokenArgs &p, int dtype);
 opattr_status token_window(Ctx &c, Serve &s, TokenArgs &p, int dtype);
 opattr_status token8_plain(Ctx &c, Serve &s, TokenArgs &p, int dtype);
 opattr_status token8_window(Ctx &c, Serve &s, TokenArgs &p, int dtype);
+// and of widths other than 64 and 128
+opattr_status token8_plain_odd(Ctx &c, Serve &s, TokenArgs &p, int dtype);
+opattr_status token8_window_odd(Ctx &c, Serve &s, TokenArgs &p, int dtype);
 
 }  // namespace opattr

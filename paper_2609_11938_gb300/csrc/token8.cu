@@ -4,7 +4,7 @@
 namespace opattr {
 
 opattr_status token8_plain(Ctx &c, Serve &s, TokenArgs &p, int dtype) {
-    return dtype == OPATTR_BF16 ? token_of<__nv_bfloat16, true, false>(c, s, p) : token_of<__half, true, false>(c, s, p);
+    return token_of<true, false, true>(c, s, p, dtype);
 }
 
 }  // namespace opattr

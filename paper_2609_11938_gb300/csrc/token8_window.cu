@@ -4,7 +4,7 @@
 namespace opattr {
 
 opattr_status token8_window(Ctx &c, Serve &s, TokenArgs &p, int dtype) {
-    return dtype == OPATTR_BF16 ? token_of<__nv_bfloat16, true, true>(c, s, p) : token_of<__half, true, true>(c, s, p);
+    return token_of<true, true, true>(c, s, p, dtype);
 }
 
 }  // namespace opattr

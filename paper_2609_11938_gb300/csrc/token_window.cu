@@ -4,7 +4,7 @@
 namespace opattr {
 
 opattr_status token_window(Ctx &c, Serve &s, TokenArgs &p, int dtype) {
-    return dtype == OPATTR_BF16 ? token_of<__nv_bfloat16, false, true>(c, s, p) : token_of<__half, false, true>(c, s, p);
+    return p.kv.head_dim == 64 || p.kv.head_dim == 128 ? token_of<false, true, true>(c, s, p, dtype) : token_of<false, true, false>(c, s, p, dtype);
 }
 
 }  // namespace opattr
