@@ -19,7 +19,7 @@
 // Pages of 8 bits (opattr_cache8): 16 tokens of a head share a scale, so a warp takes these 16 rows at
 // once: their largest element, the scale, the codes, and what the scale's growth means for the codes before
 // them.  A block of threads looks up where 16 tokens go once for all heads.  58,650 tokens to 50 empty sequences, 8 heads
-// of 128: 63 us, 5.7 TB/s read and written (a lookup for every head: 113); one token to each of 200, 16 heads of 64: 10 us;
+// of 128: 59 us, 6.1 TB/s read and written (a lookup for every head: 113; three blocks of threads to an SM in the place of four: 63); one token to each of 200, 16 heads of 64: 10 us;
 // to 48 sequences that share pages of 8, 8 heads of 128: 12 us (their copies one after another: 25).
 #include <stdlib.h>
 #include <string.h>
@@ -416,7 +416,7 @@ __device__ __forceinline__ void append_block(const T *x, int64_t stride, int fir
 // tokens that a sequence's new rows share a scale with, where their page is copied, are put together from both
 // by whoever writes the rows; the copying blocks have the full sixteens.
 template <typename T, int DP>
-__global__ void __launch_bounds__(COPY_THREADS, DP == 64 ? 4 : 3)
+__global__ void __launch_bounds__(COPY_THREADS, 4)
 k_append_rows8(opattr_cache8 c8, const int32_t *seqs, int n, const int32_t *offsets, int tokens, opattr_rows k,
                opattr_rows v, AppendPlan p, unsigned row_blocks, int parts) {
     pdl_wait();
