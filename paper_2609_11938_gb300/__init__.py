@@ -490,11 +490,13 @@ def _rows(t, heads: int | None, dim: int, like, name, device):
         raise TypeError(f"{name}: expected {like}, got {t.dtype}")
     if t.get_device() != device:
         raise ValueError(f"{name}: must live on cuda:{device}")
-    st, sh, se = t.stride()
     n, h, _ = shape
     p = t.data_ptr()
     if n == 0 or h == 0:
         return 0, 0, 0
+    if not p & 15 and not dim & 7 and t.is_contiguous():
+        return p, h * dim, dim
+    st, sh, se = t.stride()
     if n == 1:
         st = h * dim
     if h == 1:
@@ -596,6 +598,7 @@ class KVCache:
         # (pages of 8 bits: one for rows of either type, so that calls do not change what others read)
         structs = [kind(*fields, r) for r in (0, 1)] if e8 else [kind(*fields)]
         self.struct, self.device, self.by_ref = structs[0], dv, ctypes.byref(structs[0])
+        self.sizes = g, dim, self.table.shape[0]
         self.for_rows = {torch.bfloat16: self.by_ref, torch.float16: ctypes.byref(structs[1])} if e8 else \
             {self.k_pages.dtype: self.by_ref}
 
@@ -848,6 +851,9 @@ class Context:
     def _i32(self, t, n: int | None, name):
         if t is None:
             return 0
+        if t.dtype is _torch().int32 and t.get_device() == self.device and t.dim() == 1 and t.is_contiguous() and \
+                (n is None or t.numel() == n):
+            return t.data_ptr()
         shape = t.shape
         if len(shape) != 1 or (n is not None and shape[0] != n):
             raise ValueError(f"{name}: expected [{n if n is not None else 'n'}], got {list(shape)}")
@@ -906,9 +912,10 @@ class Context:
         args = _PROMPT.pack(dtype, n_seqs, heads, kv_heads, dim, 1 if causal else 0, dim ** -0.5 if scale is None else scale,
                             0, tokens, k_tokens, *rq, *rk, *rv, *ro, p_qo, p_ko, p_lse)
         cur = self._enter()
+        lib = _lib or library()
         if window is not None:
-            return self._leave(cur, opattr_attention_window(self.handle, args, window, sinks), "opattr_attention_window"), out, lse
-        return self._leave(cur, opattr_attention(self.handle, args), "opattr_attention"), out, lse
+            return self._leave(cur, lib.opattr_attention_window(self.handle, args, window, sinks), "opattr_attention_window"), out, lse
+        return self._leave(cur, lib.opattr_attention(self.handle, args), "opattr_attention"), out, lse
 
     def _ends(self, tokens: int):
         """Offsets of one sequence, made on the device: a copy of host values would wait for it."""
@@ -956,15 +963,17 @@ class Context:
         torch = _torch()
         if window is not None or sinks:
             _window(window, sinks)
-        kv = self._cache(cache)
-        by_ref = cache._rows_of(q, "q")
-        dim, dt = kv.head_dim, q.dtype
+        if cache.device != self.device:
+            self._cache(cache)
+        kv_heads, dim, n_seqs = cache.sizes
+        dt = q.dtype
+        by_ref = cache.for_rows.get(dt) or cache._rows_of(q, "q")
         rq = _rows(q, None, dim, dt, "q", self.device)
         n, heads, _ = q.shape
-        if heads < 1 or heads % kv.kv_heads:
-            raise ValueError(f"heads: {heads} of q are no multiple of {kv.kv_heads} of the cache")
-        if seqs is None and n > kv.n_seqs:
-            raise ValueError(f"q: {n} rows for {kv.n_seqs} sequences")
+        if heads < 1 or heads % kv_heads:
+            raise ValueError(f"heads: {heads} of q are no multiple of {kv_heads} of the cache")
+        if seqs is None and n > n_seqs:
+            raise ValueError(f"q: {n} rows for {n_seqs} sequences")
         if q.requires_grad:
             _no_grad(q=q)
         out, ro = self._out(out, q, heads, dim, dt)
@@ -975,30 +984,33 @@ class Context:
         p_seqs = self._i32(seqs, n, "seqs")
         args = (self.handle, by_ref, p_seqs, n, heads, _ROWS.pack(*rq), _ROWS.pack(*ro), p_lse, dim ** -0.5 if scale is None else scale)
         cur = self._enter()
+        lib = _lib or library()
         if window is not None:
-            return self._leave(cur, opattr_cache_attention_window(*args, window, sinks), "opattr_cache_attention_window"), out, lse
-        return self._leave(cur, opattr_cache_attention(*args), "opattr_cache_attention"), out, lse
+            return self._leave(cur, lib.opattr_cache_attention_window(*args, window, sinks), "opattr_cache_attention_window"), out, lse
+        return self._leave(cur, lib.opattr_cache_attention(*args), "opattr_cache_attention"), out, lse
 
     def cache_append(self, cache: KVCache, seqs, offsets, k, v) -> int:
         """Rows offsets[i] .. offsets[i + 1] of k and v ([tokens, kv_heads, dim])
         to the end of sequence seqs[i], each sequence once (opattr_cache_append).
         Pages of 8 bits: the rows are rounded on their way in, for a scale of each
         SCALE_TOKENS tokens of a head, which may round their last codes anew."""
-        kv = self._cache(cache)
-        by_ref = cache._rows_of(k, "k")
+        if cache.device != self.device:
+            self._cache(cache)
+        kv_heads, dim, _ = cache.sizes
+        dt = k.dtype
+        by_ref = cache.for_rows.get(dt) or cache._rows_of(k, "k")
         if v.shape != k.shape:
             raise ValueError(f"v: expected {list(k.shape)}, got {list(v.shape)}")
         if k.requires_grad or v.requires_grad:
             _no_grad(k=k, v=v)
-        dt = k.dtype
-        rk = _rows(k, kv.kv_heads, kv.head_dim, dt, "k", self.device)
-        rv = _rows(v, kv.kv_heads, kv.head_dim, dt, "v", self.device)
+        rk = _rows(k, kv_heads, dim, dt, "k", self.device)
+        rv = _rows(v, kv_heads, dim, dt, "v", self.device)
         p_seqs = self._i32(seqs, None, "seqs")
         n = seqs.shape[0]
         p_off = self._i32(offsets, n + 1, "offsets")
         cur = self._enter()
-        st = opattr_cache_append(self.handle, by_ref, p_seqs, n, p_off, k.shape[0],
-                                 _ROWS.pack(*rk), _ROWS.pack(*rv))
+        st = (_lib or library()).opattr_cache_append(self.handle, by_ref, p_seqs, n, p_off, k.shape[0],
+                                                     _ROWS.pack(*rk), _ROWS.pack(*rv))
         return self._leave(cur, st, "opattr_cache_append")
 
     def cache_fork(self, cache: KVCache, src, dst) -> int:
