@@ -19,7 +19,7 @@
 // Pages of 8 bits (opattr_cache8): 16 tokens of a head share a scale, so a warp takes these 16 rows at
 // once: their largest element, the scale, the codes, and what the scale's growth means for the codes before
 // them.  A block of threads looks up where 16 tokens go once for all heads.  58,650 tokens to 50 empty sequences, 8 heads
-// of 128: 59 us, 6.1 TB/s read and written (a lookup for every head: 113; three blocks of threads to an SM in the place of four: 63); one token to each of 200, 16 heads of 64: 10 us;
+// of 128: 59 us, 6.1 TB/s read and written (a lookup for every head: 113; three blocks of threads to an SM in the place of four: 63); one token to each of 200, 16 heads of 64: 8 us;
 // to 48 sequences that share pages of 8, 8 heads of 128: 12 us (their copies one after another: 25).
 #include <stdlib.h>
 #include <string.h>
@@ -99,7 +99,7 @@ __device__ __forceinline__ bool length_bad(const opattr_cache &kv, int seq) {
 // ---------------------------------------------------------------- append
 // What the plan leaves for the launch that moves the rows.
 struct AppendPlan {
-    int32_t *go;        // [1] 1: the call holds
+    int32_t *go;        // [1] 1: the call holds; 2: and pages are copied
     int32_t *old;       // [n] lengths before
     int32_t *from, *to; // [n] a partly filled page that is copied first, and where to; -1 none
     int32_t *late;      // [n] a page that this sequence keeps and shortens for one that copies it; -1 none
@@ -152,7 +152,7 @@ k_append_plan(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offset
     if (any_bad(bad, SERVE_INVALID, err)) return;
     if (marks_bad(seqs, n, p.mark, err)) return;
     int total = 0;
-    bool any_late = false;
+    bool any_late = false, any_copied = false;
     for (int i0 = 0; i0 < n; i0 += blockDim.x) {
         const int i = i0 + threadIdx.x;
         int need = 0;
@@ -176,6 +176,7 @@ k_append_plan(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offset
             p.from[i] = from;
             p.late[i] = late;
             any_late = any_late || late >= 0;
+            any_copied = any_copied || from >= 0;
             need += from >= 0;
         }
         int sum;
@@ -225,6 +226,7 @@ k_append_plan(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offset
         }
         kv.length[seqs[i]] = p.old[i] + (offsets[i + 1] - offsets[i]);
     }
+    any_copied = __syncthreads_or(any_copied);
     if (__syncthreads_or(any_late)) {
         // the sequence that keeps such a page copies it for the others before it writes there
         for (int i = threadIdx.x; i < n; i += blockDim.x) {
@@ -237,7 +239,7 @@ k_append_plan(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offset
     }
     if (threadIdx.x == 0) {
         if (total > 0) *kv.low = p.fresh[total - 1] + 1;
-        *p.go = 1;
+        *p.go = any_copied ? 2 : 1;
     }
 }
 
@@ -253,6 +255,7 @@ k_append_rows(opattr_cache kv, const int32_t *seqs, int n, const int32_t *offset
     const int per = kv.head_dim / 8;                              // pieces of a head's row
     uint4 *kp = reinterpret_cast<uint4 *>(kv.k_pages), *vp = reinterpret_cast<uint4 *>(kv.v_pages);
     if (blockIdx.x >= row_blocks) {
+        if (*p.go == 1) return;
         // a sequence's head at a time, as many threads as its filled rows have pieces
         const int64_t all = (int64_t)n * kv.kv_heads, block = (int64_t)kv.page_size * per;
         for (int64_t x = blockIdx.x - row_blocks; x < all; x += gridDim.x - row_blocks) {
@@ -435,6 +438,7 @@ k_append_rows8(opattr_cache8 c8, const int32_t *seqs, int n, const int32_t *offs
                             lo - b * BLOCK, hi - lo, dim, pool + from * BLOCK * dim, scales + from, pool + at * BLOCK * dim, scales + at);
     };
     if (blockIdx.x >= row_blocks) {
+        if (*p.go == 1) return;
         const int64_t all = (int64_t)n * kv.kv_heads;
         for (int64_t x = blockIdx.x - row_blocks; x < all; x += gridDim.x - row_blocks) {
             const int i = (int)(x / kv.kv_heads), g = (int)(x % kv.kv_heads);
