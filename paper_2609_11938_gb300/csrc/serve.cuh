@@ -1,4 +1,4 @@
-// serve.cuh -- shared by the attention operators (prompt.cu, token.cu) and the
+// serve.cuh -- shared by the attention operators (prompt.cuh, token.cuh) and the
 // paged cache under them (pages.cu).
 #pragma once
 #include <cuda_bf16.h>

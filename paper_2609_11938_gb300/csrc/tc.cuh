@@ -1,4 +1,4 @@
-// tc.cuh -- the instructions of sm_103a that prompt.cu is built from: barriers
+// tc.cuh -- the instructions of sm_103a that prompt.cuh is built from: barriers
 // in shared memory, tile copies, fifth-generation tensor cores and their memory.
 #pragma once
 #include <cuda.h>

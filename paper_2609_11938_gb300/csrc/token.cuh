@@ -19,7 +19,7 @@
 //   scores   S^T [16 keys x 8 queries] = K [16 x D] Q^T
 //   result   O^T [D x 8 queries]      += V^T [D x 16 keys] P^T
 // The queries of a key head (up to 8 or 16; more go round again) share its loads.
-// P is rounded to the inputs' type, which the products take, as in prompt.cu: against 64 bits the
+// P is rounded to the inputs' type, which the products take, as in prompt.cuh: against 64 bits the
 // results are 1.1 to 1.4 times as far off as their own rounding makes them.  As two terms, the
 // rounded weight and what that left, on the same registers of values, it took 0 to 2.4 % longer and
 // lost that factor, but an infinite value that is seen came out as NaN, since the second term may be 0.
@@ -198,7 +198,7 @@ template <typename T, int DP, int NT, int FR, bool E8, bool WIN, int TW, bool FU
 __global__ void __launch_bounds__(TOKEN_THREADS, E8 ? Eight<DP, NT>::BLOCKS : NT == 1 ? 3 : 2) k_token(const __grid_constant__ TokenArgs p, unsigned *err) {
     using P = std::conditional_t<E8, __half, T>;          // what the products take
     constexpr bool BF = std::is_same<P, __nv_bfloat16>::value;
-    // as in prompt.cu: weights up to 2^(OFFSET + SLACK), rescaled when a maximum outgrows SLACK
+    // as in prompt.cuh: weights up to 2^(OFFSET + SLACK), rescaled when a maximum outgrows SLACK
     constexpr float OFFSET = BF ? 0.f : 8.f, SLACK = BF ? 8.f : 7.f;
     constexpr int KC = DP / (E8 ? 64 : 32), VC = DP / 64, STEP = 16 * FR * TW, NQ = 8 * NT, ROW = DP + 4;
     __shared__ float so[TOKEN_WARPS][NQ][ROW];
@@ -525,8 +525,8 @@ __global__ void __launch_bounds__(TOKEN_THREADS, E8 ? Eight<DP, NT>::BLOCKS : NT
                         const uint8_t *at = (const uint8_t *)((const T *)kv.v_pages + kat[f] + (2 * col * DP + 8 * row));
                         vr[f][0][0] = get16<0>(at), vr[f][1][0] = get16<2 * DP>(at), vr[f][2][0] = get16<16 * DP>(at), vr[f][3][0] = get16<18 * DP>(at);
                         if constexpr (DP == 128) {
-                            vr[f][0][E8 ? 0 : VC - 1] = get16<128>(at), vr[f][1][E8 ? 0 : VC - 1] = get16<2 * DP + 128>(at);
-                            vr[f][2][E8 ? 0 : VC - 1] = get16<16 * DP + 128>(at), vr[f][3][E8 ? 0 : VC - 1] = get16<18 * DP + 128>(at);
+                            vr[f][0][VC - 1] = get16<128>(at), vr[f][1][VC - 1] = get16<2 * DP + 128>(at);
+                            vr[f][2][VC - 1] = get16<16 * DP + 128>(at), vr[f][3][VC - 1] = get16<18 * DP + 128>(at);
                         }
                         continue;
                     }
