@@ -68,16 +68,20 @@ constexpr unsigned PARTLY = 1u << 30;
 constexpr int WHOLE_STEPS = 3;
 constexpr float JOIN_STEPS = 12.f;
 
-// Pages of 8 bits: sixteens of keys that a warp takes at a time, and blocks that an SM holds (by registers).
+// Pages of 8 bits: a warp takes two sixteens of keys at a time, and an SM holds so many blocks (by registers).
 // Of 64 wide heads, 200 sequences of 1,028 tokens, 16 heads: two sixteens in four blocks 79 us, one in five 84, four in
 // three 94; of 128 wide, 2 sequences of 500,000, 40 heads on 8: two in three blocks 307 us, one in four 318, two in four (which do
-// not fit) 454.  Each warp has pairs of its own once there are so many for an SM (TW below), us with
-// all of a block's warps at one and by themselves: 16 heads of 64, 608 pairs of 1,028 tokens 22 and 25, 1,216 39 and 40, 1,824
-// 54 and 53, 3,648 102 and 91; 32 heads of 128 on 8, 1,216 pairs 66 and 68, 1,824 89 and 85, 3,648 173 and 163.
+// not fit) 454.
 template <int DP, int NT>
 struct Eight {
-    static constexpr int BLOCKS = NT > 1 ? 2 : DP == 64 ? 4 : 3, PAIRS = DP == 64 ? 8 : 12;
+    static constexpr int BLOCKS = NT > 1 ? 2 : DP == 64 ? 4 : 3;
 };
+// Pairs for each SM from which on a warp has pairs of its own (TW below; pages of 8 bits, and windows), us with all of a block's
+// warps at a pair and by themselves.  8 bits, 16 heads of 64: 608 pairs of 1,028 tokens 22 and 25, 1,216 39 and 40, 1,824
+// 54 and 53, 3,648 102 and 91; 32 heads of 128 on 8, 1,216 pairs 66 and 68, 1,824 89 and 85, 3,648 173 and 163.  16 bits through
+// a window of 256, 16 heads of 64: 448 pairs 15 and 19, 912 23 and 23, 1,824 37 and 31, 3,648 65 and 51; 32 of 128 on 8: 912 31
+// and 32, 1,824 52 and 46.
+constexpr int own_pairs(int dp) { return dp == 64 ? 8 : 12; }
 
 struct TokenArgs {
     opattr_cache kv;
@@ -783,8 +787,8 @@ static opattr_status run_teams(Ctx &c, Serve &s, TokenArgs &p) {
 }
 template <typename T, int DP, int NT, int FR, bool E8, bool WIN, bool FULL>
 static opattr_status run_token(Ctx &c, Serve &s, TokenArgs &p) {
-    if constexpr (E8) {
-        if ((int64_t)p.n * p.kv.kv_heads * p.blocks_of_heads >= Eight<DP, NT>::PAIRS * (int64_t)sm_count(c)) return run_teams<T, DP, NT, FR, E8, WIN, 1, FULL>(c, s, p);
+    if constexpr (E8 || WIN) {
+        if ((int64_t)p.n * p.kv.kv_heads * p.blocks_of_heads >= own_pairs(DP) * (int64_t)sm_count(c)) return run_teams<T, DP, NT, FR, E8, WIN, 1, FULL>(c, s, p);
     }
     return run_teams<T, DP, NT, FR, E8, WIN, TOKEN_WARPS, FULL>(c, s, p);
 }

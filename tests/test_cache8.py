@@ -250,6 +250,29 @@ def test_attention(ctx, dtype, dim, heads, kv, page, window, sinks):
     check_attention(ctx, c, randn(g, (len(seqs), heads, dim), dtype, 1.5), seqs, window, sinks)
 
 
+@pytest.mark.parametrize("dim,heads,dtype", [(64, 4, BF), (48, 48, HF), (128, 8, HF), (96, 40, BF)])
+@pytest.mark.parametrize("window,sinks", [(None, 0), (100, 20), (3000, 1)])
+def test_many_pairs(ctx, dim, heads, dtype, window, sinks):
+    """So many sequences and key heads that each warp has its own, with some among them that many warps share."""
+    rng = random.Random(dim)
+    lens = [rng.choice([0, 1, 15, 33, rng.randint(1, 300)]) for _ in range(490)] + [9000, 3001, 700]
+    rng.shuffle(lens)
+    c, g = filled(ctx, lens, 32, 4, dim, dtype, dim)
+    seqs = list(range(len(lens)))
+    q = randn(g, (len(lens), heads, dim), dtype, 1.5)
+    _, out, lse = ctx.cache_attention(c, None, q, need_lse=True, window=window, sinks=sinks)
+    again = ctx.cache_attention(c, i32(seqs), q, need_lse=True, window=window, sinks=sinks)
+    ctx.check()
+    assert torch.equal(out, again[1]) and torch.equal(lse, again[2])
+    for s in [i for i, n in enumerate(lens) if n > 600] + rng.sample(seqs, 40):
+        k, v = stands_for(c, s)
+        n = k.shape[0]
+        seen = near_mask(1, n, window or n, sinks, DEV) if n else torch.ones((1, 0), dtype=torch.bool, device=DEV)
+        want, wl, lim, ll = attend8(q[s:s + 1], k, v, dim ** -0.5, seen)
+        assert_within(out[s:s + 1], want, lim, f"out of sequence {s} ({n} tokens)")
+        assert_within(lse[s:s + 1], wl, ll, f"lse of sequence {s} ({n} tokens)")
+
+
 @pytest.mark.parametrize("dtype", [BF, HF])
 def test_scales_far_apart(ctx, dtype):
     """Blocks whose scales are many powers of two apart, and queries of every size."""

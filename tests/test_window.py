@@ -167,6 +167,29 @@ def test_tokens(ctx, dtype, dim, heads, kv, page, window, sinks):
     check_token(ctx, c, k, v, lens, randn(g, (len(seqs), heads, dim), dtype, 1.5), seqs, window, sinks)
 
 
+@pytest.mark.parametrize("dim,heads,dtype", [(64, 4, BF), (40, 48, HF), (128, 8, HF), (96, 40, BF)])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (100, 20), (3000, 1)])
+def test_many_pairs(ctx, dim, heads, dtype, window, sinks):
+    """So many sequences and key heads that each warp has its own, with some among them that many warps share."""
+    g = gen(dim)
+    lens = torch.randint(0, 300, (490,), generator=g, device=DEV).tolist() + [9000, 0, 1, 3001, 700]
+    c, k, v, g = filled(ctx, lens, 32, 4, dim, dtype, dim)
+    seqs = torch.randperm(len(lens), generator=g, device=DEV).tolist()
+    q = randn(g, (len(lens), heads, dim), dtype, 1.5)
+    a, b = (ctx.cache_attention(c, i32(seqs), q, need_lse=True, window=window, sinks=sinks) for _ in range(2))
+    ctx.check()
+    assert torch.equal(a[1], b[1]) and torch.equal(a[2], b[2])
+    starts = [sum(lens[:i]) for i in range(len(lens))]
+    for i, s in enumerate(seqs):
+        at, n = starts[s], lens[s]
+        if n < 600 and i % 9:
+            continue
+        seen = near_mask(1, n, window, sinks, DEV) if n else torch.ones((1, 0), dtype=torch.bool, device=DEV)
+        want, wl, lim, ll = attend(q[i:i + 1], k[at:at + n], v[at:at + n], dim ** -0.5, seen)
+        assert_within(a[1][i:i + 1], want, lim, f"out of sequence {s} ({n} tokens)")
+        assert_within(a[2][i:i + 1], wl, ll, f"lse of sequence {s} ({n} tokens)")
+
+
 @pytest.mark.parametrize("window,sinks", [(20_000, 4), (30_000, 9000), (64, 0)])
 def test_long_contexts(ctx, window, sinks):
     """Windows of many blocks' runs, and one that is little of what there is."""
