@@ -43,7 +43,7 @@
 // ones have the sinks, the others begin where the window does.
 //   8 bits, bytes as above: 2 of 500,000, 40 heads of 128 on 8: 304 us, 6.8 TB/s; 64 of 1 .. 16,001, 32 heads on 8: 44 us,
 //   4.7, of which about 13 are the launch, first loads and joins; 200 of 4,096, 16 heads of 64: 279 us, 6.0.
-//   A window of 4,096 and 4 sinks, 16 bits: 96 of 1 .. 20,001, 32 heads of 128 on 8: 83 us, 6.0.
+//   A window of 4,096 and 4 sinks, 16 bits: 96 of 1 .. 20,001, 32 heads of 128 on 8: 80 us, 6.2.
 // Tried for 8 bits: a ring of copies in shared memory, three to six steps ahead, in the place of loads into registers: 350 us
 // for the 304 at every depth, and 77 for 79 at 200 sequences of 64 wide heads.
 #pragma once

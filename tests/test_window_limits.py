@@ -31,15 +31,16 @@ def i32(*x):
     return torch.tensor(x, dtype=torch.int32, device=DEV)
 
 
-@pytest.mark.parametrize("eight,dim", [(False, 8), (False, 72), (True, 16), (True, 64), (True, 128)])
+KINDS = [(False, 8), (False, 72), (True, 16), (True, 64), (True, 128)]        # 8 bits, and the width
+VIEWS = [(None, 0), (1000, 0), (1000, 1000), (5, 1), (MOST, MOST), (1, MOST), (MOST // 2, 0)]
+
+
 @pytest.mark.parametrize("page,short", [(1024, 0), (1024, 1), (16, 0), (16, 17)])
-@pytest.mark.parametrize("window,sinks", [(None, 0), (1000, 0), (1000, 1000), (5, 1), (MOST, MOST), (1, MOST), (MOST // 2, 0)])
+@pytest.mark.parametrize("eight,dim,window,sinks", [k + v for k in KINDS for v in VIEWS if k[0] or v[0]])
 def test_token_longest(opa, ctx, eight, dim, page, short, window, sinks):
     """A sequence as long as a table can say, all of whose pages but the last are the same one.  The
     first head sees all keys alike, half with a value of 1 and half of 3; the second nothing but the
     last key."""
-    if not eight and window is None:
-        pytest.skip("tested without a window elsewhere")
     per = MOST // page
     length = per * page - short
     k, v = (torch.zeros((2, 1, page, dim), device=DEV) for _ in range(2))
