@@ -76,6 +76,14 @@ template <int DP, int NT>
 struct Eight {
     static constexpr int BLOCKS = NT > 1 ? 2 : DP == 64 ? 4 : 3;
 };
+// (pages of 8 bits) A weight stands at 2^15 at most, and a row's sums are divided by that of its weights at the end: sums of
+// values from 2^113 on may leave 32 bits before.  A warp whose results come out at LARGE or more, or not finite, makes
+// them again, LOWERED times as large: 2^31 tokens of 2^128 stay below 2^(15 + 31 + 128 - 64) so, and small values beside them
+// lose 2^-86 a token.  Values below 2^49 are LARGE in no sum of 2^31 tokens.  All other calls pay a product for each 16
+// keys and a look at the results, 0 to 4 % (114 sequences of 2,060 tokens, 16 heads of 64: 87.1 us without, 87.9; half through a
+// window, 128 wide, 31.0 and 33.6).  Scales watched on the way took registers that are not there: 18 % where 12 heads of 128 share
+// keys.
+constexpr float LARGE = 0x1p96f, LOWERED = 0x1p-64f;
 // Pairs for each SM from which on a warp has pairs of its own (TW below; pages of 8 bits, and windows), us with all of a block's
 // warps at a pair and by themselves.  8 bits, 16 heads of 64: 608 pairs of 1,028 tokens 22 and 25, 1,216 39 and 40, 1,824
 // 54 and 53, 3,648 102 and 91; 32 heads of 128 on 8, 1,216 pairs 66 and 68, 1,824 89 and 85, 3,648 173 and 163.  16 bits through
@@ -111,6 +119,12 @@ __device__ __forceinline__ uint2 load8(const void *p, bool on) {
 __device__ __forceinline__ float root(float x) {
     float r;
     asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+// The larger of two, NaN where one is.
+__device__ __forceinline__ float max_nan(float x, float y) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
     return r;
 }
 template <typename T>
@@ -326,6 +340,7 @@ __global__ void __launch_bounds__(TOKEN_THREADS, E8 ? Eight<DP, NT>::BLOCKS : NT
             }
         }
         float o[NT][DP / 16][4] = {}, m[NT][2], l[NT][2] = {};
+        float level = 1.f;                                // (pages of 8 bits) o is that many times what it stands for
 #pragma unroll
         for (int t = 0; t < NT; ++t) m[t][0] = m[t][1] = -INFINITY;
         // (unsigned where a step past a length near 2^31 is counted)
@@ -547,130 +562,154 @@ __global__ void __launch_bounds__(TOKEN_THREADS, E8 ? Eight<DP, NT>::BLOCKS : NT
                 }
             }
         };
-        load_keys(from);
-        load_values();
-        for (int step = from; step < to; ++step) {
-            if (E8 && vnone) {                            // (of a warp: nothing of this step is its own)
-                if (step + 1 < to) load_keys(step + 1), load_values();
-                continue;
-            }
-            float x[FR][NT][4] = {};
-#pragma unroll
-            for (int f = 0; f < FR; ++f)
-#pragma unroll
-                for (int i = 0; i < KC; ++i) {
-                    const uint4 u = kr[f][0][i], w = kr[f][1][i];
-                    if constexpr (E8) {
-                        const uint32_t *u4 = &u.x, *w4 = &w.x;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const uint32_t a0 = half_lo(u4[j]), a1 = half_lo(w4[j]), a2 = half_hi(u4[j]), a3 = half_hi(w4[j]);
-#pragma unroll
-                            for (int t = 0; t < NT; ++t) mma16<P>(x[f][t], a0, a1, a2, a3, qf[t][i][2 * j], qf[t][i][2 * j + 1]);
-                        }
-                    } else {
-#pragma unroll
-                        for (int t = 0; t < NT; ++t) {
-                            mma16<T>(x[f][t], u.x, w.x, u.y, w.y, qf[t][i][0], qf[t][i][1]);
-                            mma16<T>(x[f][t], u.z, w.z, u.w, w.w, qf[t][i][2], qf[t][i][3]);
-                        }
-                    }
+        for (;;) {
+            load_keys(from);
+            load_values();
+            for (int step = from; step < to; ++step) {
+                if (E8 && vnone) {                            // (of a warp: nothing of this step is its own)
+                    if (step + 1 < to) load_keys(step + 1), load_values();
+                    continue;
                 }
-            if constexpr (E8) {
+                float x[FR][NT][4] = {};
 #pragma unroll
                 for (int f = 0; f < FR; ++f)
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        const float k0 = ks[f] * cq[t][0], k1 = ks[f] * cq[t][1];
-                        x[f][t][0] *= k0, x[f][t][1] *= k1, x[f][t][2] *= k0, x[f][t][3] *= k1;
+                    for (int i = 0; i < KC; ++i) {
+                        const uint4 u = kr[f][0][i], w = kr[f][1][i];
+                        if constexpr (E8) {
+                            const uint32_t *u4 = &u.x, *w4 = &w.x;
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const uint32_t a0 = half_lo(u4[j]), a1 = half_lo(w4[j]), a2 = half_hi(u4[j]), a3 = half_hi(w4[j]);
+#pragma unroll
+                                for (int t = 0; t < NT; ++t) mma16<P>(x[f][t], a0, a1, a2, a3, qf[t][i][2 * j], qf[t][i][2 * j + 1]);
+                            }
+                        } else {
+#pragma unroll
+                            for (int t = 0; t < NT; ++t) {
+                                mma16<T>(x[f][t], u.x, w.x, u.y, w.y, qf[t][i][0], qf[t][i][1]);
+                                mma16<T>(x[f][t], u.z, w.z, u.w, w.w, qf[t][i][2], qf[t][i][3]);
+                            }
+                        }
                     }
-                if (!vall) {
+                if constexpr (E8) {
 #pragma unroll
                     for (int f = 0; f < FR; ++f)
 #pragma unroll
-                        for (int t = 0; t < NT; ++t)
+                        for (int t = 0; t < NT; ++t) {
+                            const float k0 = ks[f] * cq[t][0], k1 = ks[f] * cq[t][1];
+                            x[f][t][0] *= k0, x[f][t][1] *= k1, x[f][t][2] *= k0, x[f][t][3] *= k1;
+                        }
+                    if (!vall) {
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) x[f][t][i] = seen(row + 8 * (i >> 1), vlim[f]) ? x[f][t][i] : -INFINITY;
+                        for (int f = 0; f < FR; ++f)
+#pragma unroll
+                            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) x[f][t][i] = seen(row + 8 * (i >> 1), vlim[f]) ? x[f][t][i] : -INFINITY;
+                    }
                 }
-            }
-            if (step + 1 < to) load_keys(step + 1);
-            float top[NT][2];
-            bool more = false;
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                top[t][0] = top[t][1] = -INFINITY;
-#pragma unroll
-                for (int f = 0; f < FR; ++f)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if (!E8) x[f][t][i] = (WIN && vall) || seen(row + 8 * (i >> 1), vlim[f]) ? x[f][t][i] * c : -INFINITY;
-                        top[t][i & 1] = fmaxf(top[t][i & 1], x[f][t][i]);
-                    }
-                more = more || top[t][0] - m[t][0] > SLACK || top[t][1] - m[t][1] > SLACK;
-            }
-            if (__any_sync(0xffffffffu, more)) {
-#pragma unroll
-                for (int t = 0; t < NT; ++t)
-#pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        float y = fmaxf(m[t][q], top[t][q]);
-#pragma unroll
-                        for (int e = 4; e < 32; e <<= 1) y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, e));
-                        const float keep = y == m[t][q] ? 1.f : exp2_fast(m[t][q] - y);
-                        m[t][q] = y;
-                        l[t][q] *= keep;
-#pragma unroll
-                        for (int i = 0; i < DP / 16; ++i) o[t][i][q] *= keep, o[t][i][q + 2] *= keep;
-                    }
-            }
-#pragma unroll
-            for (int f = 0; f < FR; ++f) {
-                uint32_t pb[NT][2];
+                if (step + 1 < to) load_keys(step + 1);
+                float top[NT][2];
+                bool more = false;
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
-                    float y[4];
+                    top[t][0] = top[t][1] = -INFINITY;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float ref = m[t][i & 1];
-                        y[i] = exp2_fast(x[f][t][i] - (ref == -INFINITY ? -OFFSET : ref - OFFSET));
-                        l[t][i & 1] += y[i];
-                    }
-                    pb[t][0] = transpose8(Type2<P>::down(y[0], y[1]));
-                    pb[t][1] = transpose8(Type2<P>::down(y[2], y[3]));
-                }
-                if constexpr (E8) {
-                    // a block's products by themselves, times its scale: scales may lie too far apart for
-                    // weights that carry them
-                    const uint32_t *v0 = &vr[f][0][0].x, *v1 = &vr[f][1][0].x, *v2 = &vr[f][2][0].x, *v3 = &vr[f][3][0].x;
+                    for (int f = 0; f < FR; ++f)
 #pragma unroll
-                    for (int j = 0; j < DP / 32; ++j)
-#pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const uint32_t u = __byte_perm(v0[j], v1[j], e ? 0x7362 : 0x5140), w = __byte_perm(v2[j], v3[j], e ? 0x7362 : 0x5140);
-                            const uint32_t a0 = half_lo(u), a1 = half_hi(u), a2 = half_lo(w), a3 = half_hi(w);
-#pragma unroll
-                            for (int t = 0; t < NT; ++t) {
-                                float z[4];
-                                mma16_new(z, a0, a1, a2, a3, pb[t][0], pb[t][1]);
-                                float (&y)[4] = o[t][2 * j + e];
-                                fma_pair(y[0], y[1], z[0], z[1], vs[f]);
-                                fma_pair(y[2], y[3], z[2], z[3], vs[f]);
-                            }
+                        for (int i = 0; i < 4; ++i) {
+                            if (!E8) x[f][t][i] = (WIN && vall) || seen(row + 8 * (i >> 1), vlim[f]) ? x[f][t][i] * c : -INFINITY;
+                            top[t][i & 1] = fmaxf(top[t][i & 1], x[f][t][i]);
                         }
-                } else
+                    more = more || top[t][0] - m[t][0] > SLACK || top[t][1] - m[t][1] > SLACK;
+                }
+                if constexpr (E8)
 #pragma unroll
-                for (int i = 0; i < VC; ++i) {
-                    const uint32_t *v0 = &vr[f][0][i].x, *v1 = &vr[f][1][i].x, *v2 = &vr[f][2][i].x, *v3 = &vr[f][3][i].x;
+                    for (int f = 0; f < FR; ++f) vs[f] *= level;
+                if (__any_sync(0xffffffffu, more)) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t a0 = __byte_perm(v0[e], v1[e], 0x5410), a1 = __byte_perm(v0[e], v1[e], 0x7632);
-                        const uint32_t a2 = __byte_perm(v2[e], v3[e], 0x5410), a3 = __byte_perm(v2[e], v3[e], 0x7632);
+                    for (int t = 0; t < NT; ++t)
 #pragma unroll
-                        for (int t = 0; t < NT; ++t) mma16<T>(o[t][4 * i + e], a0, a1, a2, a3, pb[t][0], pb[t][1]);
+                        for (int q = 0; q < 2; ++q) {
+                            float y = fmaxf(m[t][q], top[t][q]);
+#pragma unroll
+                            for (int e = 4; e < 32; e <<= 1) y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, e));
+                            const float keep = y == m[t][q] ? 1.f : exp2_fast(m[t][q] - y);
+                            m[t][q] = y;
+                            l[t][q] *= keep;
+#pragma unroll
+                            for (int i = 0; i < DP / 16; ++i) o[t][i][q] *= keep, o[t][i][q + 2] *= keep;
+                        }
+                }
+#pragma unroll
+                for (int f = 0; f < FR; ++f) {
+                    uint32_t pb[NT][2];
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        float y[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float ref = m[t][i & 1];
+                            y[i] = exp2_fast(x[f][t][i] - (ref == -INFINITY ? -OFFSET : ref - OFFSET));
+                            l[t][i & 1] += y[i];
+                        }
+                        pb[t][0] = transpose8(Type2<P>::down(y[0], y[1]));
+                        pb[t][1] = transpose8(Type2<P>::down(y[2], y[3]));
+                    }
+                    if constexpr (E8) {
+                        // a block's products by themselves, times its scale: scales may lie too far apart for
+                        // weights that carry them
+                        const uint32_t *v0 = &vr[f][0][0].x, *v1 = &vr[f][1][0].x, *v2 = &vr[f][2][0].x, *v3 = &vr[f][3][0].x;
+#pragma unroll
+                        for (int j = 0; j < DP / 32; ++j)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const uint32_t u = __byte_perm(v0[j], v1[j], e ? 0x7362 : 0x5140), w = __byte_perm(v2[j], v3[j], e ? 0x7362 : 0x5140);
+                                const uint32_t a0 = half_lo(u), a1 = half_hi(u), a2 = half_lo(w), a3 = half_hi(w);
+#pragma unroll
+                                for (int t = 0; t < NT; ++t) {
+                                    float z[4];
+                                    mma16_new(z, a0, a1, a2, a3, pb[t][0], pb[t][1]);
+                                    float (&y)[4] = o[t][2 * j + e];
+                                    fma_pair(y[0], y[1], z[0], z[1], vs[f]);
+                                    fma_pair(y[2], y[3], z[2], z[3], vs[f]);
+                                }
+                            }
+                    } else
+#pragma unroll
+                    for (int i = 0; i < VC; ++i) {
+                        const uint32_t *v0 = &vr[f][0][i].x, *v1 = &vr[f][1][i].x, *v2 = &vr[f][2][i].x, *v3 = &vr[f][3][i].x;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t a0 = __byte_perm(v0[e], v1[e], 0x5410), a1 = __byte_perm(v0[e], v1[e], 0x7632);
+                            const uint32_t a2 = __byte_perm(v2[e], v3[e], 0x5410), a3 = __byte_perm(v2[e], v3[e], 0x7632);
+#pragma unroll
+                            for (int t = 0; t < NT; ++t) mma16<T>(o[t][4 * i + e], a0, a1, a2, a3, pb[t][0], pb[t][1]);
+                        }
                     }
                 }
+                if (step + 1 < to) load_values();
             }
-            if (step + 1 < to) load_values();
+            if constexpr (!E8) break;
+            float most = 0.f;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < DP / 16; ++i)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) most = max_nan(most, fabsf(o[t][i][q]));
+            if (__all_sync(0xffffffffu, level != 1.f || most < LARGE)) break;
+            level = LOWERED;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+#pragma unroll
+                for (int i = 0; i < DP / 16; ++i)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) o[t][i][q] = 0.f;
+                m[t][0] = m[t][1] = -INFINITY;
+                l[t][0] = l[t][1] = 0.f;
+            }
         }
 
         // ---- the warps' parts together
@@ -682,7 +721,8 @@ __global__ void __launch_bounds__(TOKEN_THREADS, E8 ? Eight<DP, NT>::BLOCKS : NT
 #pragma unroll
                 for (int e = 4; e < 32; e <<= 1) y += __shfl_xor_sync(0xffffffffu, y, e);
                 const int h = 8 * t + 2 * col + q;
-                if (row == 0) sm[warp][h] = m[t][q], sl[warp][h] = y;
+                // (a sum is at least 0; its sign says whether the results are lowered)
+                if (row == 0) sm[warp][h] = m[t][q], sl[warp][h] = E8 && level != 1.f ? -y : y;
 #pragma unroll
                 for (int i = 0; i < VC; ++i) {
                     float *at = &so[warp][h][E8 ? DP / 8 * row + 8 * i : 64 * i + 8 * row];
@@ -693,13 +733,16 @@ __global__ void __launch_bounds__(TOKEN_THREADS, E8 ? Eight<DP, NT>::BLOCKS : NT
         together();
         const bool whole = from == 0 && to == steps;
         constexpr int PART = NQ * (DP + 2);
-        auto finish = [&](int h, int d, float top, float sum, const float *y) {
+        auto is_low = [](float sum) { return E8 && __float_as_int(sum) < 0; };
+        auto finish = [&](int h, int d, float top, float sum, float (&y)[8], bool lowered) {
             const float share = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = lowered ? y[e] * share * (1.f / LOWERED) : y[e] * share;
             uint4 r;
-            r.x = sum == 0.f ? 0u : Type2<T>::down(y[0] * share, y[1] * share);
-            r.y = sum == 0.f ? 0u : Type2<T>::down(y[2] * share, y[3] * share);
-            r.z = sum == 0.f ? 0u : Type2<T>::down(y[4] * share, y[5] * share);
-            r.w = sum == 0.f ? 0u : Type2<T>::down(y[6] * share, y[7] * share);
+            r.x = sum == 0.f ? 0u : Type2<T>::down(y[0], y[1]);
+            r.y = sum == 0.f ? 0u : Type2<T>::down(y[2], y[3]);
+            r.z = sum == 0.f ? 0u : Type2<T>::down(y[4], y[5]);
+            r.w = sum == 0.f ? 0u : Type2<T>::down(y[6], y[7]);
             *reinterpret_cast<uint4 *>((T *)p.out.data + b * p.out.token_stride + (head0 + h) * p.out.head_stride + d) = r;
             if (p.lse && d == 0)
                 p.lse[(long long)b * p.q_heads + head0 + h] =
@@ -710,20 +753,22 @@ __global__ void __launch_bounds__(TOKEN_THREADS, E8 ? Eight<DP, NT>::BLOCKS : NT
             const int h = i / (DP / 8), d = i % (DP / 8) * 8;
             if (h >= heads || d >= kv.head_dim) continue;
             float top = -INFINITY, sum = 0.f, y[8] = {};
+            bool any_low = false;
 #pragma unroll
-            for (int w = own; w < own + TW; ++w) top = fmaxf(top, sm[w][h]);
+            for (int w = own; w < own + TW; ++w) top = fmaxf(top, sm[w][h]), any_low = any_low || is_low(sl[w][h]);
 #pragma unroll
             for (int w = own; w < own + TW; ++w) {
                 const float keep = sm[w][h] == top ? 1.f : exp2_fast(sm[w][h] - top);
-                sum = __fmaf_rn(sl[w][h], keep, sum);
+                sum = __fmaf_rn(fabsf(sl[w][h]), keep, sum);
+                const float share = any_low && !is_low(sl[w][h]) ? keep * LOWERED : keep;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = __fmaf_rn(so[w][h][d + e], keep, y[e]);
+                for (int e = 0; e < 8; ++e) y[e] = __fmaf_rn(so[w][h][d + e], share, y[e]);
             }
-            if (whole) finish(h, d, top, sum, y);
+            if (whole) finish(h, d, top, sum, y, any_low);
             else {
                 __stcg(reinterpret_cast<float4 *>(part + h * DP + d), make_float4(y[0], y[1], y[2], y[3]));
                 __stcg(reinterpret_cast<float4 *>(part + h * DP + d + 4), make_float4(y[4], y[5], y[6], y[7]));
-                if (d == 0) __stcg(reinterpret_cast<float2 *>(part + NQ * DP) + h, make_float2(top, sum));
+                if (d == 0) __stcg(reinterpret_cast<float2 *>(part + NQ * DP) + h, make_float2(top, any_low ? -sum : sum));
             }
         }
         if (!whole) {
@@ -746,21 +791,25 @@ __global__ void __launch_bounds__(TOKEN_THREADS, E8 ? Eight<DP, NT>::BLOCKS : NT
                     const int h = i / (DP / 8), d = i % (DP / 8) * 8;
                     if (h >= heads || d >= kv.head_dim) continue;
                     float top = -INFINITY, sum = 0.f, y[8] = {};
+                    bool any_low = false;
 #pragma unroll 4
                     for (int k = block1; k <= block2; ++k) {
                         const float *at = p.parts + ((long long)k * 2 + (k == block1)) * PART;
                         const float2 ml = __ldcg(reinterpret_cast<const float2 *>(at + NQ * DP) + h);
                         const float4 u = __ldcg(reinterpret_cast<const float4 *>(at + h * DP + d));
                         const float4 w = __ldcg(reinterpret_cast<const float4 *>(at + h * DP + d + 4));
-                        const float t = fmaxf(top, ml.x), a = top == t ? 1.f : exp2_fast(top - t), z = ml.x == t ? 1.f : exp2_fast(ml.x - t);
+                        const float t = fmaxf(top, ml.x);
+                        float a = top == t ? 1.f : exp2_fast(top - t), z = ml.x == t ? 1.f : exp2_fast(ml.x - t);
                         top = t;
-                        sum = __fmaf_rn(ml.y, z, sum * a);
+                        sum = __fmaf_rn(fabsf(ml.y), z, sum * a);
+                        // (parts that are not lowered, where others are)
+                        if (E8 && is_low(ml.y) != any_low) (any_low ? z : a) *= LOWERED, any_low = true;
                         y[0] = __fmaf_rn(u.x, z, y[0] * a), y[1] = __fmaf_rn(u.y, z, y[1] * a);
                         y[2] = __fmaf_rn(u.z, z, y[2] * a), y[3] = __fmaf_rn(u.w, z, y[3] * a);
                         y[4] = __fmaf_rn(w.x, z, y[4] * a), y[5] = __fmaf_rn(w.y, z, y[5] * a);
                         y[6] = __fmaf_rn(w.z, z, y[6] * a), y[7] = __fmaf_rn(w.w, z, y[7] * a);
                     }
-                    finish(h, d, top, sum, y);
+                    finish(h, d, top, sum, y, any_low);
                 }
                 if (me == 0) p.tickets[block1] = 0;
             }
