@@ -55,7 +55,7 @@ bool cache_ok(const opattr_cache *k) {
 opattr_status serve_ready(Ctx &c, Serve &s) {
     if (s.err) return OPATTR_OK;
     if (capturing(c)) return OPATTR_E_OOM;               // as for the scratch
-    const size_t bytes = 256 + sizeof(uint32_t) * TICKETS;
+    const size_t bytes = 256 + sizeof(uint32_t) * ALL_TICKETS;
     cudaError_t e = cudaMalloc(&s.err, bytes);
     if (e == cudaErrorMemoryAllocation) {
         cudaGetLastError();

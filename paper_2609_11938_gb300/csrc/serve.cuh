@@ -29,6 +29,7 @@ struct Serve {
 constexpr int SILENT_PARTS = -1;
 
 constexpr int TICKETS = 4096;        // at most four blocks an SM, or their sixteen warps, count in them
+constexpr int ALL_TICKETS = 3 * TICKETS;   // and in two more each, where parts are joined in groups
 opattr_status serve_ready(Ctx &c, Serve &s);
 void serve_free(Serve &s);
 

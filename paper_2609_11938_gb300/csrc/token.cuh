@@ -67,6 +67,11 @@ constexpr int TOKEN_WARPS = 4, TOKEN_THREADS = 32 * TOKEN_WARPS;
 constexpr unsigned PARTLY = 1u << 30;
 constexpr int WHOLE_STEPS = 3;
 constexpr float JOIN_STEPS = 12.f;
+// A warp by itself (TW below) takes 0.2 us to join a part more, 0.4 of 128 wide heads, and a sequence that is long among
+// many short ones has hundreds.  Past GROUP parts it joins in two stages, groups of about their root, whose last warps do it side by
+// side: one of 200,000 tokens among 1,500 of 300, 8 bits, 8 heads of 64 on one: 160 us in one stage, 37; among 2,300 of 1,000, 128 wide
+// 160, 119; through a window of 100,000, 16 bits, among 2,300 of 300, 64 wide 75, 49.
+constexpr int GROUP = 8;
 
 // Pages of 8 bits: a warp takes two sixteens of keys at a time, and an SM holds so many blocks (by registers).
 // Of 64 wide heads, 200 sequences of 1,028 tokens, 16 heads: two sixteens in four blocks 79 us, one in five 84, four in
@@ -100,7 +105,7 @@ struct TokenArgs {
     float scale;
     int shift;                                // log2 of the page size
     float *parts;                             // [grid][2] partial results
-    uint32_t *tickets;                        // [grid]
+    uint32_t *tickets;                        // [TICKETS] of pairs, then [2 TICKETS] of groups of their parts
     const float *k_scales, *v_scales;         // (pages of 8 bits)
     int window, sinks;                        // (through a window) last tokens that are seen, and first ones
 };
@@ -748,7 +753,11 @@ __global__ void __launch_bounds__(TOKEN_THREADS, E8 ? Eight<DP, NT>::BLOCKS : NT
                 p.lse[(long long)b * p.q_heads + head0 + h] =
                     sum == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) - OFFSET + log2f(sum)) * LN2;
         };
-        float *part = p.parts + ((long long)team * 2 + (from == 0)) * PART;
+        auto put_part = [&](float *part, int h, int d, float top, float sum, float (&y)[8], bool any_low) {
+            __stcg(reinterpret_cast<float4 *>(part + h * DP + d), make_float4(y[0], y[1], y[2], y[3]));
+            __stcg(reinterpret_cast<float4 *>(part + h * DP + d + 4), make_float4(y[4], y[5], y[6], y[7]));
+            if (d == 0) __stcg(reinterpret_cast<float2 *>(part + NQ * DP) + h, make_float2(top, any_low ? -sum : sum));
+        };
         for (int i = me; i < NQ * (DP / 8); i += 32 * TW) {
             const int h = i / (DP / 8), d = i % (DP / 8) * 8;
             if (h >= heads || d >= kv.head_dim) continue;
@@ -765,53 +774,75 @@ __global__ void __launch_bounds__(TOKEN_THREADS, E8 ? Eight<DP, NT>::BLOCKS : NT
                 for (int e = 0; e < 8; ++e) y[e] = __fmaf_rn(so[w][h][d + e], share, y[e]);
             }
             if (whole) finish(h, d, top, sum, y, any_low);
-            else {
-                __stcg(reinterpret_cast<float4 *>(part + h * DP + d), make_float4(y[0], y[1], y[2], y[3]));
-                __stcg(reinterpret_cast<float4 *>(part + h * DP + d + 4), make_float4(y[4], y[5], y[6], y[7]));
-                if (d == 0) __stcg(reinterpret_cast<float2 *>(part + NQ * DP) + h, make_float2(top, any_low ? -sum : sum));
-            }
+            else put_part(p.parts + ((long long)team * 2 + (from == 0)) * PART, h, d, top, sum, y, any_low);
         }
         if (!whole) {
             // a pair's parts: the block it begins in keeps its own in place 1, later ones in place 0
             const int block1 = (int)(((unit_at + 1) * W - 1) / total), block2 = (int)(((unit_at + steps) * W - 1) / total);
-            __threadfence();
-            together();
-            int last = 0;
-            if (me == 0) last = atomicAdd(&p.tickets[block1], 1u) == (unsigned)(block2 - block1);
-            if (TW == 1) {
-                last = __shfl_sync(0xffffffffu, last, 0);
-            } else {
-                if (me == 0) last_one = last;
-                together();
-                last = last_one;
-            }
-            if (last) {
+            auto place = [&](int k) { return 2ll * k + (k == block1); };
+            // whether this is the last of `count` that come here, which has what the others brought
+            auto last_of = [&](uint32_t *ticket, int count) {
                 __threadfence();
+                together();
+                int last = 0;
+                if (me == 0) last = atomicAdd(ticket, 1u) == (unsigned)(count - 1);
+                if (TW == 1) {
+                    last = __shfl_sync(0xffffffffu, last, 0);
+                } else {
+                    if (me == 0) last_one = last;
+                    together();
+                    last = last_one;
+                }
+                if (last) {
+                    __threadfence();
+                    if (me == 0) *ticket = 0;
+                }
+                return last != 0;
+            };
+            // parts k0, k0 + by .. k1, in order: their sums, to put
+            auto join = [&](int k0, int k1, int by, auto &&put) {
                 for (int i = me; i < NQ * (DP / 8); i += 32 * TW) {
                     const int h = i / (DP / 8), d = i % (DP / 8) * 8;
-                    if (h >= heads || d >= kv.head_dim) continue;
+                    const bool on = h < heads && d < kv.head_dim;
                     float top = -INFINITY, sum = 0.f, y[8] = {};
                     bool any_low = false;
+                    if (on)
 #pragma unroll 4
-                    for (int k = block1; k <= block2; ++k) {
-                        const float *at = p.parts + ((long long)k * 2 + (k == block1)) * PART;
-                        const float2 ml = __ldcg(reinterpret_cast<const float2 *>(at + NQ * DP) + h);
-                        const float4 u = __ldcg(reinterpret_cast<const float4 *>(at + h * DP + d));
-                        const float4 w = __ldcg(reinterpret_cast<const float4 *>(at + h * DP + d + 4));
-                        const float t = fmaxf(top, ml.x);
-                        float a = top == t ? 1.f : exp2_fast(top - t), z = ml.x == t ? 1.f : exp2_fast(ml.x - t);
-                        top = t;
-                        sum = __fmaf_rn(fabsf(ml.y), z, sum * a);
-                        // (parts that are not lowered, where others are)
-                        if (E8 && is_low(ml.y) != any_low) (any_low ? z : a) *= LOWERED, any_low = true;
-                        y[0] = __fmaf_rn(u.x, z, y[0] * a), y[1] = __fmaf_rn(u.y, z, y[1] * a);
-                        y[2] = __fmaf_rn(u.z, z, y[2] * a), y[3] = __fmaf_rn(u.w, z, y[3] * a);
-                        y[4] = __fmaf_rn(w.x, z, y[4] * a), y[5] = __fmaf_rn(w.y, z, y[5] * a);
-                        y[6] = __fmaf_rn(w.z, z, y[6] * a), y[7] = __fmaf_rn(w.w, z, y[7] * a);
-                    }
-                    finish(h, d, top, sum, y, any_low);
+                        for (int k = k0; k <= k1; k += by) {
+                            const float *at = p.parts + place(k) * PART;
+                            const float2 ml = __ldcg(reinterpret_cast<const float2 *>(at + NQ * DP) + h);
+                            const float4 u = __ldcg(reinterpret_cast<const float4 *>(at + h * DP + d));
+                            const float4 w = __ldcg(reinterpret_cast<const float4 *>(at + h * DP + d + 4));
+                            const float t = fmaxf(top, ml.x);
+                            float a = top == t ? 1.f : exp2_fast(top - t), z = ml.x == t ? 1.f : exp2_fast(ml.x - t);
+                            top = t;
+                            sum = __fmaf_rn(fabsf(ml.y), z, sum * a);
+                            // (parts that are not lowered, where others are)
+                            if (E8 && is_low(ml.y) != any_low) (any_low ? z : a) *= LOWERED, any_low = true;
+                            y[0] = __fmaf_rn(u.x, z, y[0] * a), y[1] = __fmaf_rn(u.y, z, y[1] * a);
+                            y[2] = __fmaf_rn(u.z, z, y[2] * a), y[3] = __fmaf_rn(u.w, z, y[3] * a);
+                            y[4] = __fmaf_rn(w.x, z, y[4] * a), y[5] = __fmaf_rn(w.y, z, y[5] * a);
+                            y[6] = __fmaf_rn(w.z, z, y[6] * a), y[7] = __fmaf_rn(w.w, z, y[7] * a);
+                        }
+                    __syncwarp();                         // (put may write where the warp has read)
+                    if (on) put(h, d, top, sum, y, any_low);
                 }
-                if (me == 0) p.tickets[block1] = 0;
+            };
+            // A warp by itself joins a long pair in two stages, groups first: their last warps do it side by side.
+            const int count = block2 - block1 + 1;
+            int group = count, groups = 1, k0 = block1;
+            if (TW == 1 && count > GROUP) {
+                for (group = GROUP; group * group < count;) group *= 2;
+                groups = (count + group - 1) / group;
+                k0 = block1 + (team - block1) / group * group;
+            }
+            if (groups == 1) {
+                if (last_of(&p.tickets[block1], count)) join(block1, block2, 1, finish);
+            } else if (last_of(&p.tickets[TICKETS + place(k0)], min(group, block2 - k0 + 1))) {
+                join(k0, min(block2, k0 + group - 1), 1, [&](int h, int d, float top, float sum, float (&y)[8], bool any_low) {
+                    put_part(p.parts + place(k0) * PART, h, d, top, sum, y, any_low);
+                });
+                if (last_of(&p.tickets[block1], groups)) join(block1, block2, group, finish);
             }
         }
         together();
