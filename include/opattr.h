@@ -518,7 +518,7 @@ opattr_status opattr_match_noalloc(const opattr_kernels *kernels, const opattr_n
  * refers to is kept when a larger call outgrows it); as the calls themselves,
  * replays use the context's scratch, and are ordered with one another and with
  * its calls: on its stream, or by events.  Sizes and pointers are checked at the
- * call; offsets, sequence ids, lengths and page numbers live on the device
+ * call (the n of a cache's call is at most 2^31 - 1,025); offsets, sequence ids, lengths and page numbers live on the device
  * and are checked there.  A call that finds one of those out of range does
  * nothing (the cache's calls), or leaves out the rows concerned (the two
  * attention calls: a sequence id or length out of range gives rows of zeros,

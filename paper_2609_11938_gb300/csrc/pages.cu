@@ -478,19 +478,20 @@ k_append_rows8(opattr_cache8 c8, const int32_t *seqs, int n, const int32_t *offs
         }
         return;
     }
-    const int64_t all = ((int64_t)tokens / BLOCK + 2 * n) * parts;
+    const int64_t all = (tokens / BLOCK + 2ll * n) * parts;
     for (int64_t x = blockIdx.x; x < all; x += row_blocks) {
-        const int place = (int)(x / parts), part = (int)(x - (int64_t)place * parts);
+        const int64_t place = x / parts;
+        const int part = (int)(x - place * parts);
         // the last sequence whose places begin there or before, 32 at a time
         int i = 0;
         for (int m = n; m > 1;) {
             const int step = (m + 31) / 32, e = i + step * lane;
-            const bool le = step * lane < m && offsets[e] / BLOCK + 2 * e <= place;
+            const bool le = step * lane < m && offsets[e] / BLOCK + 2ll * e <= place;
             const int at = 31 - __clz(__ballot_sync(0xffffffffu, le));
             i += at * step;
             m = min(step, m - at * step);
         }
-        const int old = p.old[i], more = offsets[i + 1] - offsets[i], b = old / BLOCK + place - (offsets[i] / BLOCK + 2 * i);
+        const int old = p.old[i], more = offsets[i + 1] - offsets[i], b = (int)(old / BLOCK + place - (offsets[i] / BLOCK + 2ll * i));
         if (more == 0 || b > (old + more - 1) / BLOCK) continue;
         const int j = b / subs, page = kv.table[(int64_t)seqs[i] * kv.pages_per_seq + j];
         if (page < 0 || page >= kv.n_pages) continue;             // a table that was not consistent before the call
@@ -505,7 +506,7 @@ k_append_rows8(opattr_cache8 c8, const int32_t *seqs, int n, const int32_t *offs
 // One thread to a sequence, or to four new pages; of few, a block that is quick to begin.
 static unsigned plan_threads(int64_t n) { return n <= 256 ? 256 : PLAN_THREADS; }
 static opattr_status seqs_ok(const opattr_cache *kv, const int32_t *seqs, int32_t n) {
-    return cache_ok(kv) && n >= 0 && n <= kv->n_seqs && (n == 0 || seqs) ? OPATTR_OK : OPATTR_E_INVALID_ARG;
+    return cache_ok(kv) && n >= 0 && n <= std::min(kv->n_seqs, MOST_SEQS) && (n == 0 || seqs) ? OPATTR_OK : OPATTR_E_INVALID_ARG;
 }
 
 template <typename T>
@@ -513,7 +514,7 @@ static opattr_status rows8_of(Ctx &c, const opattr_cache8 &c8, const int32_t *se
                               const opattr_rows &k, const opattr_rows &v, const AppendPlan &p) {
     const opattr_cache &kv = c8.pages;
     // few places: their heads are shared out, so that every SM has some
-    const int64_t places = (int64_t)tokens / BLOCK + 2 * n, wave = 8 * sm_count(c);
+    const int64_t places = tokens / BLOCK + 2ll * n, wave = 8 * sm_count(c);
     const int parts = (int)std::max<int64_t>(1, std::min<int64_t>(wave / places, (2 * kv.kv_heads + COPY_THREADS / 32 - 1) / (COPY_THREADS / 32)));
     const unsigned rows = (unsigned)std::min<int64_t>(places * parts, 2 * wave);
     const unsigned shared = (unsigned)std::min<int64_t>((int64_t)n * kv.kv_heads, 2 * sm_count(c));

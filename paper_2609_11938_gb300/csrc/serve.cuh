@@ -30,6 +30,8 @@ constexpr int SILENT_PARTS = -1;
 
 constexpr int TICKETS = 4096;        // at most four blocks an SM, or their sixteen warps, count in them
 constexpr int ALL_TICKETS = 3 * TICKETS;   // and in two more each, where parts are joined in groups
+// Entries of a cache call: loops over them step past the last one by a block of threads at most, in 32 bits.
+constexpr int32_t MOST_SEQS = INT32_MAX - 1024;
 opattr_status serve_ready(Ctx &c, Serve &s);
 void serve_free(Serve &s);
 

@@ -16,7 +16,7 @@ opattr_status do_cache_attention(Ctx &c, Serve &s, const opattr_cache *kv, const
     if (window < 0 || sinks < 0 || (window == 0 && sinks > 0)) return OPATTR_E_INVALID_ARG;
     if (!cache_ok(kv) || n < 0 || q_heads < 1 || q_heads % kv->kv_heads || !isfinite(scale)) return OPATTR_E_INVALID_ARG;
     if (!rows_ok(*q, n, q_heads, kv->head_dim) || !rows_ok(*out, n, q_heads, kv->head_dim)) return OPATTR_E_INVALID_ARG;
-    if (!seqs && n > kv->n_seqs) return OPATTR_E_INVALID_ARG;
+    if (n > MOST_SEQS || (!seqs && n > kv->n_seqs)) return OPATTR_E_INVALID_ARG;
     if (n == 0) return OPATTR_OK;
     TokenArgs p{};
     p.kv = *kv;
