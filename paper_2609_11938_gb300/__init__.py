@@ -912,10 +912,9 @@ class Context:
         args = _PROMPT.pack(dtype, n_seqs, heads, kv_heads, dim, 1 if causal else 0, dim ** -0.5 if scale is None else scale,
                             0, tokens, k_tokens, *rq, *rk, *rv, *ro, p_qo, p_ko, p_lse)
         cur = self._enter()
-        lib = _lib or library()
         if window is not None:
-            return self._leave(cur, lib.opattr_attention_window(self.handle, args, window, sinks), "opattr_attention_window"), out, lse
-        return self._leave(cur, lib.opattr_attention(self.handle, args), "opattr_attention"), out, lse
+            return self._leave(cur, opattr_attention_window(self.handle, args, window, sinks), "opattr_attention_window"), out, lse
+        return self._leave(cur, opattr_attention(self.handle, args), "opattr_attention"), out, lse
 
     def _ends(self, tokens: int):
         """Offsets of one sequence, made on the device: a copy of host values would wait for it."""
@@ -984,10 +983,9 @@ class Context:
         p_seqs = self._i32(seqs, n, "seqs")
         args = (self.handle, by_ref, p_seqs, n, heads, _ROWS.pack(*rq), _ROWS.pack(*ro), p_lse, dim ** -0.5 if scale is None else scale)
         cur = self._enter()
-        lib = _lib or library()
         if window is not None:
-            return self._leave(cur, lib.opattr_cache_attention_window(*args, window, sinks), "opattr_cache_attention_window"), out, lse
-        return self._leave(cur, lib.opattr_cache_attention(*args), "opattr_cache_attention"), out, lse
+            return self._leave(cur, opattr_cache_attention_window(*args, window, sinks), "opattr_cache_attention_window"), out, lse
+        return self._leave(cur, opattr_cache_attention(*args), "opattr_cache_attention"), out, lse
 
     def cache_append(self, cache: KVCache, seqs, offsets, k, v) -> int:
         """Rows offsets[i] .. offsets[i + 1] of k and v ([tokens, kv_heads, dim])
@@ -1009,8 +1007,7 @@ class Context:
         n = seqs.shape[0]
         p_off = self._i32(offsets, n + 1, "offsets")
         cur = self._enter()
-        st = (_lib or library()).opattr_cache_append(self.handle, by_ref, p_seqs, n, p_off, k.shape[0],
-                                                     _ROWS.pack(*rk), _ROWS.pack(*rv))
+        st = opattr_cache_append(self.handle, by_ref, p_seqs, n, p_off, k.shape[0], _ROWS.pack(*rk), _ROWS.pack(*rv))
         return self._leave(cur, st, "opattr_cache_append")
 
     def cache_fork(self, cache: KVCache, src, dst) -> int:
