@@ -527,7 +527,11 @@ opattr_status opattr_match_noalloc(const opattr_kernels *kernels, const opattr_n
  * Values are bfloat16 or IEEE half (a cache's pages may hold them in 8 bits,
  * below); products are summed, and the softmax is held, in 32 bits; its weights
  * are rounded to the values' type before they are multiplied with the values
- * (to half where those are of 8 bits), and the results once at the end.  A key
+ * (to half where those are of 8 bits: by 2^-11 of a weight, or by 2^-33 of its
+ * row's largest, and one below that counts as 0 whatever its value), and the
+ * results once at the end.  In bfloat16 a row's values times their weights, as
+ * shares of its largest weight, may sum up to 2^120 before the division; over
+ * pages of 8 bits, to anything.  A key
  * outside a row's mask has no influence on it, whatever it holds. */
 typedef enum { OPATTR_BF16 = 0, OPATTR_F16 = 1, OPATTR_E4M3 = 2 /* pages of an opattr_cache8 alone */ } opattr_dtype;
 

@@ -33,8 +33,10 @@
 //
 // Pages of 8 bits (E8): half the bytes, so that what is done for each of them counts.  Codes become halves, exactly,
 // on the way into the products (a query of bfloat16 is brought into half's range by a power of
-// two); the scale of 16 keys multiplies their scores, and the sums of their values' products: no weight carries a
-// scale, so blocks may be as far apart as they like.  Where a warp's keys are whole sixteens, which
+// two); the scale of 16 keys multiplies their scores, and the sums of their values' products.  No weight carries a
+// scale, so that blocks may be far apart, but not as far as they like: a weight that is rounded to half is off by 2^-33 of
+// its row's largest at most, and below that it is 0, however large its block's values are.  (Weights of 16 keys brought to
+// their own power of two would keep them; their maximum is three exchanges between lanes, in every step.)  Where a warp's keys are whole sixteens, which
 // is checked once for a lane's 32 coming steps, its loads have no conditions; those of heads 64 or 128 wide have their
 // offsets in the instruction (2 sequences of 500,000 tokens, 40 heads of 128 on 8: 374 us with the conditions, 304
 // without), those of other widths add them, in kernels of their own (16 of 30,000, 32 heads of 96 on 8: 160, 145).  Where

@@ -121,3 +121,23 @@ def test_scales_of_others(ctx):  # noqa: F811
     c.v_scales[2, 0, 0] = math.nan
     out = ctx.cache_attention(c, None, q)[1]
     assert out[0, :2].isnan().all() and out[0, 2:].isfinite().all()
+
+
+@pytest.mark.parametrize("dim,heads", [(64, 4), (128, 4)])
+@pytest.mark.parametrize("bits", [10, 24, 30, 32, 33, 34, 40, 70])
+def test_small_weights_of_large_values(ctx, dim, heads, bits):  # noqa: F811
+    """A block of values 2^60 times the others' at weights 2^-bits of the largest: a weight is off by 2^-11 of
+    itself, or 2^-33 of the largest, whatever its value; one above 2^-32 of it still counts."""
+    k, v = torch.zeros((48, 1, dim), dtype=BF, device=DEV), torch.ones((48, 1, dim), dtype=BF, device=DEV)
+    k[:16, 0, 0], v[16:32, 0, ::2] = 1.0, 2.0 ** 60
+    # scores 0 and -bits, in powers of two
+    q = torch.zeros((1, heads, dim), dtype=BF, device=DEV)
+    q[:, :, 0] = 1.0
+    scale = bits * math.log(2.0)
+    c = filled(ctx, [48], k, v)
+    out, _ = check_attention(ctx, c, q, [0], scale=scale)
+    # (16 keys with weight 1, 32 with 2^-bits, 16 of which have the large values)
+    want = 2.0 ** (60 - bits) + 1.0
+    if bits < 33:
+        assert ((out[:, :, ::2].double() / want - 1).abs() < 2.0 ** -7 + 2.0 ** (bits - 33)).all()
+    assert ((out[:, :, 1::2].double() - 1.0).abs() < 2.0 ** -7).all()
