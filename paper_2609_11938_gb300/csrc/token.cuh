@@ -91,11 +91,19 @@ struct Eight {
 // window, 128 wide, 31.0 and 33.6).  Scales watched on the way took registers that are not there: 18 % where 12 heads of 128 share
 // keys.
 constexpr float LARGE = 0x1p96f, LOWERED = 0x1p-64f;
-// Pairs for each SM from which on a warp has pairs of its own (TW below; pages of 8 bits, and windows), us with all of a block's
-// warps at a pair and by themselves.  8 bits, 16 heads of 64: 608 pairs of 1,028 tokens 22 and 25, 1,216 39 and 40, 1,824
-// 54 and 53, 3,648 102 and 91; 32 heads of 128 on 8, 1,216 pairs 66 and 68, 1,824 89 and 85, 3,648 173 and 163.  16 bits through
-// a window of 256, 16 heads of 64: 448 pairs 15 and 19, 912 23 and 23, 1,824 37 and 31, 3,648 65 and 51; 32 of 128 on 8: 912 31
-// and 32, 1,824 52 and 46.
+// Pairs for each SM from which on a warp has pairs of its own (TW below; pages of 8 bits, and windows).  It pays where pairs are
+// short: a warp's time as a share of a block's, bfloat16, tokens (or window) a pair  256  1,024  4,096  32,768
+//   8 bits, 16 heads of 64, 1,232 pairs                                              1.08   0.99   1.02   1.02
+//                           3,664                                                    0.89   0.94   1.00   1.02
+//   32 of 128 on 8, 1,832                                                            0.99   1.01   1.02   1.02
+//                   3,656                                                            0.91   1.00   1.02   1.02
+//   64 of 64 on 4, 48 of 128 on 4, 3,652                                             0.79   0.90   0.97   1.00
+//   32 of 96 on 8, 3,656 (half 0.98 .. 1.10)                                         0.84   0.89   0.93   0.94
+//   through windows, those of 3,650 (96 wide 0.79 .. 1.12; 128 in half 0.74 .. 0.93) 0.72   0.89   0.97   1.01
+//   16 bits, windows, 16 of 64 and 32 of 128 on 8, 3,660                             0.84   0.98   1.00   1.00
+// (608 pairs of 64 wide 1,028 tokens 1.14; 912 of 128 through a window of 256 1.03.)  The host knows the room of a table, not what is in it:
+// to go by that too would cost short sequences in a large table up to a quarter, for 2 % of long ones.  Pages of 16 bits
+// without a window read with conditions in any case, and a warp by itself only loses: 64 wide 1.10 from 1,024 tokens on, 128 1.01.
 constexpr int own_pairs(int dp) { return dp == 64 ? 8 : 12; }
 
 struct TokenArgs {
