@@ -33,12 +33,12 @@ def test_many_rows(ctx, heads, dim, page, dtype):  # noqa: F811
     m.same(c)
 
 
-@pytest.mark.parametrize("page,heads,dim,dtype", [(64, 2, 64, BF), (128, 1, 128, HF), (32, 3, 32, BF)])
+@pytest.mark.parametrize("page,heads,dim,dtype,n", [(64, 2, 64, BF, 80), (128, 1, 128, HF, 80), (32, 3, 32, BF, 80), (32, 1, 16, BF, 2300)])
 @pytest.mark.parametrize("last", [3, 16, 17])
-def test_more_sharers_than_lanes(ctx, page, heads, dim, dtype, last):  # noqa: F811
-    """80 sequences hold one page; each goes on at its own place of it in one call, and the last, which
+def test_more_sharers_than_lanes(ctx, page, heads, dim, dtype, n, last):  # noqa: F811
+    """80 sequences, or 2,300, hold one page; each goes on at its own place of it in one call, and the last, which
     keeps it, behind fewer tokens than the others have."""
-    rng, g, n = random.Random(page + last), gen(page + last), 80
+    rng, g = random.Random(page + last), gen(page + last)
     c, m = fresh(ctx, 3 * n, page, heads, dim, n, 3)
     k, v = (randn(g, (page, heads, dim), dtype) for _ in range(2))
     both(ctx, c, m, [0], [page], k, v)
