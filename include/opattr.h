@@ -611,7 +611,8 @@ typedef struct {
 } opattr_cache;
 
 /* A cache whose pages hold 8 bits an element: `pages` with dtype OPATTR_E4M3,
- * and what follows it here.  Every call that takes a cache takes &c.pages of one.
+ * and what follows it here.  Every call that takes a cache takes &c.pages of one;
+ * that dtype alone says that more follows, so give it in no other opattr_cache.
  * The element that code x of a page stands for is x (4 bits of exponent, 3 of
  * mantissa, at most 448, NaN) times its block's scale, a block being
  * OPATTR_SCALE_TOKENS tokens of one head, from a multiple of that on:
@@ -668,7 +669,10 @@ opattr_status opattr_cache_fork(opattr_ctx *ctx, const opattr_cache *cache, cons
 
 /* Sequence seqs[i] (each once) keeps its first lengths[i] tokens (i32[n]
  * device, at most its length; may lie in the cache's own array; NULL: none), and
- * lets go of the pages past them.  Errors: as opattr_attention. */
+ * lets go of the pages past them.  Pages of 8 bits: tokens that are taken back
+ * leave the scale of the block that they shared with kept ones as it grew for
+ * them, and the kept ones' codes as they were rounded for it.
+ * Errors: as opattr_attention. */
 opattr_status opattr_cache_trim(opattr_ctx *ctx, const opattr_cache *cache, const int32_t *seqs,
                                 const int32_t *lengths, int32_t n);
 

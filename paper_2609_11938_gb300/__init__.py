@@ -1021,7 +1021,8 @@ class Context:
 
     def cache_trim(self, cache: KVCache, seqs, lengths=None) -> int:
         """Sequence seqs[i] keeps its first lengths[i] tokens (none: it is
-        freed), and the pages past them are let go (opattr_cache_trim)."""
+        freed), and the pages past them are let go (opattr_cache_trim).  In pages
+        of 8 bits a scale that grew for tokens that are taken back stays."""
         self._cache(cache)
         p_seqs = self._i32(seqs, None, "seqs")
         n = seqs.shape[0]

@@ -39,12 +39,12 @@
 // their own power of two would keep them; their maximum is three exchanges between lanes, in every step.)  Where a warp's keys are whole sixteens, which
 // is checked once for a lane's 32 coming steps, its loads have no conditions; those of heads 64 or 128 wide have their
 // offsets in the instruction (2 sequences of 500,000 tokens, 40 heads of 128 on 8: 374 us with the conditions, 304
-// without), those of other widths add them, in kernels of their own (16 of 30,000, 32 heads of 96 on 8: 160, 145).  Where
+// without), those of other widths add them, in kernels of their own (16 of 30,000, 32 heads of 96 on 8: 160, 150).  Where
 // pairs are many each warp has some of its own, and nobody waits for a block.
 // Through a window (WIN) the sixteens of keys that are not seen are left out of a sequence's steps; the first
 // ones have the sinks, the others begin where the window does.
-//   8 bits, bytes as above: 2 of 500,000, 40 heads of 128 on 8: 304 us, 6.8 TB/s; 64 of 1 .. 16,001, 32 heads on 8: 44 us,
-//   4.7, of which about 13 are the launch, first loads and joins; 200 of 4,096, 16 heads of 64: 279 us, 6.0.
+//   8 bits, bytes as above: 2 of 500,000, 40 heads of 128 on 8: 304 to 308 us, 6.7 TB/s; 64 of 1 .. 16,001, 32 heads on 8: 44 us,
+//   4.7, of which about 13 are the launch, first loads and joins; 200 of 4,096, 16 heads of 64: 276 us, 6.1.
 //   A window of 4,096 and 4 sinks, 16 bits: 96 of 1 .. 20,001, 32 heads of 128 on 8: 80 us, 6.2.
 // Tried for 8 bits: a ring of copies in shared memory, three to six steps ahead, in the place of loads into registers: 350 us
 // for the 304 at every depth, and 77 for 79 at 200 sequences of 64 wide heads.
