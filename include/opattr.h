@@ -623,7 +623,8 @@ typedef struct {
  * 2^-126 to 2^119 that takes the largest to 448 at most; one that had tokens
  * before keeps its scale where that is larger, and where it is not, their codes
  * are rounded anew for the larger one (exact, but for those below 2^-6 after
- * that, where scales are powers of two).  An element is rounded to nearest
+ * that, where scales are powers of two).  A query of bfloat16 counts exactly
+ * but for its elements below 2^-31 of its largest, which lose bits.  An element is rounded to nearest
  * even, one above 448 becomes 448, and one that is not finite NaN. */
 #define OPATTR_SCALE_TOKENS 16
 typedef struct {

@@ -193,8 +193,9 @@ __device__ __forceinline__ void query_halves(uint32_t (&r)[KC][8], float &back) 
         }
 #pragma unroll
     for (int e = 1; e < 4; e <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, e));
-    // the largest comes to 2^14 .. 2^15; both powers are normal numbers
-    const int e = max(-112, (int)(top >> 23) - 127);
+    // the largest comes to 2^14 .. 2^15; both powers are normal numbers, and so is `back` times the call's scale down to
+    // 2^-14 of that (rows below 2^-98 stay smaller: their least element, 2^-133, comes to 2^-21, which half has)
+    const int e = max(-98, (int)(top >> 23) - 127);
     const float up = __int_as_float((14 - e + 127) << 23);
     back = __int_as_float((e - 14 + 127) << 23);
 #pragma unroll

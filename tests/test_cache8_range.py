@@ -141,3 +141,15 @@ def test_small_weights_of_large_values(ctx, dim, heads, bits):  # noqa: F811
     if bits < 33:
         assert ((out[:, :, ::2].double() / want - 1).abs() < 2.0 ** -7 + 2.0 ** (bits - 33)).all()
     assert ((out[:, :, 1::2].double() - 1.0).abs() < 2.0 ** -7).all()
+
+
+@pytest.mark.parametrize("dim,heads", [(64, 4), (128, 12), (48, 2)])
+@pytest.mark.parametrize("small", [-98, -105, -112, -118, -124])
+@pytest.mark.parametrize("bits", [0, 6, 13])
+def test_small_queries_of_large_keys(ctx, dim, heads, small, bits):  # noqa: F811
+    """Queries near bfloat16's least numbers, keys large enough that their scores count, and a small scale."""
+    g, n = gen(-small + dim), 300
+    k = randn(g, (n, 2, dim), torch.float32).clamp(-3, 3).mul(2.0 ** min(126, -small + bits)).to(BF)
+    v = randn(g, (n, 2, dim), BF)
+    q = randn(g, (1, heads, dim), torch.float32).mul(2.0 ** small).to(BF)
+    check_attention(ctx, filled(ctx, [n], k, v), q, [0], scale=2.0 ** -bits)
