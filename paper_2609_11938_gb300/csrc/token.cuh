@@ -136,6 +136,12 @@ __device__ __forceinline__ float root(float x) {
     asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
+// The nearest finite number; NaN stays.
+__device__ __forceinline__ float within(float x) {
+    float r;
+    asm("min.NaN.f32 %0, %1, 0f7f7fffff;\n max.NaN.f32 %0, %0, 0fff7fffff;" : "=f"(r) : "f"(x));
+    return r;
+}
 // The larger of two, NaN where one is.
 __device__ __forceinline__ float max_nan(float x, float y) {
     float r;
@@ -613,7 +619,9 @@ __global__ void __launch_bounds__(TOKEN_THREADS, E8 ? Eight<DP, NT>::BLOCKS : NT
                     for (int f = 0; f < FR; ++f)
 #pragma unroll
                         for (int t = 0; t < NT; ++t) {
-                            const float k0 = ks[f] * cq[t][0], k1 = ks[f] * cq[t][1];
+                            float k0 = ks[f] * cq[t][0], k1 = ks[f] * cq[t][1];
+                            // (past 32 bits, where products of zero stay zero)
+                            if (level != 1.f) k0 = within(k0), k1 = within(k1);
                             x[f][t][0] *= k0, x[f][t][1] *= k1, x[f][t][2] *= k0, x[f][t][3] *= k1;
                         }
                     if (!vall) {

@@ -153,3 +153,23 @@ def test_small_queries_of_large_keys(ctx, dim, heads, small, bits):  # noqa: F81
     v = randn(g, (n, 2, dim), BF)
     q = randn(g, (1, heads, dim), torch.float32).mul(2.0 ** small).to(BF)
     check_attention(ctx, filled(ctx, [n], k, v), q, [0], scale=2.0 ** -bits)
+
+
+@pytest.mark.parametrize("dim,heads", [(64, 2), (128, 20), (80, 2)])
+@pytest.mark.parametrize("size", [1.0, -1.0])
+def test_products_of_zero(ctx, dim, heads, size):  # noqa: F811
+    """Scales whose product with a query's size leaves 32 bits: a key whose products are all zero has the score 0."""
+    n = 40
+    g = gen(dim)
+    k, v = torch.zeros((n, 2, dim), dtype=BF, device=DEV), randn(g, (n, 2, dim), BF)
+    k[:, :, 1] = 2.0 ** 100                             # (queries have zeros there)
+    k[7, :, 0], k[23, :, 0] = -size * 2.0 ** 100, -size * 2.0 ** 99
+    q = torch.zeros((1, heads, dim), dtype=BF, device=DEV)
+    q[:, :, 0] = size * 2.0 ** 100
+    c = filled(ctx, [n], k, v)
+    _, out, lse = ctx.cache_attention(c, None, q, need_lse=True)
+    ctx.check()
+    rest = [i for i in range(n) if i not in (7, 23)]
+    want = stands_for(c, 0)[1][rest].mean(0).repeat_interleave(heads // 2, 0)
+    assert ((out[0].double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -10 * v.abs().max()).all()
+    assert ((lse.double() - math.log(len(rest))).abs() <= 2.0 ** -18).all()
