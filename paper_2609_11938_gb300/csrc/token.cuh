@@ -87,7 +87,7 @@ struct Eight {
 // values from 2^113 on may leave 32 bits before.  A warp whose results come out at LARGE or more, or not finite, makes
 // them again, LOWERED times as large: 2^31 tokens of 2^128 stay below 2^(15 + 31 + 128 - 64) so, and small values beside them
 // lose 2^-86 a token.  Values below 2^49 are LARGE in no sum of 2^31 tokens.  All other calls pay a product for each 16
-// keys and a look at the results, 0 to 4 % (114 sequences of 2,060 tokens, 16 heads of 64: 87.1 us without, 87.9; half through a
+// keys and a look at the results, 0 to 4 % (114 sequences of 2,060 tokens, 16 heads of 64: 87.1 us without, 89.5; half through a
 // window, 128 wide, 31.0 and 33.6).  Scales watched on the way took registers that are not there: 18 % where 12 heads of 128 share
 // keys.
 constexpr float LARGE = 0x1p96f, LOWERED = 0x1p-64f;
